@@ -14,7 +14,10 @@
  * the window statistics from it), writes
  * each decoded token into its ring row (snap_cache_append, Sec. III-C), and
  * runs decode attention over the valid rows (snap_decode_attn; snap_decode_step
- * does both for one layer).
+ * does both for one layer).  Beside it stand rotary positions for the queries
+ * and keys that go in (snap_rope) and a paged cache of growing length, for
+ * layers that are not compressed and for sequences that are cut back to the
+ * budget later by the attention their rows received (snap_paged_*).
  *
  * Conventions shared by every call
  *  - Token positions are 0-based; a prompt of length L holds tokens 0..L-1 and
@@ -37,9 +40,10 @@
  *    n_topk entries, since those calls only write them, with the same values
  *    (L and min(K, |C|)).
  *  - Batch limits of the launch grids: n_seq * n_kv_heads <= 65535
- *    (snap_compress, snap_prefill, snap_prefill_attn) and n * n_q_heads <=
- *    65535 (snap_decode_attn, snap_decode_step); larger calls return
- *    SNAP_ERR_UNSUPPORTED (split the batch).
+ *    (snap_compress, snap_prefill, snap_prefill_attn, snap_paged_append,
+ *    snap_paged_evict) and n * n_q_heads <= 65535 (snap_decode_attn,
+ *    snap_decode_step, snap_paged_decode_attn, snap_paged_decode_step); larger
+ *    calls return SNAP_ERR_UNSUPPORTED (split the batch).
  */
 #ifndef SNAPSTREAM_H
 #define SNAPSTREAM_H
@@ -299,6 +303,173 @@ snap_status snap_decode_step_noalloc(const snap_params* p, const snap_cache* cac
 snap_status snap_advance(int32_t* pos, int32_t n_slots, int32_t n, const int32_t* slot_ids,
                          void* stream);
 
+/* ---- rotary positions ------------------------------------------------------
+ * The compression and attention calls take queries and keys that already carry
+ * their positions.  snap_rope puts them there: each pair (x1, x2) of a head's
+ * rotated dims turns by the angle position * f_i,
+ *   y1 = a (x1 cos - x2 sin),  y2 = a (x2 cos + x1 sin),
+ * with f_i = base^(-2i / rot_dim) changed by a rule for contexts longer than
+ * the model was trained on. */
+typedef enum {
+  SNAP_ROPE_HALVES = 0, /* pair i: dims (i, i + rot_dim / 2) of the rotated part */
+  SNAP_ROPE_PAIRS = 1   /* pair i: dims (2i, 2i + 1) of the rotated part         */
+} snap_rope_layout;
+
+typedef enum {
+  SNAP_ROPE_PLAIN = 0,    /* f_i                                                */
+  SNAP_ROPE_DIVIDE = 1,   /* f_i / factor: positions divided by factor          */
+  SNAP_ROPE_BY_TURNS = 2, /* w f_i + (1 - w) f_i / factor, w from the turns that
+                             pair i makes over orig_len positions: 0 up to
+                             low_turns, 1 from high_turns, linear between       */
+  SNAP_ROPE_BY_INDEX = 3  /* the same, w linear in i: 1 up to lo = max(0,
+                             floor(at(high_turns))), 0 from hi = min(rot_dim-1,
+                             ceil(at(low_turns))), at(t) the (real) index that
+                             makes t turns over orig_len positions              */
+} snap_rope_rule;
+
+typedef struct {
+  int32_t rot_start;  /* first rotated dim of a head                             */
+  int32_t rot_dim;    /* rotated dims: even, 2..128; the others are copied       */
+  int32_t layout;     /* snap_rope_layout                                        */
+  int32_t rule;       /* snap_rope_rule                                          */
+  float base;         /* > 1                                                     */
+  float factor;       /* >= 1 (every rule but PLAIN)                             */
+  float low_turns;    /* 0 < low_turns < high_turns (BY_TURNS, BY_INDEX)         */
+  float high_turns;
+  int32_t orig_len;   /* >= 1 (BY_TURNS, BY_INDEX)                               */
+  float amplitude;    /* a, > 0 (1: a rotation)                                  */
+} snap_rope_params;
+
+/* Heads to rotate: x -> y, [sequence][head][token][d] with any strides (in
+ * elements) of the first three; the d dims of a head are contiguous.  y may be
+ * x with the same strides (in place: only the rotated dims are touched);
+ * otherwise the memory x spans and the memory y spans must be disjoint.
+ * A stride of y is not 0 where its size is more than 1. */
+typedef struct {
+  const void* x;
+  void* y;
+  int64_t x_stride[3]; /* sequence, head, token */
+  int64_t y_stride[3];
+  int32_t n_heads;
+} snap_rope_heads;
+
+/* Rotates the heads of q and (unless NULL) of k, both of width d and type
+ * dtype (SNAP_F32 or SNAP_BF16), in one launch.  Token t < lengths[b] (max_len
+ * when lengths is NULL; lengths are clamped to [0, max_len]) of sequence b is
+ * at position pos[slot_ids[b]] + t, or at t when pos is NULL (slot_ids and
+ * n_slots are then not read); tokens past it are neither read nor written, nor
+ * are sequences whose slot id is outside [0, n_slots).  Angles are formed in
+ * 64 bits and the products in 32; each output is rounded once.  n_seq == 0 is a
+ * no-op. */
+snap_status snap_rope(const snap_rope_params* r, int32_t dtype, int32_t n_seq, int32_t max_len, int32_t d,
+                      const int32_t* pos, int32_t n_slots, const int32_t* slot_ids, const int32_t* lengths,
+                      const snap_rope_heads* q, const snap_rope_heads* k, void* stream);
+
+/* ---- paged cache -----------------------------------------------------------
+ * A cache of growing length beside the fixed one: layers that are not
+ * compressed at the end of prefill, and sequences that are cut back to the
+ * budget sink + recent + topk later, by the attention their rows received.
+ * Rows live in pages of page_size rows; row r of slot s is row r % page_size of
+ * page page_table[s][r / page_size], for every KV head alike.
+ *   k      [n_pages][n_kv_heads][page_size][d_qk] kv_dtype
+ *   v      [n_pages][n_kv_heads][page_size][d_v]  kv_dtype; NULL when v_in_k
+ *   k_scale, v_scale [n_slots][n_kv_heads] fp32: fp8 only, set by the caller
+ *   token  [n_pages][n_kv_heads][page_size] int32: the position of the token in
+ *          each row (eviction leaves each KV head its own tokens); NULL when
+ *          nothing is evicted
+ *   weight [n_pages][n_kv_heads][page_size] fp32: the attention the row has
+ *          received so far; NULL when it is not kept
+ *   page_table [n_slots][max_pages] int32
+ * A page id outside [0, n_pages) is a page that is not there: rows in it are
+ * not written and receive no attention.  Slots may share pages that none of
+ * them writes to, weighs or evicts from.
+ * Counters of a slot (device int32[n_slots], caller-owned, shared by every
+ * layer): rows[slot] the rows it holds, which is the row of the token being
+ * decoded; pos[slot] that token's position.  snap_advance moves each of them on
+ * after a step.  The two differ once rows have been evicted.
+ * Of snap_params the paged calls take the head layout, widths, types, sm_scale
+ * and kv_reuse, and eviction the budget; fp8_qk must be 0. */
+typedef struct {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  int32_t* token;
+  float* weight;
+  const int32_t* page_table;
+  int32_t n_slots;
+  int32_t n_pages;
+  int32_t page_size; /* a power of two, 16..4096 */
+  int32_t max_pages; /* max_pages * page_size <= 2^28 */
+} snap_paged_cache;
+
+/* Stores new tokens: token t < lengths[b] (max_len when lengths is NULL) of
+ * sequence b goes to row rows[slot] + t of its slot, with token = pos[slot] + t
+ * and weight = weight_new[b][g][t] (0 when weight_new is NULL or the value is
+ * not finite, as snap_compress's pooled_out is outside the candidates).
+ *   k_new [n][n_kv_heads][max_len][d_qk] in_dtype, v_new likewise (NULL when
+ *   v_in_k), at strides k_stride / v_stride (host arrays: sequence, head, token
+ *   in elements, multiples of 16 bytes; NULL: contiguous),
+ *   weight_new [n][n_kv_heads][max_len] fp32, contiguous.
+ * Sequences with rows[slot] < 0 and rows past the page table are skipped.  rows
+ * and pos are left as they are; pos may be NULL when the cache has no token
+ * array.  The sequences' slots must be distinct. */
+snap_status snap_paged_append(const snap_params* p, const snap_paged_cache* cache, const int32_t* rows,
+                              const int32_t* pos, int32_t n, const int32_t* slot_ids, const int32_t* lengths,
+                              int32_t max_len, const void* k_new, const int64_t* k_stride, const void* v_new,
+                              const int64_t* v_stride, const float* weight_new, void* stream);
+
+/* Bytes of workspace snap_paged_decode_attn / _step need for n sequences of at
+ * most max_rows rows (the new one included).  0 on invalid parameters. */
+size_t snap_paged_decode_workspace(const snap_params* p, int32_t n, int32_t max_rows, int32_t weigh);
+
+/* Attention of one new token per sequence (already stored) over rows
+ * [0, min(rows[slot] + 1, max_rows)) of its slot: out[b][h] =
+ * sum_j softmax_j(sm_scale q.k_j) v_j, zero for a sequence without rows.
+ * max_rows (host, at most max_pages * page_size) bounds the rows of every
+ * sequence of the call; it sizes the launch and the workspace, work follows the
+ * rows that are there.  weigh = 1: softmax_j summed over the query heads of each
+ * KV head is added to weight of row j (the slots of the call are then distinct).
+ *   q   [n][n_q_heads][d_qk] in_dtype, out [n][n_q_heads][d_v] out_dtype,
+ *   workspace >= snap_paged_decode_workspace(p, n, max_rows, weigh) bytes,
+ *             256-byte aligned; its contents on entry do not matter. */
+snap_status snap_paged_decode_attn(const snap_params* p, const snap_paged_cache* cache, const int32_t* rows, int32_t n,
+                                   const int32_t* slot_ids, int32_t max_rows, const void* q, void* out,
+                                   int32_t out_dtype, int32_t weigh, void* workspace, size_t ws_bytes, void* stream);
+
+/* snap_paged_append of one token per sequence (k_new [n][n_kv_heads][d_qk],
+ * v_new [n][n_kv_heads][d_v], contiguous; weight 0) followed by
+ * snap_paged_decode_attn: the same results and cache contents.  The slots of the
+ * call are distinct. */
+snap_status snap_paged_decode_step(const snap_params* p, const snap_paged_cache* cache, const int32_t* rows,
+                                   const int32_t* pos, int32_t n, const int32_t* slot_ids, int32_t max_rows,
+                                   const void* q, const void* k_new, const void* v_new, void* out, int32_t out_dtype,
+                                   int32_t weigh, void* workspace, size_t ws_bytes, void* stream);
+
+/* Bytes of workspace snap_paged_evict needs.  0 on invalid parameters. */
+size_t snap_paged_evict_workspace(const snap_params* p, int32_t n, int32_t max_rows);
+
+/* Cuts slots back to the budget B = sink + recent + topk, between two steps
+ * (rows[slot] rows held, pos[slot] the next position).  A slot of more than B
+ * rows keeps, per KV head, the rows with token < sink or token >= pos - recent
+ * (the first B of them by row, should there be more) and the heaviest others
+ * up to B rows in all (equal weights: the lower row; NaN and negative weights
+ * count as 0).  Kept rows below B stay where they are; the j-th kept row from B
+ * on moves to the j-th row below B that was not kept, with its token and weight.
+ * Rows from B on are left as they were.
+ *   rows_out [n_slots] int32: min(rows, B) of the call's slots (the same from
+ *            every layer; rows itself is left, so that every layer sees it),
+ *   kept_out optional [n][n_kv_heads][B] int32: the row whose contents are now
+ *            in each row, -1 past the rows held (NULL to skip),
+ *   max_rows (host, at most max_pages * page_size): rows past it are not looked at,
+ *   workspace >= snap_paged_evict_workspace(p, n, max_rows) bytes, 256-byte
+ *             aligned; its contents on entry do not matter.
+ * The cache needs token and weight; the slots must be distinct and must not
+ * share pages; rows_out must not alias rows. */
+snap_status snap_paged_evict(const snap_params* p, const snap_paged_cache* cache, const int32_t* rows,
+                             const int32_t* pos, int32_t* rows_out, int32_t n, const int32_t* slot_ids,
+                             int32_t max_rows, int32_t* kept_out, void* workspace, size_t ws_bytes, void* stream);
+
 /* Device-side checks of the debug build (libsnapstream_debug.so, built with
  * SNAP_DEBUG_CHECKS): its kernels test the invariants their indexing rests on
  * (keys inside the prompt, kept tokens inside the candidates, rows inside the
@@ -310,7 +481,8 @@ snap_status snap_advance(int32_t* pos, int32_t n_slots, int32_t n, const int32_t
  * 2 selection past K_eff, 4 kept token outside the candidates, 8 re-scored key
  * outside the candidates, 16 decode rows past the budget, 32 new token's row
  * outside the sink/ring rows, 64 too many split-K chunks, 128 appended row
- * outside the sink/ring rows, 256 prefill block outside the prompt. */
+ * outside the sink/ring rows, 256 prefill block outside the prompt, 512 paged
+ * work item past the workspace, 1024 evicted rows past their move list. */
 snap_status snap_debug_checks(uint32_t* flags, int32_t reset);
 
 /* Static description of a status code. */

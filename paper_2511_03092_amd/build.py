@@ -11,7 +11,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsnapstream.so")
 DEBUG_LIB = os.path.join(HERE, "libsnapstream_debug.so")
-SOURCES = ["abi.hip", "compress.hip", "decode.hip", "prefill.hip", "noalloc.hip"]
+SOURCES = ["abi.hip", "compress.hip", "decode.hip", "prefill.hip", "noalloc.hip",
+           "rope.hip", "paged.hip", "evict.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 

@@ -99,6 +99,84 @@ static snap_status check_cache(const snap_params* p, const snap_cache* c) {
   return SNAP_OK;
 }
 
+// One operand of snap_rope: strides that keep distinct outputs apart, and x and
+// y either the same or apart.
+static snap_status check_rope_heads(const snap_rope_heads* h, const char* name, int32_t n_seq, int32_t max_len, int32_t d,
+                                    int elt) {
+  if (h->n_heads < 1) return fail(SNAP_ERR_INVALID_ARG, "%s: n_heads must be >= 1", name);
+  if (!h->x || !h->y) return fail(SNAP_ERR_INVALID_ARG, "%s: x or y is NULL", name);
+  if (((uintptr_t)h->x | (uintptr_t)h->y) & (uintptr_t)(elt - 1))
+    return fail(SNAP_ERR_INVALID_ARG, "%s: x or y is not aligned to its elements", name);
+  const int64_t size[3] = {n_seq, h->n_heads, max_len};
+  // first and last byte (from x, y) that the strides reach; a stride beyond
+  // 2^40 elements reaches nothing that exists
+  __int128 lo[2] = {0, 0}, hi[2] = {d, d};
+  for (int i = 0; i < 3; ++i) {
+    if (size[i] > 1 && h->y_stride[i] == 0) return fail(SNAP_ERR_INVALID_ARG, "%s: a stride of y is 0", name);
+    const int64_t st[2] = {h->x_stride[i], h->y_stride[i]};
+    for (int o = 0; o < 2; ++o) {
+      if (size[i] > 1 && (st[o] > ((int64_t)1 << 40) || st[o] < -((int64_t)1 << 40)))
+        return fail(SNAP_ERR_INVALID_ARG, "%s: a stride is beyond 2^40 elements", name);
+      const __int128 reach = size[i] > 1 ? (__int128)(size[i] - 1) * st[o] : 0;
+      (reach < 0 ? lo[o] : hi[o]) += reach;
+    }
+  }
+  bool same = h->x == h->y;
+  for (int i = 0; i < 3; ++i) same = same && (size[i] == 1 || h->x_stride[i] == h->y_stride[i]);
+  const __int128 x0 = (__int128)(uintptr_t)h->x + lo[0] * elt, x1 = (__int128)(uintptr_t)h->x + hi[0] * elt;
+  const __int128 y0 = (__int128)(uintptr_t)h->y + lo[1] * elt, y1 = (__int128)(uintptr_t)h->y + hi[1] * elt;
+  if (!same && x0 < y1 && y0 < x1)
+    return fail(SNAP_ERR_INVALID_ARG, "%s: x and y overlap and are not the same", name);
+  return SNAP_OK;
+}
+
+static snap_status check_paged(const snap_params* p, const snap_paged_cache* c) {
+  if (p->fp8_qk) return fail(SNAP_ERR_UNSUPPORTED, "the paged cache has no fp8 query products (fp8_qk)");
+  if (!c) return fail(SNAP_ERR_INVALID_ARG, "cache is NULL");
+  if (c->n_slots < 1 || c->n_pages < 1 || c->max_pages < 1)
+    return fail(SNAP_ERR_INVALID_ARG, "cache n_slots, n_pages and max_pages must be >= 1 (got %d, %d, %d)", c->n_slots,
+                c->n_pages, c->max_pages);
+  if (c->page_size < 16 || c->page_size > 4096 || (c->page_size & (c->page_size - 1)))
+    return fail(SNAP_ERR_UNSUPPORTED, "page_size must be a power of two in [16, 4096] (got %d)", c->page_size);
+  if ((long long)c->max_pages * c->page_size > (1 << 28))
+    return fail(SNAP_ERR_INVALID_ARG, "max_pages * page_size exceeds 2^28 rows");
+  if (!c->page_table) return fail(SNAP_ERR_INVALID_ARG, "cache page_table is NULL");
+  if (!c->k || !aligned16(c->k)) return fail(SNAP_ERR_INVALID_ARG, "cache k is NULL or not 16-byte aligned");
+  if (!p->v_in_k && (!c->v || !aligned16(c->v)))
+    return fail(SNAP_ERR_INVALID_ARG, "cache v is NULL or not 16-byte aligned");
+  if (p->kv_dtype == SNAP_FP8_E4M3 && (!c->k_scale || (!p->v_in_k && !c->v_scale)))
+    return fail(SNAP_ERR_INVALID_ARG, "an fp8 cache needs k_scale and v_scale");
+  return SNAP_OK;
+}
+
+static snap_status check_max_rows(const snap_paged_cache* c, int32_t max_rows) {
+  if (max_rows < 1 || (long long)max_rows > (long long)c->max_pages * c->page_size)
+    return fail(SNAP_ERR_INVALID_ARG, "max_rows must be in [1, max_pages * page_size = %lld] (got %d)",
+                (long long)c->max_pages * c->page_size, max_rows);
+  return SNAP_OK;
+}
+
+// Checks of snap_paged_decode_attn and, but for the new token, of
+// snap_paged_decode_step (n > 0).
+static snap_status check_paged_decode(const snap_params* p, const snap_paged_cache* c, const int32_t* rows, int32_t n,
+                                      const int32_t* slot_ids, int32_t max_rows, const void* q, void* out,
+                                      int32_t out_dtype, int32_t weigh, void* workspace, size_t ws_bytes) {
+  snap_status st = check_max_rows(c, max_rows);
+  if (st != SNAP_OK) return st;
+  if ((long long)n * p->n_q_heads > kMaxGridY)
+    return fail(SNAP_ERR_UNSUPPORTED, "n * n_q_heads must be at most %d", kMaxGridY);
+  if (!rows || !slot_ids) return fail(SNAP_ERR_INVALID_ARG, "rows/slot_ids NULL");
+  if (!q || !aligned16(q)) return fail(SNAP_ERR_INVALID_ARG, "q is NULL or not 16-byte aligned");
+  if (!out || !aligned16(out)) return fail(SNAP_ERR_INVALID_ARG, "out is NULL or not 16-byte aligned");
+  if (out_dtype != SNAP_F32 && out_dtype != SNAP_BF16) return fail(SNAP_ERR_INVALID_ARG, "out_dtype must be F32 or BF16");
+  if (weigh != 0 && weigh != 1) return fail(SNAP_ERR_INVALID_ARG, "weigh must be 0 or 1");
+  if (weigh && !c->weight) return fail(SNAP_ERR_INVALID_ARG, "weigh needs the cache's weight array");
+  const size_t need = paged_geometry(*p, n, max_rows, weigh != 0).bytes;
+  if (!workspace || ((uintptr_t)workspace & 255u) || ws_bytes < need)
+    return fail(SNAP_ERR_WORKSPACE, "workspace needs %zu bytes, 256-byte aligned (got %zu)", need, ws_bytes);
+  return SNAP_OK;
+}
+
 }  // namespace snap
 
 using namespace snap;
@@ -319,6 +397,150 @@ snap_status snap_decode_step_noalloc(const snap_params* p, const snap_cache* cac
   return st;
 }
 
+snap_status snap_rope(const snap_rope_params* r, int32_t dtype, int32_t n_seq, int32_t max_len, int32_t d,
+                      const int32_t* pos, int32_t n_slots, const int32_t* slot_ids, const int32_t* lengths,
+                      const snap_rope_heads* q, const snap_rope_heads* k, void* stream) {
+  g_err[0] = 0;
+  if (!r) return fail(SNAP_ERR_INVALID_ARG, "rope params is NULL");
+  if (dtype != SNAP_F32 && dtype != SNAP_BF16) return fail(SNAP_ERR_INVALID_ARG, "dtype must be F32 or BF16");
+  if (d < 2 || d > 4096) return fail(SNAP_ERR_INVALID_ARG, "d must be in [2, 4096] (got %d)", d);
+  if (r->rot_dim < 2 || r->rot_dim > 2 * kRopeMaxPairs || (r->rot_dim & 1))
+    return fail(SNAP_ERR_INVALID_ARG, "rot_dim must be even in [2, %d] (got %d)", 2 * kRopeMaxPairs, r->rot_dim);
+  if (r->rot_start < 0 || r->rot_start > d - r->rot_dim)
+    return fail(SNAP_ERR_INVALID_ARG, "the rotated dims [%d, +%d) are not within d = %d", r->rot_start, r->rot_dim, d);
+  if (r->layout != SNAP_ROPE_HALVES && r->layout != SNAP_ROPE_PAIRS) return fail(SNAP_ERR_INVALID_ARG, "unknown rope layout");
+  if (r->rule < SNAP_ROPE_PLAIN || r->rule > SNAP_ROPE_BY_INDEX) return fail(SNAP_ERR_INVALID_ARG, "unknown rope rule");
+  if (!isfinite(r->base) || !(r->base > 1.f)) return fail(SNAP_ERR_INVALID_ARG, "rope base must be finite and > 1");
+  if (!isfinite(r->amplitude) || !(r->amplitude > 0.f))
+    return fail(SNAP_ERR_INVALID_ARG, "rope amplitude must be finite and > 0");
+  if (r->rule != SNAP_ROPE_PLAIN && (!isfinite(r->factor) || !(r->factor >= 1.f)))
+    return fail(SNAP_ERR_INVALID_ARG, "rope factor must be finite and >= 1");
+  if (r->rule == SNAP_ROPE_BY_TURNS || r->rule == SNAP_ROPE_BY_INDEX) {
+    if (!isfinite(r->high_turns) || !(r->low_turns > 0.f) || !(r->high_turns > r->low_turns))
+      return fail(SNAP_ERR_INVALID_ARG, "need 0 < low_turns < high_turns");
+    if (r->orig_len < 1) return fail(SNAP_ERR_INVALID_ARG, "orig_len must be >= 1");
+  }
+  if (n_seq < 0) return fail(SNAP_ERR_INVALID_ARG, "n_seq must be >= 0");
+  if (n_seq == 0) return SNAP_OK;
+  if (max_len < 1 || max_len > (1 << 28)) return fail(SNAP_ERR_INVALID_ARG, "max_len must be in [1, 2^28]");
+  if ((long long)n_seq * max_len > (1ll << 31) / d)  // at most a thread per token and dim of a head
+    return fail(SNAP_ERR_UNSUPPORTED, "n_seq * max_len * d must be at most 2^31 (split the batch)");
+  if (pos && (!slot_ids || n_slots < 1)) return fail(SNAP_ERR_INVALID_ARG, "pos needs slot_ids and n_slots >= 1");
+  if (!q) return fail(SNAP_ERR_INVALID_ARG, "q is NULL");
+  const int elt = dtype == SNAP_F32 ? 4 : 2;
+  snap_status st = check_rope_heads(q, "q", n_seq, max_len, d, elt);
+  if (st != SNAP_OK) return st;
+  if (k && (st = check_rope_heads(k, "k", n_seq, max_len, d, elt)) != SNAP_OK) return st;
+  if ((long long)q->n_heads + (k ? k->n_heads : 0) > (1 << 20))
+    return fail(SNAP_ERR_UNSUPPORTED, "at most 2^20 heads");
+  st = launch_rope(*r, dtype, n_seq, max_len, d, pos, n_slots, slot_ids, lengths, q, k, (hipStream_t)stream);
+  if (st == SNAP_ERR_HIP) set_error("kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+  return st;
+}
+
+snap_status snap_paged_append(const snap_params* p, const snap_paged_cache* cache, const int32_t* rows,
+                              const int32_t* pos, int32_t n, const int32_t* slot_ids, const int32_t* lengths,
+                              int32_t max_len, const void* k_new, const int64_t* k_stride, const void* v_new,
+                              const int64_t* v_stride, const float* weight_new, void* stream) {
+  g_err[0] = 0;
+  snap_status st = check_params(p);
+  if (st != SNAP_OK) return st;
+  if ((st = check_paged(p, cache)) != SNAP_OK) return st;
+  if (n < 0) return fail(SNAP_ERR_INVALID_ARG, "n must be >= 0");
+  if (n == 0) return SNAP_OK;
+  if (max_len < 1 || max_len > (1 << 28)) return fail(SNAP_ERR_INVALID_ARG, "max_len must be in [1, 2^28]");
+  if ((long long)n * p->n_kv_heads > kMaxGridY)
+    return fail(SNAP_ERR_UNSUPPORTED, "n * n_kv_heads must be at most %d", kMaxGridY);
+  if (!rows || !slot_ids) return fail(SNAP_ERR_INVALID_ARG, "rows/slot_ids NULL");
+  if (cache->token && !pos) return fail(SNAP_ERR_INVALID_ARG, "a cache with a token array needs pos");
+  if (!k_new || !aligned16(k_new)) return fail(SNAP_ERR_INVALID_ARG, "k_new is NULL or not 16-byte aligned");
+  if (!p->v_in_k && (!v_new || !aligned16(v_new)))
+    return fail(SNAP_ERR_INVALID_ARG, "v_new is NULL or not 16-byte aligned");
+  const int per16 = p->in_dtype == SNAP_F32 ? 4 : 8;
+  for (int i = 0; i < 3; ++i)
+    if ((k_stride && k_stride[i] % per16) || (!p->v_in_k && v_stride && v_stride[i] % per16))
+      return fail(SNAP_ERR_INVALID_ARG, "strides of k_new / v_new must be multiples of 16 bytes");
+  st = launch_paged_append(*p, *cache, rows, pos, n, slot_ids, lengths, max_len, k_new, k_stride, v_new, v_stride,
+                           weight_new, (hipStream_t)stream);
+  if (st == SNAP_ERR_HIP) set_error("kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+  return st;
+}
+
+size_t snap_paged_decode_workspace(const snap_params* p, int32_t n, int32_t max_rows, int32_t weigh) {
+  if (check_params(p) != SNAP_OK || n < 0 || max_rows < 1 || max_rows > (1 << 28)) return 0;
+  if ((long long)n * p->n_q_heads > kMaxGridY) return 0;
+  return paged_geometry(*p, n, max_rows, weigh != 0).bytes;
+}
+
+snap_status snap_paged_decode_attn(const snap_params* p, const snap_paged_cache* cache, const int32_t* rows, int32_t n,
+                                   const int32_t* slot_ids, int32_t max_rows, const void* q, void* out,
+                                   int32_t out_dtype, int32_t weigh, void* workspace, size_t ws_bytes, void* stream) {
+  g_err[0] = 0;
+  snap_status st = check_params(p);
+  if (st != SNAP_OK) return st;
+  if ((st = check_paged(p, cache)) != SNAP_OK) return st;
+  if (n < 0) return fail(SNAP_ERR_INVALID_ARG, "n must be >= 0");
+  if (n == 0) return SNAP_OK;
+  st = check_paged_decode(p, cache, rows, n, slot_ids, max_rows, q, out, out_dtype, weigh, workspace, ws_bytes);
+  if (st != SNAP_OK) return st;
+  st = launch_paged_decode(*p, *cache, rows, nullptr, n, slot_ids, max_rows, q, nullptr, nullptr, out, out_dtype,
+                           weigh != 0, workspace, (hipStream_t)stream);
+  if (st == SNAP_ERR_HIP) set_error("kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+  return st;
+}
+
+snap_status snap_paged_decode_step(const snap_params* p, const snap_paged_cache* cache, const int32_t* rows,
+                                   const int32_t* pos, int32_t n, const int32_t* slot_ids, int32_t max_rows,
+                                   const void* q, const void* k_new, const void* v_new, void* out, int32_t out_dtype,
+                                   int32_t weigh, void* workspace, size_t ws_bytes, void* stream) {
+  g_err[0] = 0;
+  snap_status st = check_params(p);
+  if (st != SNAP_OK) return st;
+  if ((st = check_paged(p, cache)) != SNAP_OK) return st;
+  if (n < 0) return fail(SNAP_ERR_INVALID_ARG, "n must be >= 0");
+  if (n == 0) return SNAP_OK;
+  st = check_paged_decode(p, cache, rows, n, slot_ids, max_rows, q, out, out_dtype, weigh, workspace, ws_bytes);
+  if (st != SNAP_OK) return st;
+  if (cache->token && !pos) return fail(SNAP_ERR_INVALID_ARG, "a cache with a token array needs pos");
+  if (!k_new || !aligned16(k_new)) return fail(SNAP_ERR_INVALID_ARG, "k_new is NULL or not 16-byte aligned");
+  if (!p->v_in_k && (!v_new || !aligned16(v_new)))
+    return fail(SNAP_ERR_INVALID_ARG, "v_new is NULL or not 16-byte aligned");
+  st = launch_paged_decode(*p, *cache, rows, pos, n, slot_ids, max_rows, q, k_new, v_new, out, out_dtype, weigh != 0,
+                           workspace, (hipStream_t)stream);
+  if (st == SNAP_ERR_HIP) set_error("kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+  return st;
+}
+
+size_t snap_paged_evict_workspace(const snap_params* p, int32_t n, int32_t max_rows) {
+  if (check_params(p) != SNAP_OK || n < 0 || max_rows < 1 || max_rows > (1 << 28)) return 0;
+  if ((long long)n * p->n_kv_heads > kMaxGridY) return 0;
+  return evict_geometry(*p, n, max_rows).bytes;
+}
+
+snap_status snap_paged_evict(const snap_params* p, const snap_paged_cache* cache, const int32_t* rows,
+                             const int32_t* pos, int32_t* rows_out, int32_t n, const int32_t* slot_ids,
+                             int32_t max_rows, int32_t* kept_out, void* workspace, size_t ws_bytes, void* stream) {
+  g_err[0] = 0;
+  snap_status st = check_params(p);
+  if (st != SNAP_OK) return st;
+  if ((st = check_paged(p, cache)) != SNAP_OK) return st;
+  if (!cache->token || !cache->weight) return fail(SNAP_ERR_INVALID_ARG, "eviction needs the cache's token and weight arrays");
+  if (n < 0) return fail(SNAP_ERR_INVALID_ARG, "n must be >= 0");
+  if (n == 0) return SNAP_OK;
+  if ((st = check_max_rows(cache, max_rows)) != SNAP_OK) return st;
+  if ((long long)n * p->n_kv_heads > kMaxGridY)
+    return fail(SNAP_ERR_UNSUPPORTED, "n * n_kv_heads must be at most %d", kMaxGridY);
+  if (!rows || !pos || !rows_out || !slot_ids) return fail(SNAP_ERR_INVALID_ARG, "rows/pos/rows_out/slot_ids NULL");
+  if (rows_out == rows) return fail(SNAP_ERR_INVALID_ARG, "rows_out must not alias rows");
+  const size_t need = evict_geometry(*p, n, max_rows).bytes;
+  if (!workspace || ((uintptr_t)workspace & 255u) || ws_bytes < need)
+    return fail(SNAP_ERR_WORKSPACE, "workspace needs %zu bytes, 256-byte aligned (got %zu)", need, ws_bytes);
+  st = launch_paged_evict(*p, *cache, rows, pos, rows_out, n, slot_ids, max_rows, kept_out, workspace,
+                          (hipStream_t)stream);
+  if (st == SNAP_ERR_HIP) set_error("kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+  return st;
+}
+
 snap_status snap_debug_checks(uint32_t* flags, int32_t reset) {
   g_err[0] = 0;
   if (!flags) return fail(SNAP_ERR_INVALID_ARG, "flags is NULL");
@@ -326,10 +548,11 @@ snap_status snap_debug_checks(uint32_t* flags, int32_t reset) {
 #ifdef SNAP_DEBUG_CHECKS
   if (hipDeviceSynchronize() != hipSuccess) return fail(SNAP_ERR_HIP, "hipDeviceSynchronize failed");
   const uint32_t c = debug_flags_compress(reset != 0), d = debug_flags_decode(reset != 0),
-                 f = debug_flags_prefill(reset != 0);
-  if (c == 0xffffffffu || d == 0xffffffffu || f == 0xffffffffu)
+                 f = debug_flags_prefill(reset != 0), g = debug_flags_paged(reset != 0),
+                 e = debug_flags_evict(reset != 0);
+  if (c == 0xffffffffu || d == 0xffffffffu || f == 0xffffffffu || g == 0xffffffffu || e == 0xffffffffu)
     return fail(SNAP_ERR_HIP, "reading the check words failed");
-  *flags = c | d | f;
+  *flags = c | d | f | g | e;
   return SNAP_OK;
 #else
   (void)reset;

@@ -1,0 +1,192 @@
+// rope.hip -- rotary positions (Sec. III-B: keys are cached after positional
+// encoding and never re-encoded): q and k heads turned pair by pair, from the
+// layout a projection leaves them in to the one the attention calls take.
+//
+// Angles.  position * f is up to 2^31 radians and only its fraction of a turn
+// matters, so the product, its rounding to a quarter turn and the remainder are
+// formed in 64 bits (the remainder is exact); sine and cosine of the remainder,
+// at most an eighth of a turn, are then Taylor sums in 32 bits: the terms left
+// out are under 2^-29 (x^11 / 11! and x^12 / 12! at pi/4).
+#include <math.h>
+
+#include "snap_internal.h"
+
+namespace snap {
+
+struct RopeArgs {
+  const void* x[2];
+  void* y[2];
+  int64_t xs[2][3], ys[2][3];  // sequence, head, token strides (elements)
+  int heads[2];
+  int n, max_len, d, rot_start, rot, pairs, n_slots, in_place, slices;
+  const int32_t* pos;
+  const int32_t* slot_ids;
+  const int32_t* lengths;
+  float amp;
+  double turns[kRopeMaxPairs];  // turns a position of each pair
+};
+
+// amp * (cos, sin) of `turns` turns
+__device__ __forceinline__ void turn_of(double turns, float amp, float& c, float& s) {
+  const double quarter = __builtin_rint(turns * 4.0);
+  const float x = (float)(__builtin_fma(-0.25, quarter, turns) * 6.283185307179586476925);
+  const float x2 = x * x;
+  float sn = fmaf(x2, 2.7557319e-6f, -1.9841270e-4f);  // 1/9!, -1/7!
+  sn = fmaf(x2, sn, 8.3333333e-3f);
+  sn = fmaf(x2, sn, -1.6666667e-1f);
+  sn = fmaf(x * x2, sn, x);
+  float cs = fmaf(x2, -2.7557319e-7f, 2.4801587e-5f);  // -1/10!, 1/8!
+  cs = fmaf(x2, cs, -1.3888889e-3f);
+  cs = fmaf(x2, cs, 4.1666667e-2f);
+  cs = fmaf(x2, cs, -0.5f);
+  cs = fmaf(x2, cs, 1.f);
+  // |turns| * 4 < 2^34: the quarter's last two bits by its remainder mod 4
+  const int q = (int)(quarter - 4.0 * __builtin_floor(quarter * 0.25));
+  const float a = (q & 1) ? sn : cs, b = (q & 1) ? cs : sn;
+  c = amp * ((q == 1 || q == 2) ? -a : a);
+  s = amp * (q >= 2 ? -b : b);
+}
+
+// The token of flat index i: its sequence, whether it is there, its position.
+struct RopeToken {
+  int b, t;
+  bool live;
+  double position;
+};
+__device__ __forceinline__ RopeToken rope_token(const RopeArgs& a, int64_t i) {
+  RopeToken k;
+  k.b = (int)(i / a.max_len);
+  k.t = (int)(i - (int64_t)k.b * a.max_len);
+  k.live = !a.lengths || k.t < a.lengths[k.b];
+  int start = 0;
+  if (a.pos) {
+    const int slot = a.slot_ids[k.b];
+    if (slot < 0 || slot >= a.n_slots)
+      k.live = false;
+    else
+      start = a.pos[slot];
+  }
+  k.position = (double)start + (double)k.t;
+  return k;
+}
+
+template <typename T>
+__device__ __forceinline__ float rope_get(const T* p) {
+  if constexpr (sizeof(T) == 2)
+    return bf16_bits_to_f32(*p);
+  else
+    return *p;
+}
+template <typename T>
+__device__ __forceinline__ void rope_set(T* p, float v) {
+  if constexpr (sizeof(T) == 2)
+    *p = (uint16_t)f32_to_bf16_bits(v);
+  else
+    *p = v;
+}
+
+// One (token, pair or unrotated dim) per thread, over the heads of a slice.
+template <typename T>
+__global__ __launch_bounds__(256) void rope_any(RopeArgs a) {
+  const int np = a.rot / 2, cols = np + (a.in_place ? 0 : a.d - a.rot);
+  const int64_t i = (int64_t)bid_x() * 256 + tid();
+  if (i >= (int64_t)a.n * a.max_len * cols) return;
+  const int col = (int)(i % cols);
+  const RopeToken k = rope_token(a, i / cols);
+  if (!k.live) return;
+  int d1, d2 = -1;
+  float c = 1.f, s = 0.f;
+  if (col < np) {
+    d1 = a.rot_start + (a.pairs ? 2 * col : col);
+    d2 = d1 + (a.pairs ? 1 : np);
+    turn_of(k.position * a.turns[col], a.amp, c, s);
+  } else {
+    d1 = col - np;
+    if (d1 >= a.rot_start) d1 += a.rot;
+  }
+  for (int h = bid_y(); h < a.heads[0] + a.heads[1]; h += a.slices) {
+    const int o = h < a.heads[0] ? 0 : 1, hh = o ? h - a.heads[0] : h;
+    const T* x = (const T*)a.x[o] + k.b * a.xs[o][0] + hh * a.xs[o][1] + k.t * a.xs[o][2];
+    T* y = (T*)a.y[o] + k.b * a.ys[o][0] + hh * a.ys[o][1] + k.t * a.ys[o][2];
+    if (d2 < 0) {
+      y[d1] = x[d1];
+    } else {
+      const float x1 = rope_get(x + d1), x2 = rope_get(x + d2);
+      rope_set(y + d1, fmaf(x1, c, -(x2 * s)));
+      rope_set(y + d2, fmaf(x2, c, x1 * s));
+    }
+  }
+}
+
+// ---------------------------------------------------------------- host side
+// Turns a position of every pair, by the rule (64 bits and more: far positions
+// multiply them by up to 2^31).
+static void rope_turns(const snap_rope_params& r, double* out) {
+  const int np = r.rot_dim / 2;
+  const long double two_pi = 6.283185307179586476925286766559L;
+  const long double step = powl((long double)r.base, -2.0L / r.rot_dim);
+  double lo = 0, hi = 0;
+  if (r.rule == SNAP_ROPE_BY_INDEX) {
+    const double per = r.rot_dim / (2.0 * log((double)r.base)), circle = 6.283185307179586476925;
+    lo = fmax(0.0, floor(per * log(r.orig_len / (circle * r.high_turns))));
+    hi = fmin(r.rot_dim - 1.0, ceil(per * log(r.orig_len / (circle * r.low_turns))));
+  }
+  long double f = 1.0L;
+  for (int i = 0; i < np; ++i, f *= step) {
+    long double w = 1.0L;  // share of the unchanged frequency
+    if (r.rule == SNAP_ROPE_DIVIDE) {
+      w = 0.0L;
+    } else if (r.rule == SNAP_ROPE_BY_TURNS) {
+      w = (r.orig_len * f / two_pi - r.low_turns) / ((long double)r.high_turns - r.low_turns);
+    } else if (r.rule == SNAP_ROPE_BY_INDEX) {
+      w = 1.0L - (i - lo) / fmax(hi - lo, 0.001);
+    }
+    w = w < 0 ? 0 : (w > 1 ? 1 : w);
+    const long double g = w == 1.0L ? f : w * f + (1.0L - w) * f / r.factor;
+    out[i] = (double)(g / two_pi);
+  }
+}
+
+snap_status launch_rope(const snap_rope_params& r, int dtype, int n_seq, int max_len, int d, const int32_t* pos,
+                        int n_slots, const int32_t* slot_ids, const int32_t* lengths, const snap_rope_heads* q,
+                        const snap_rope_heads* k, hipStream_t stream) {
+  RopeArgs a = {};
+  const snap_rope_heads* op[2] = {q, k};
+  bool in_place = true;
+  for (int o = 0; o < 2; ++o) {
+    if (!op[o]) continue;
+    a.x[o] = op[o]->x;
+    a.y[o] = op[o]->y;
+    a.heads[o] = op[o]->n_heads;
+    for (int i = 0; i < 3; ++i) {
+      a.xs[o][i] = op[o]->x_stride[i];
+      a.ys[o][i] = op[o]->y_stride[i];
+    }
+    in_place = in_place && op[o]->x == op[o]->y;
+  }
+  a.n = n_seq;
+  a.max_len = max_len;
+  a.d = d;
+  a.rot_start = r.rot_start;
+  a.rot = r.rot_dim;
+  a.pairs = r.layout == SNAP_ROPE_PAIRS;
+  a.n_slots = n_slots;
+  a.in_place = in_place;
+  a.pos = pos;
+  a.slot_ids = slot_ids;
+  a.lengths = lengths;
+  a.amp = r.amplitude;
+  rope_turns(r, a.turns);
+  const int cols = a.rot / 2 + (in_place ? 0 : d - a.rot);
+  const int64_t threads = (int64_t)n_seq * max_len * cols;
+  const int heads = a.heads[0] + a.heads[1];
+  a.slices = heads < 64 ? heads : 64;
+  const dim3 grid((unsigned)((threads + 255) / 256), (unsigned)a.slices);
+  if (dtype == SNAP_BF16)
+    hipLaunchKernelGGL(rope_any<uint16_t>, grid, dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL(rope_any<float>, grid, dim3(256), 0, stream, a);
+  return hipGetLastError() == hipSuccess ? SNAP_OK : SNAP_ERR_HIP;
+}
+
+}  // namespace snap

@@ -135,6 +135,8 @@ enum : uint32_t {
   kDbgCombine = 1u << 6,     // more split-K chunks than the combine holds
   kDbgAppend = 1u << 7,      // an appended row outside the sink / ring rows
   kDbgPrefill = 1u << 8,     // a prefill block's positions outside the prompt
+  kDbgPagedItem = 1u << 9,   // a paged work item past the workspace's partials
+  kDbgPagedMove = 1u << 10,  // an evicted slot's move list past its end
 };
 #ifdef SNAP_DEBUG_CHECKS
 static __device__ uint32_t g_debug_flags;  // one per translation unit
@@ -163,6 +165,8 @@ __device__ __forceinline__ bool debug_check(bool, uint32_t) { return true; }
 uint32_t debug_flags_compress(bool reset);
 uint32_t debug_flags_decode(bool reset);
 uint32_t debug_flags_prefill(bool reset);
+uint32_t debug_flags_paged(bool reset);
+uint32_t debug_flags_evict(bool reset);
 
 // ---------------------------------------------------------------- launch context
 struct Geometry {
@@ -247,6 +251,38 @@ snap_status launch_decode(const snap_params& p, const snap_cache& c, const int32
                           const void* k_new, const void* v_new, void* out, int out_dtype, void* ws,
                           hipStream_t stream);
 snap_status launch_advance(int32_t* pos, int n_slots, int n, const int32_t* slot_ids, hipStream_t stream);
+
+constexpr int kRopeMaxPairs = 64;  // rotated pairs of a head
+snap_status launch_rope(const snap_rope_params& r, int dtype, int n_seq, int max_len, int d, const int32_t* pos,
+                        int n_slots, const int32_t* slot_ids, const int32_t* lengths, const snap_rope_heads* q,
+                        const snap_rope_heads* k, hipStream_t stream);
+
+// Paged decode: the call's work items (chunks of one (sequence, KV head)'s
+// rows, cut on the device from the rows that are there) and its workspace.
+struct PagedGeometry {
+  int target;     // items that the rows are cut into, besides one per unit at most
+  int max_items;  // items at most: target + units
+  size_t off_part, off_ml, off_z, bytes;
+};
+PagedGeometry paged_geometry(const snap_params& p, int n, int max_rows, bool weigh);
+snap_status launch_paged_append(const snap_params& p, const snap_paged_cache& c, const int32_t* rows,
+                                const int32_t* pos, int n, const int32_t* slot_ids, const int32_t* lengths, int max_len,
+                                const void* k_new, const int64_t* k_stride, const void* v_new, const int64_t* v_stride,
+                                const float* weight_new, hipStream_t stream);
+// k_new non-NULL: the token at pos is stored first, as launch_paged_append does
+snap_status launch_paged_decode(const snap_params& p, const snap_paged_cache& c, const int32_t* rows,
+                                const int32_t* pos, int n, const int32_t* slot_ids, int max_rows, const void* q,
+                                const void* k_new, const void* v_new, void* out, int out_dtype, bool weigh, void* ws,
+                                hipStream_t stream);
+
+struct EvictGeometry {
+  int max_moves;  // moves of a (sequence, KV head) at most
+  size_t off_count, off_src, off_dst, bytes;
+};
+EvictGeometry evict_geometry(const snap_params& p, int n, int max_rows);
+snap_status launch_paged_evict(const snap_params& p, const snap_paged_cache& c, const int32_t* rows, const int32_t* pos,
+                               int32_t* rows_out, int n, const int32_t* slot_ids, int max_rows, int32_t* kept_out,
+                               void* ws, hipStream_t stream);
 
 // device address of the current GPU's snap_decode_step_noalloc scratch array
 snap_status noalloc_scratch(void** addr);
