@@ -144,6 +144,8 @@ static snap_status check_paged(const snap_params* p, const snap_paged_cache* c) 
   if (!c->k || !aligned16(c->k)) return fail(SNAP_ERR_INVALID_ARG, "cache k is NULL or not 16-byte aligned");
   if (!p->v_in_k && (!c->v || !aligned16(c->v)))
     return fail(SNAP_ERR_INVALID_ARG, "cache v is NULL or not 16-byte aligned");
+  if (!aligned16(c->token) || !aligned16(c->weight))
+    return fail(SNAP_ERR_INVALID_ARG, "cache token or weight is not 16-byte aligned");
   if (p->kv_dtype == SNAP_FP8_E4M3 && (!c->k_scale || (!p->v_in_k && !c->v_scale)))
     return fail(SNAP_ERR_INVALID_ARG, "an fp8 cache needs k_scale and v_scale");
   return SNAP_OK;

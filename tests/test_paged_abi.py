@@ -126,6 +126,8 @@ ALL = "append attn step evict"
     (dict(ckw=dict(v=None)), INVALID, ALL),
     (dict(ckw=dict(k=FAKE + 8)), INVALID, ALL),
     (dict(ckw=dict(page_table=None)), INVALID, ALL),
+    (dict(ckw=dict(weight=FAKE + 4)), INVALID, ALL),
+    (dict(ckw=dict(token=FAKE + 8)), INVALID, ALL),
     (dict(ckw=dict(n_slots=0)), INVALID, ALL),
     (dict(ckw=dict(n_pages=0)), INVALID, ALL),
     (dict(ckw=dict(max_pages=0)), INVALID, ALL),
