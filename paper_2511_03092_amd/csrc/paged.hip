@@ -3,10 +3,12 @@
 //
 //   paged_append   stores the tokens of a prompt or of a step
 //   paged_gqa      64- and 128-wide rows: one wave per work item on the matrix
-//                  units; a step's new token is stored in the same launch
-//   paged_decode   latent rows: one wave per (work item, query head)
+//                  units
+//   paged_latent   latent rows: four waves per work item, through LDS
 //   paged_join     merges the items of a (sequence, query head) -> out, and adds
 //                  the rows' softmax weights to their accumulated ones
+// A step's new token is stored in the attention launch, by the item that ends
+// with it, which reads it from its input.
 //
 // Work items.  Sequences are of unequal length and their lengths are on the
 // device, so the rows are cut there: every unit (sequence, KV head) takes
@@ -15,6 +17,7 @@
 // sequence it is of.  Every wave finds its item from the lengths alone.
 #include <math.h>
 
+#include "lds_dma.h"
 #include "snap_internal.h"
 
 namespace snap {
@@ -23,7 +26,6 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kBlockRows = 32;  // rows of a block
-constexpr int kItemTarget = 2048;
 // with the SNAP_KV_AUTO hint, calls of at least this many cache bytes (at
 // max_rows) read with streaming loads: half the 256 MB last-level cache
 constexpr size_t kStreamingCallBytes = (size_t)128 << 20;
@@ -39,7 +41,7 @@ struct PagedArgs {
   const int32_t* table;
   float* part;   // [items][G][dv]
   float2* ml;    // [items][G]  (max in log2 units, sum)
-  float* z;      // logits in log2 units, [unit][G][its rows, whole blocks]; NULL without weights
+  float* z;      // logits in log2 units, [unit][its blocks][G][32 rows]; NULL without weights
   float* weight;
   void* out;
   // a step: the token to store at row rows[slot] before it is attended, [n][Hkv][dk]
@@ -133,69 +135,6 @@ __device__ __forceinline__ int64_t paged_row(const PagedArgs& a, int slot, int g
   return (((int64_t)page * a.Hkv + g) << a.page_shift) + (r & ((1 << a.page_shift) - 1));
 }
 
-template <typename KV>
-__device__ __forceinline__ float kv_f32(KV x) {
-  if constexpr (sizeof(KV) == 2)
-    return bf16_bits_to_f32(x);
-  else
-    return e4m3_to_f32(x);
-}
-
-template <typename KV>
-__global__ __launch_bounds__(64) void paged_decode(PagedArgs a) {
-  const int lane = tid(), item = bid_x(), h = bid_y();
-  PagedSeq s;
-  if (!paged_seq(a, item, true, s)) return;
-  if (!debug_check(item < a.max_items, kDbgPagedItem)) return;
-  const int local = item - s.item0, g = local / s.items, chunk = local % s.items;
-  const int r0 = (int)((int64_t)chunk * s.blocks / s.items) * kBlockRows;
-  const int r1 = min(s.len, (int)((int64_t)(chunk + 1) * s.blocks / s.items) * kBlockRows);
-  constexpr int kMaxPer = 9;  // dims a lane: 576 / 64
-  const int nk = a.dk / 64, nv = a.dv / 64;
-  const size_t qo = ((size_t)s.b * a.Hq + g * a.G + h) * a.dk;
-  const float ksc = sizeof(KV) == 1 ? a.k_scale[(size_t)s.slot * a.Hkv + g] : 1.f;
-  const float vsc = sizeof(KV) == 1 ? (a.cv ? a.v_scale : a.k_scale)[(size_t)s.slot * a.Hkv + g] : 1.f;
-  const float xs = a.scale * kLog2e * ksc;
-  float q[kMaxPer], acc[kMaxPer];
-#pragma unroll
-  for (int i = 0; i < kMaxPer; ++i) {
-    q[i] = 0.f;
-    acc[i] = 0.f;
-    if (i < nk)
-      q[i] = bf16_bits_to_f32(((const uint16_t*)a.q)[qo + i * 64 + lane]);
-  }
-  float m = -INFINITY, l = 0.f;
-  float* z = a.z ? a.z + ((s.block0 + (int64_t)g * s.blocks) * a.G + (int64_t)h * s.blocks) * kBlockRows : nullptr;
-  for (int r = r0; r < r1; ++r) {
-    const int64_t row = paged_row(a, s.slot, g, r);
-    float x = -INFINITY;
-    if (row >= 0) {
-      const KV* kp = (const KV*)a.ck + row * a.dk;
-      float dot = 0.f;
-#pragma unroll
-      for (int i = 0; i < kMaxPer; ++i)
-        if (i < nk) dot = fmaf(q[i], kv_f32<KV>(kp[i * 64 + lane]), dot);
-      x = warp_sum(dot) * xs;
-      const float mn = fmaxf(m, x);
-      if (mn != -INFINITY) {
-        const float al = fast_exp2(m - mn), p = fast_exp2(x - mn);
-        l = fmaf(l, al, p);
-        const KV* vp = a.cv ? (const KV*)a.cv + row * a.dv : kp;
-#pragma unroll
-        for (int i = 0; i < kMaxPer; ++i)
-          if (i < nv) acc[i] = fmaf(acc[i], al, p * kv_f32<KV>(vp[i * 64 + lane]));
-        m = mn;
-      }
-    }
-    if (z && lane == 0) z[r] = x;
-  }
-  const size_t pi = (size_t)item * a.G + h;
-  if (lane == 0) a.ml[pi] = make_float2(m, l);
-#pragma unroll
-  for (int i = 0; i < kMaxPer; ++i)
-    if (i < nv) a.part[pi * a.dv + i * 64 + lane] = acc[i] * vsc;
-}
-
 // ---------------------------------------------------------------- 64- and 128-wide rows
 // One wave per work item, for the G query heads of its KV head at once: a block
 // of 32 rows against the heads (padded to 16 columns) on the matrix units, an
@@ -247,6 +186,25 @@ __device__ __forceinline__ u32x2 bf16_to_codes(u32x4 raw, float scale) {
   return u32x2{e4m3x4_hw(f[0], f[1], f[2], f[3]), e4m3x4_hw(f[4], f[5], f[6], f[7])};
 }
 
+// Eight probabilities as two bf16 terms (pe is used up).  The second is kept off
+// zero (2^-126), so that an infinite value times it stays infinite, as with the
+// whole probability.
+__device__ __forceinline__ void two_terms(float (&pe)[8], bf16x8 (&p)[2]) {
+#pragma unroll
+  for (int part = 0; part < 2; ++part) {
+    u32x4 pw;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float lo = part ? fmaxf(pe[2 * i], 0x1p-126f) : pe[2 * i];
+      const float hi = part ? fmaxf(pe[2 * i + 1], 0x1p-126f) : pe[2 * i + 1];
+      pe[2 * i] -= __uint_as_float(__float_as_uint(pe[2 * i]) & 0xffff0000u);
+      pe[2 * i + 1] -= __uint_as_float(__float_as_uint(pe[2 * i + 1]) & 0xffff0000u);
+      pw[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+    }
+    p[part] = __builtin_bit_cast(bf16x8, pw);
+  }
+}
+
 // The ids of 64 pages of a slot from page `first` on, one a lane.
 struct PageIds {
   int first, id;
@@ -283,8 +241,16 @@ __device__ __forceinline__ bool paged_item(const PagedArgs& a, int item, PagedIt
   return true;
 }
 
-template <int D, int KV, bool NT>
+// W: the logits go to the workspace, for the weights.  They are staged in LDS and
+// leave in runs of 16 KB: writes between the streaming reads cost by their number
+// more than by their bytes (8 sequences of 4k to 128k rows, 142 MB of logits beside
+// 2.28 GB: 512-byte runs 527 us, 1 KB runs 510, 16 KB runs 450, none 397).  Eight
+// waves a CU leave each 20 KB of LDS.
+constexpr int kZStage = 4096;  // logits that are staged before they leave
+
+template <int D, int KV, bool NT, bool W>
 __global__ __launch_bounds__(64) void paged_gqa(PagedArgs a) {
+  extern __shared__ __align__(16) float zstage[];  // W: kZStage and a block more
   constexpr int E = KV == kKvFp8 ? 1 : (KV == kKvBf16 ? 2 : 4);  // bytes of an element
   constexpr int NK = D * E / 64;                                 // key loads a half
   constexpr int VE = D / 16;                                     // value dims a lane
@@ -360,9 +326,8 @@ __global__ __launch_bounds__(64) void paged_gqa(PagedArgs a) {
   f32x4 acc[VE];
 #pragma unroll
   for (int c = 0; c < VE; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float* z = a.z && hval
-                 ? a.z + ((it.s.block0 + (int64_t)g * it.s.blocks) * a.G + (int64_t)l16 * it.s.blocks) * kBlockRows + 4 * lg
-                 : nullptr;
+  float* z = W ? a.z + (it.s.block0 + (int64_t)g * it.s.blocks) * a.G * kBlockRows : nullptr;
+  int zrow = r0;  // first row staged
 
   u32x4 k0[NK], k1[NK];
   int64_t h0 = pages.row(a, slot, g, r0), h1 = r0 + 16 < r1 ? pages.row(a, slot, g, r0 + 16) : -1;
@@ -430,9 +395,21 @@ __global__ __launch_bounds__(64) void paged_gqa(PagedArgs a) {
         if (h1 < 0 || vb + 16 + 4 * lg + e >= r1) x[4 + e] = -INFINITY;
       }
     }
-    if (z) {
-      *(f32x4*)(z + vb) = f32x4{x[0], x[1], x[2], x[3]} * xs;
-      *(f32x4*)(z + vb + 16) = f32x4{x[4], x[5], x[6], x[7]} * xs;
+    if constexpr (W) {
+      if (hval) {
+        float* st = zstage + (vb - zrow) * a.G + l16 * kBlockRows + 4 * lg;
+        *(f32x4*)st = f32x4{x[0], x[1], x[2], x[3]} * xs;
+        *(f32x4*)(st + 16) = f32x4{x[4], x[5], x[6], x[7]} * xs;
+      }
+      const int staged = (vb + 32 - zrow) * a.G;
+      if (staged >= kZStage || vb + 32 >= r1) {
+        // one wave, whose LDS operations take effect in order: no barrier (which
+        // would also wait for the loads in flight), only the compiler is held
+        asm volatile("" ::: "memory");
+        for (int i = 4 * lane; i < staged; i += 256) *(f32x4*)(z + (int64_t)zrow * a.G + i) = *(const f32x4*)(zstage + i);
+        asm volatile("" ::: "memory");
+        zrow = vb + 32;
+      }
     }
     float bm = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
     bm = fmaxf(bm, __shfl_xor(bm, 16));
@@ -459,22 +436,8 @@ __global__ __launch_bounds__(64) void paged_gqa(PagedArgs a) {
         for (int c = 0; c < NF; ++c)
           acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[i][c]), pe[i], acc[c], 0, 0, 0);
     } else {
-      // the second term is kept off zero (2^-126), so that an infinite value
-      // times it stays infinite, as with the whole probability
       bf16x8 p[2];
-#pragma unroll
-      for (int part = 0; part < 2; ++part) {
-        u32x4 pw;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float lo = part ? fmaxf(pe[2 * i], 0x1p-126f) : pe[2 * i];
-          const float hi = part ? fmaxf(pe[2 * i + 1], 0x1p-126f) : pe[2 * i + 1];
-          pe[2 * i] -= __uint_as_float(__float_as_uint(pe[2 * i]) & 0xffff0000u);
-          pe[2 * i + 1] -= __uint_as_float(__float_as_uint(pe[2 * i + 1]) & 0xffff0000u);
-          pw[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
-        }
-        p[part] = __builtin_bit_cast(bf16x8, pw);
-      }
+      two_terms(pe, p);
       uint32_t vw[8][VE / 2];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -532,6 +495,240 @@ __global__ __launch_bounds__(64) void paged_gqa(PagedArgs a) {
 #pragma unroll
     for (int c = 0; c < VE; c += 4)
       *(f32x4*)(dst + e * VE + c) = f32x4{acc[c][e], acc[c + 1][e], acc[c + 2][e], acc[c + 3][e]} * vsc;
+}
+
+// ---------------------------------------------------------------- latent rows
+// 576-wide rows whose first 512 dims are the values, bf16 or fp8.  Four waves per
+// work item take blocks of 64 rows through two LDS stages of direct global -> LDS
+// loads: wave w loads the rows [16w, 16w+16) of a block (in one page), forms their
+// logits as soon as its own loads are there, and leaves them in LDS; after one
+// barrier, which every wave reaches with its rows landed, each wave takes the
+// softmax of all 64 rows and the value product for dims [128w, 128w+128).  So no
+// key is read from LDS twice, no code converted twice for the same product, and a
+// block needs two barriers: that one, and one before its stage is loaded again.
+// A stage holds rows of CPR 16-byte pieces; piece c of row r sits at r CPR + (c ^
+// swizzle(r)), within aligned groups of 8 (fp8: 4), which spreads both the key
+// reads (one piece of 16 rows) and the value reads (16 pieces of a row) over the
+// banks.  bf16 stages take 147 KB, one workgroup a CU; fp8 ones half, two.
+// Rows past the sequence and in pages that are not there are loaded from a row of
+// zeros: their probabilities are zero, and zero times whatever else might stand
+// there need not be.
+constexpr int kLatRows = 64;
+__device__ const u32x4 kZeroRow[72] = {};
+
+template <bool FP8>
+struct Lat {
+  static constexpr int RB = FP8 ? 576 : 1152;  // bytes of a row
+  static constexpr int CPR = RB / 16;
+  static constexpr int NL = 16 * CPR / 64;     // loads a wave and block: 18 or 9
+  static constexpr int Stage = kLatRows * RB;
+  static __device__ __forceinline__ int swz(int r) { return (r >> 1) & (FP8 ? 3 : 7); }
+  static __device__ __forceinline__ int at(int r, int c) { return (r * CPR + (c ^ swz(r))) * 16; }
+};
+
+typedef __attribute__((address_space(3))) void* lds_ptr;
+// One wave-instruction of global -> LDS copy: lane i's 16 bytes land at lds + 16 i.
+// In asm, so that the only order with later LDS reads is the explicit wait; M0
+// (the LDS base) is saved and restored.
+template <bool NT>
+__device__ __forceinline__ void copy_to_lds(const void* from, const void* lds) {
+  const uint32_t la = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)lds);
+  uint32_t saved;
+  if constexpr (NT)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off nt\n\ts_nop 0\n\ts_mov_b32 m0, %0"
+                 : "=&s"(saved) : "s"(la), "v"(from) : "memory");
+  else
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_nop 0\n\ts_mov_b32 m0, %0"
+                 : "=&s"(saved) : "s"(la), "v"(from) : "memory");
+}
+
+template <bool FP8, bool NT, bool W>
+__global__ __launch_bounds__(256, FP8 ? 2 : 1) void paged_latent(PagedArgs a) {
+  typedef Lat<FP8> L;
+  constexpr int D = 576, DV = 512, XLd = kLatRows + 4;
+  __shared__ __align__(16) unsigned char stage[2][L::Stage];
+  __shared__ __align__(16) float xs_all[16 * XLd];  // a block's products by head
+  const int lane = tid() & 63, w = uniform(tid() >> 6), l16 = lane & 15, lg = lane >> 4;
+  PagedItem it;
+  if (!paged_item(a, bid_x(), it)) return;
+  const int slot = it.s.slot, g = it.g, r0 = it.r0, r1 = it.r1, b = it.s.b;
+  PageIds pages;
+  pages.load(a, slot, r0 >> a.page_shift);
+  const bool hval = l16 < a.G;
+  const unsigned char* cache = (const unsigned char*)a.ck;
+  const unsigned char* knew = it.rnew >= 0 ? (const unsigned char*)a.k_new + ((size_t)b * a.Hkv + g) * (D * 2) : nullptr;
+  const float ksc = FP8 ? a.k_scale[(size_t)slot * a.Hkv + g] : 1.f;
+  const float xs = a.scale * kLog2e * ksc;
+  // lane group lg feeds the piece 18 lg + t (fp8: half t % 2 of 9 lg + t / 2) of a
+  // row to k-step t
+  bf16x8 q[18];
+  {
+    const uint16_t* qp = (const uint16_t*)a.q + ((size_t)b * a.Hq + g * a.G + (hval ? l16 : 0)) * D;
+#pragma unroll
+    for (int t = 0; t < 18; ++t)
+      q[t] = __builtin_bit_cast(bf16x8, hval ? *(const u32x4*)(qp + 8 * (18 * lg + t)) : u32x4{0u, 0u, 0u, 0u});
+  }
+  int off[L::NL];  // this lane's pieces of a wave's 16 rows: bytes from their first
+#pragma unroll
+  for (int i = 0; i < L::NL; ++i) {
+    const int sl = i * 64 + lane, r = sl / L::CPR;
+    off[i] = r * L::RB + ((sl % L::CPR) ^ L::swz(r)) * 16;
+  }
+  int there = 0;  // bit s: the page of this wave's rows in stage s is there
+  auto issue = [&](int blk) {
+    const int vb = r0 + kLatRows * blk + 16 * w;
+    unsigned char* dst = &stage[blk & 1][16 * w * L::RB];
+    const int64_t base = vb < r1 ? pages.row(a, slot, g, vb) : -1;
+    there = (there & ~(1 << (blk & 1))) | (base >= 0 ? 1 << (blk & 1) : 0);
+    const unsigned char* rows = cache + (size_t)base * L::RB;
+    if (base >= 0 && vb + 16 <= r1 && (it.rnew < vb || it.rnew >= vb + 16)) {
+#pragma unroll
+      for (int i = 0; i < L::NL; ++i) copy_to_lds<NT>(rows + off[i], dst + 1024 * i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < L::NL; ++i) {
+        const int r = vb + off[i] / L::RB, piece = off[i] % L::RB;
+        const unsigned char* from = rows + off[i];
+        if (base < 0 || r >= r1) from = (const unsigned char*)kZeroRow + piece;
+        else if (r == it.rnew) from = (FP8 ? (const unsigned char*)kZeroRow : knew) + piece;
+        copy_to_lds<NT>(from, dst + 1024 * i);
+      }
+    }
+  };
+
+  float m = -INFINITY, mref = 0.f, lsum = 0.f;
+  f32x4 acc[8];
+#pragma unroll
+  for (int c = 0; c < 8; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float* z = W ? a.z + (it.s.block0 + (int64_t)g * it.s.blocks) * a.G * kBlockRows : nullptr;
+  const int nblk = (r1 - r0 + kLatRows - 1) / kLatRows;
+  issue(0);
+  if (nblk > 1) issue(1);
+  for (int i = 0; i < nblk; ++i) {
+    // this wave's rows of block i have landed: only the next block's loads (and
+    // what was issued after them) are in flight
+    if (i + 1 < nblk)
+      wait_vm<L::NL>();
+    else
+      wait_vm<0>();
+    asm volatile("" ::: "memory");
+    unsigned char* st = &stage[i & 1][0];
+    const int vb = r0 + kLatRows * i, vw = vb + 16 * w;
+    const bool have = (there >> (i & 1)) & 1;
+    if constexpr (FP8) {
+      if (have && it.rnew >= vw && it.rnew < min(r1, vw + 16) && lane < L::CPR) {  // the new row's codes, over the zeros
+        const u32x4* src = (const u32x4*)knew + 2 * lane;
+        const u32x2 c0 = bf16_to_codes(src[0], ksc), c1 = bf16_to_codes(src[1], ksc);
+        *(u32x4*)(st + L::at(it.rnew - vb, lane)) = u32x4{c0[0], c0[1], c1[0], c1[1]};
+      }
+      asm volatile("" ::: "memory");
+    }
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < 18; t += FP8 ? 2 : 1) {
+      const u32x4 k = *(const u32x4*)(st + L::at(16 * w + l16, FP8 ? 9 * lg + t / 2 : 18 * lg + t));
+      if constexpr (FP8) {
+        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, codes_to_bf16(k[0], k[1])), q[t], s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, codes_to_bf16(k[2], k[3])), q[t + 1], s, 0, 0, 0);
+      } else {
+        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), q[t], s, 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (!have || vw + 4 * lg + e >= r1) s[e] = -INFINITY;
+    *(f32x4*)(xs_all + l16 * XLd + 16 * w + 4 * lg) = s;
+    lds_barrier();  // every wave's rows have landed and its products are there
+    float x[16];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const f32x4 v = *(const f32x4*)(xs_all + l16 * XLd + 16 * k + 4 * lg);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[4 * k + e] = v[e];
+    }
+    if (W && w == 0 && hval) {
+      float* zb = z + ((int64_t)(vb / kBlockRows) * a.G + l16) * kBlockRows + 4 * lg;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (vb + 16 * k < r1)
+          *(f32x4*)(zb + (k >> 1) * a.G * kBlockRows + 16 * (k & 1)) = f32x4{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]} * xs;
+    }
+    float bm = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) bm = fmaxf(bm, x[k]);
+    bm = fmaxf(bm, __shfl_xor(bm, 16));
+    bm = fmaxf(bm, __shfl_xor(bm, 32));
+    bm *= xs;
+    const bool up = bm > m + kStaleMax;
+    if (wave_any(up)) {
+      const float mnew = up ? bm : m;
+      const float alpha = up ? fast_exp2(m - mnew) : 1.f;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) acc[c] *= alpha;
+      lsum *= alpha;
+      m = mnew;
+      mref = m == -INFINITY ? 0.f : m;
+    }
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      float pe[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) pe[k] = fast_exp2(fmaf(x[8 * kk + k], xs, -mref));
+      lsum += ((pe[0] + pe[1]) + (pe[2] + pe[3])) + ((pe[4] + pe[5]) + (pe[6] + pe[7]));
+      bf16x8 p[2];
+      two_terms(pe, p);
+      u32x4 v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int r = 32 * kk + (k < 4 ? 0 : 16) + 4 * lg + (k & 3);
+        if constexpr (FP8) {
+          const u32x2 c = *(const u32x2*)(st + L::at(r, 8 * w + (l16 >> 1)) + 8 * (l16 & 1));
+          v[k] = codes_to_bf16(c[0], c[1]);
+        } else {
+          v[k] = *(const u32x4*)(st + L::at(r, 16 * w + l16));
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const uint32_t sel = (c & 1) ? 0x07060302u : 0x05040100u;
+        u32x4 av;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) av[k] = __builtin_amdgcn_perm(v[2 * k + 1][c >> 1], v[2 * k][c >> 1], sel);
+        acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, av), p[1], acc[c], 0, 0, 0);
+        acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, av), p[0], acc[c], 0, 0, 0);
+      }
+    }
+    lds_barrier();  // every wave is done with this stage and these products
+    if (i + 2 < nblk) issue(i + 2);
+  }
+  lsum += __shfl_xor(lsum, 16);
+  lsum += __shfl_xor(lsum, 32);
+  if (w == 0 && it.rnew >= 0 && it.rnew < (a.max_pages << a.page_shift)) {
+    const int64_t row = paged_row(a, slot, g, it.rnew);
+    if (row >= 0) {
+      unsigned char* to = (unsigned char*)const_cast<void*>(a.ck) + row * L::RB;
+      if constexpr (FP8) {
+        if (lane < L::CPR) {
+          const u32x4* src = (const u32x4*)knew + 2 * lane;
+          const u32x2 c0 = bf16_to_codes(src[0], ksc), c1 = bf16_to_codes(src[1], ksc);
+          *(u32x4*)(to + 16 * lane) = u32x4{c0[0], c0[1], c1[0], c1[1]};
+        }
+      } else {
+        for (int c = lane; c < L::CPR; c += 64) *(u32x4*)(to + 16 * c) = *((const u32x4*)knew + c);
+      }
+      if (lane == 0 && a.token) a.token[row] = a.pos[slot];
+      if (lane == 0 && a.weight) a.weight[row] = 0.f;
+    }
+  }
+  if (!hval) return;
+  const size_t pi = (size_t)bid_x() * a.G + l16;
+  if (w == 0 && lg == 0) a.ml[pi] = make_float2(m, lsum);
+  float* dst = a.part + pi * DV + 128 * w + 8 * 4 * lg;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+#pragma unroll
+    for (int c = 0; c < 8; c += 4)
+      *(f32x4*)(dst + 8 * e + c) = f32x4{acc[c][e], acc[c + 1][e], acc[c + 2][e], acc[c + 3][e]} * ksc;
 }
 
 // ---------------------------------------------------------------- join
@@ -610,7 +807,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join(PagedArgs a, int merg
     if (row < 0) continue;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
     for (int h = 0; h < a.G; ++h) {
-      const f32x4 y = *(const f32x4*)(z + (int64_t)h * it.s.blocks * kBlockRows + r);
+      const f32x4 y = *(const f32x4*)(z + ((int64_t)(r / kBlockRows) * a.G + h) * kBlockRows + r % kBlockRows);
       const float2 ml = sml[h];
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[e] = fmaf(fast_exp2(y[e] - ml.x), ml.y, sum[e]);
@@ -711,11 +908,26 @@ inline int log2_of(int x) { return 31 - __builtin_clz((unsigned)x); }
 
 SNAP_DEBUG_READER(debug_flags_paged)
 
+// Work items that the card holds at once: more, shorter ones leave a partial
+// second round, fewer leave loads unissued.  Latent rows: a workgroup a CU (fp8:
+// two).  The others by the registers of a wave (two a SIMD): 2048, from 1024 items
+// 224 -> 230 us on 128-wide fp32 rows, which fit one a SIMD, and 105 -> 102 (bf16)
+// and 91 -> 59 (fp8) on 128-wide ones, 85 -> 56 on 64-wide bf16, all 32 x 4 heads of
+// up to 16384 rows; from 3072 on all but 64-wide fp8 rows are slower (115, 61, 58).
+// Those have half the bytes in flight a wave: 4096 items 46 -> 38 us, but with
+// weights, whose staging leaves room for 2048, 59 -> 66.
+static int resident_items(const snap_params& p, bool weigh) {
+  if (p.d_qk == 576) return p.kv_dtype == SNAP_FP8_E4M3 ? 512 : 256;
+  if (p.kv_dtype == SNAP_F32 && p.d_qk == 128) return 1024;
+  return p.kv_dtype == SNAP_FP8_E4M3 && p.d_qk == 64 && !weigh ? 4096 : 2048;
+}
+
 // ---------------------------------------------------------------- host side
 PagedGeometry paged_geometry(const snap_params& p, int n, int max_rows, bool weigh) {
   PagedGeometry g{};
   const int units = (n > 0 ? n : 1) * p.n_kv_heads, G = p.n_q_heads / p.n_kv_heads;
-  g.target = units < kItemTarget / 2 ? kItemTarget - units : kItemTarget / 2;
+  const int waves = resident_items(p, weigh);
+  g.target = units < waves / 2 ? waves - units : waves / 2;
   const int64_t blocks = (int64_t)units * ((max_rows + kBlockRows - 1) / kBlockRows);
   // ceil(blocks / C) a unit, C >= blocks / target: at most target + units items,
   // and no more than there are blocks
@@ -778,12 +990,6 @@ snap_status launch_paged_decode(const snap_params& p, const snap_paged_cache& c,
                                 const int32_t* pos, int n, const int32_t* slot_ids, int max_rows, const void* q,
                                 const void* k_new, const void* v_new, void* out, int out_dtype, bool weigh, void* ws,
                                 hipStream_t stream) {
-  const bool gqa = p.d_qk == p.d_v;
-  if (k_new && !gqa) {
-    const snap_status st = launch_paged_append(p, c, rows, pos, n, slot_ids, nullptr, 1, k_new, nullptr, v_new, nullptr,
-                                               nullptr, stream);
-    if (st != SNAP_OK) return st;
-  }
   const PagedGeometry geo = paged_geometry(p, n, max_rows, weigh);
   PagedArgs a = {};
   a.q = q;
@@ -814,30 +1020,32 @@ snap_status launch_paged_decode(const snap_params& p, const snap_paged_cache& c,
   a.max_items = geo.max_items;
   a.out_bf16 = out_dtype == SNAP_BF16;
   a.scale = p.sm_scale > 0.f ? p.sm_scale : 1.0f / sqrtf((float)p.d_qk);
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.pos = pos;
+  a.token = c.token;
   const size_t elt = p.kv_dtype == SNAP_F32 ? 4 : (p.kv_dtype == SNAP_BF16 ? 2 : 1);
   const size_t call_bytes = (size_t)n * p.n_kv_heads * max_rows * (p.d_qk + (p.v_in_k ? 0 : p.d_v)) * elt;
   const bool nt = p.kv_reuse == SNAP_KV_STREAM || (p.kv_reuse == SNAP_KV_AUTO && call_bytes >= kStreamingCallBytes);
-  if (gqa) {
-    a.k_new = k_new;
-    a.v_new = v_new;
-    a.pos = pos;
-    a.token = c.token;
-    void (*k)(PagedArgs);
-    if (p.d_qk == 64)
-      k = p.kv_dtype == SNAP_F32    ? (nt ? paged_gqa<64, kKvF32, true> : paged_gqa<64, kKvF32, false>)
-          : p.kv_dtype == SNAP_BF16 ? (nt ? paged_gqa<64, kKvBf16, true> : paged_gqa<64, kKvBf16, false>)
-                                    : (nt ? paged_gqa<64, kKvFp8, true> : paged_gqa<64, kKvFp8, false>);
-    else
-      k = p.kv_dtype == SNAP_F32    ? (nt ? paged_gqa<128, kKvF32, true> : paged_gqa<128, kKvF32, false>)
-          : p.kv_dtype == SNAP_BF16 ? (nt ? paged_gqa<128, kKvBf16, true> : paged_gqa<128, kKvBf16, false>)
-                                    : (nt ? paged_gqa<128, kKvFp8, true> : paged_gqa<128, kKvFp8, false>);
-    hipLaunchKernelGGL(k, dim3(geo.max_items), dim3(64), 0, stream, a);
+  if (p.d_qk == 576) {
+    static constexpr void (*kernels[2][2][2])(PagedArgs) = {  // [fp8][NT][W]
+        {{paged_latent<false, false, false>, paged_latent<false, false, true>},
+         {paged_latent<false, true, false>, paged_latent<false, true, true>}},
+        {{paged_latent<true, false, false>, paged_latent<true, false, true>},
+         {paged_latent<true, true, false>, paged_latent<true, true, true>}}};
+    void (*k)(PagedArgs) = kernels[p.kv_dtype == SNAP_FP8_E4M3][nt][weigh];
+    hipLaunchKernelGGL(k, dim3(geo.max_items), dim3(256), 0, stream, a);
   } else {
-    const dim3 grid(geo.max_items, a.G);
-    if (p.kv_dtype == SNAP_BF16)
-      hipLaunchKernelGGL((paged_decode<uint16_t>), grid, dim3(64), 0, stream, a);
-    else
-      hipLaunchKernelGGL((paged_decode<uint8_t>), grid, dim3(64), 0, stream, a);
+    static constexpr void (*kernels[2][3][2][2])(PagedArgs) = {  // [width][type][NT][W]
+#define SNAP_PAGED_GQA(D, KV) \
+  {{paged_gqa<D, KV, false, false>, paged_gqa<D, KV, false, true>}, {paged_gqa<D, KV, true, false>, paged_gqa<D, KV, true, true>}}
+        {SNAP_PAGED_GQA(64, kKvBf16), SNAP_PAGED_GQA(64, kKvFp8), SNAP_PAGED_GQA(64, kKvF32)},
+        {SNAP_PAGED_GQA(128, kKvBf16), SNAP_PAGED_GQA(128, kKvFp8), SNAP_PAGED_GQA(128, kKvF32)}};
+#undef SNAP_PAGED_GQA
+    const int kv = p.kv_dtype == SNAP_F32 ? kKvF32 : (p.kv_dtype == SNAP_BF16 ? kKvBf16 : kKvFp8);
+    void (*k)(PagedArgs) = kernels[p.d_qk == 128][kv][nt][weigh];
+    hipLaunchKernelGGL(k, dim3(geo.max_items), dim3(64),
+                       weigh ? (kZStage + kBlockRows * a.G) * sizeof(float) : 0, stream, a);
   }
   if (hipGetLastError() != hipSuccess) return SNAP_ERR_HIP;
   const int merges = n * p.n_q_heads * (p.d_v == 512 ? 4 : 1);
