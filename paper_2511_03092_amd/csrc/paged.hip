@@ -50,7 +50,7 @@ struct PagedArgs {
   const void* v_new;
   const int32_t* pos;
   int32_t* token;
-  int n, Hq, Hkv, G, dk, dv, n_slots, n_pages, page_shift, max_pages, max_rows, target, max_items, out_bf16;
+  int n, Hq, Hkv, G, dk, dv, n_slots, n_pages, page_shift, max_pages, max_rows, waves, target, max_items, out_bf16;
   float scale;
 };
 
@@ -90,14 +90,30 @@ struct PagedSeq {
 __device__ __forceinline__ bool paged_seq(const PagedArgs& a, int key, bool by_item, PagedSeq& s) {
   const int lane = tid() & 63;
   int64_t total = 0;
+  int nb0 = 0;
   for (int b0 = 0; b0 < a.n; b0 += 64) {
     int slot;
     const int b = b0 + lane;
     const int nb = b < a.n ? (rows_of(a, b, slot) + kBlockRows - 1) / kBlockRows : 0;
-    total += wave_sum_i(nb);
+    if (b0 == 0) nb0 = nb;
+    total += uniform(wave_sum_i(nb));
   }
-  const int64_t c64 = (total * a.Hkv + a.target - 1) / a.target;
-  const int C = c64 < 1 ? 1 : (int)c64;  // blocks an item
+  // Blocks an item: as few as keep the items within a.waves.  total / waves of
+  // them may give more (a unit's last item is short), total / target never does;
+  // up to 64 sequences, whose lengths the lanes hold, some between are tried.
+  const int64_t t64 = total * a.Hkv;
+  int64_t c64 = (t64 + a.target - 1) / a.target;
+  if (a.n <= 64) {
+    const int64_t least = (t64 + a.waves - 1) / a.waves, step = (c64 - least) / 4 + 1;
+    for (int64_t c = least; c < c64; c += step) {
+      const int ni = c > 0 ? (nb0 + (int)c - 1) / (int)c : 0;
+      if ((int64_t)a.Hkv * wave_sum_i(ni) <= a.waves) {
+        c64 = c;
+        break;
+      }
+    }
+  }
+  const int C = c64 < 1 ? 1 : (int)c64;
   int items_before = 0;
   int64_t blocks_before = 0;
   for (int b0 = 0; b0 < a.n; b0 += 64) {
@@ -205,6 +221,14 @@ __device__ __forceinline__ void two_terms(float (&pe)[8], bf16x8 (&p)[2]) {
   }
 }
 
+// A loaded value is waited for here.  Before a loop, and behind a branch in one:
+// where the compiler sees a load that may be in flight as the loop comes round, it
+// waits at the value's use, every time, for all loads in flight.
+template <typename T>
+__device__ __forceinline__ void settle(T& v) {
+  asm volatile("" : "+v"(v));
+}
+
 // The ids of 64 pages of a slot from page `first` on, one a lane.
 struct PageIds {
   int first, id;
@@ -217,7 +241,10 @@ struct PageIds {
   // rows of all pages, or -1
   __device__ __forceinline__ int64_t row(const PagedArgs& a, int slot, int g, int r) {
     const int page = r >> a.page_shift;
-    if (page - first >= 64) load(a, slot, page);
+    if (page - first >= 64) {
+      load(a, slot, page);
+      settle(id);
+    }
     const int id_r = __builtin_amdgcn_readlane(id, page - first);
     if (id_r < 0 || id_r >= a.n_pages) return -1;
     return (((int64_t)id_r * a.Hkv + g) << a.page_shift) + (r & ((1 << a.page_shift) - 1));
@@ -329,6 +356,9 @@ __global__ __launch_bounds__(64) void paged_gqa(PagedArgs a) {
   float* z = W ? a.z + (it.s.block0 + (int64_t)g * it.s.blocks) * a.G * kBlockRows : nullptr;
   int zrow = r0;  // first row staged
 
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) settle(q[j]);
+  settle(pages.id);
   u32x4 k0[NK], k1[NK];
   int64_t h0 = pages.row(a, slot, g, r0), h1 = r0 + 16 < r1 ? pages.row(a, slot, g, r0 + 16) : -1;
   load_k(r0, h0, h1, k0, k1);
@@ -567,6 +597,9 @@ __global__ __launch_bounds__(256, FP8 ? 2 : 1) void paged_latent(PagedArgs a) {
 #pragma unroll
     for (int t = 0; t < 18; ++t)
       q[t] = __builtin_bit_cast(bf16x8, hval ? *(const u32x4*)(qp + 8 * (18 * lg + t)) : u32x4{0u, 0u, 0u, 0u});
+#pragma unroll
+    for (int t = 0; t < 18; ++t) settle(q[t]);
+    settle(pages.id);
   }
   int off[L::NL];  // this lane's pieces of a wave's 16 rows: bytes from their first
 #pragma unroll
@@ -926,8 +959,8 @@ static int resident_items(const snap_params& p, bool weigh) {
 PagedGeometry paged_geometry(const snap_params& p, int n, int max_rows, bool weigh) {
   PagedGeometry g{};
   const int units = (n > 0 ? n : 1) * p.n_kv_heads, G = p.n_q_heads / p.n_kv_heads;
-  const int waves = resident_items(p, weigh);
-  g.target = units < waves / 2 ? waves - units : waves / 2;
+  g.waves = resident_items(p, weigh);
+  g.target = units < g.waves / 2 ? g.waves - units : g.waves / 2;
   const int64_t blocks = (int64_t)units * ((max_rows + kBlockRows - 1) / kBlockRows);
   // ceil(blocks / C) a unit, C >= blocks / target: at most target + units items,
   // and no more than there are blocks
@@ -1016,6 +1049,7 @@ snap_status launch_paged_decode(const snap_params& p, const snap_paged_cache& c,
   a.page_shift = log2_of(c.page_size);
   a.max_pages = c.max_pages;
   a.max_rows = max_rows;
+  a.waves = geo.waves;
   a.target = geo.target;
   a.max_items = geo.max_items;
   a.out_bf16 = out_dtype == SNAP_BF16;

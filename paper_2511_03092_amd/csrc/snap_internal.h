@@ -260,6 +260,7 @@ snap_status launch_rope(const snap_rope_params& r, int dtype, int n_seq, int max
 // Paged decode: the call's work items (chunks of one (sequence, KV head)'s
 // rows, cut on the device from the rows that are there) and its workspace.
 struct PagedGeometry {
+  int waves;      // items that the card holds at once
   int target;     // items that the rows are cut into, besides one per unit at most
   int max_items;  // items at most: target + units
   size_t off_part, off_ml, off_z, bytes;
