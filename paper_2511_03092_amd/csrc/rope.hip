@@ -53,10 +53,10 @@ struct RopeToken {
   bool live;
   double position;
 };
-__device__ __forceinline__ RopeToken rope_token(const RopeArgs& a, int64_t i) {
+__device__ __forceinline__ RopeToken rope_token(const RopeArgs& a, unsigned i) {
   RopeToken k;
-  k.b = (int)(i / a.max_len);
-  k.t = (int)(i - (int64_t)k.b * a.max_len);
+  k.b = (int)(i / (unsigned)a.max_len);
+  k.t = (int)(i - (unsigned)k.b * (unsigned)a.max_len);
   k.live = !a.lengths || k.t < a.lengths[k.b];
   int start = 0;
   if (a.pos) {
@@ -85,14 +85,118 @@ __device__ __forceinline__ void rope_set(T* p, float v) {
     *p = v;
 }
 
-// One (token, pair or unrotated dim) per thread, over the heads of a slice.
+// One 16-byte piece (halves: a piece of the first half and its partner of the
+// second) of a token per thread, over the heads of a slice: the angles are formed
+// once and turn every head.  Copied dims take threads of their own.  HBM bound: four
+// heads' pieces are loaded before the first is turned, and the token's share of
+// every head is read by the same threads, so that both a token-by-token input and a
+// head-by-head output move in whole 128-byte lines.
+constexpr int kRopeHeads = 4;
+
+template <typename T>
+struct RopePiece {
+  static constexpr int E = 16 / sizeof(T);
+  float v[E];
+  __device__ __forceinline__ void unpack(u32x4 raw) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 2) {
+        v[2 * i] = __uint_as_float(raw[i] << 16);
+        v[2 * i + 1] = __uint_as_float(raw[i] & 0xffff0000u);
+      } else {
+        v[i] = __uint_as_float(raw[i]);
+      }
+    }
+  }
+  __device__ __forceinline__ u32x4 pack() const {
+    u32x4 raw;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 2)
+        raw[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+      else
+        raw[i] = __float_as_uint(v[i]);
+    }
+    return raw;
+  }
+};
+
+template <typename T, bool PAIRS>
+__global__ __launch_bounds__(256) void rope_pieces(RopeArgs a) {
+  constexpr int E = RopePiece<T>::E, NA = PAIRS ? E / 2 : E;  // angles of a thread
+  const unsigned nc = a.rot / (PAIRS ? E : 2 * E), cols = nc + (a.in_place ? 0 : (a.d - a.rot) / E);
+  const unsigned i = (unsigned)bid_x() * 256u + (unsigned)tid();
+  const unsigned tok = i / cols, col = i % cols;
+  if (tok >= (unsigned)a.n * (unsigned)a.max_len) return;
+  const RopeToken k = rope_token(a, tok);
+  if (!k.live) return;
+  const bool turn = col < nc;
+  float c[NA], s[NA];
+  int d1, d2 = 0;
+  if (turn) {
+#pragma unroll
+    for (int e = 0; e < NA; ++e) turn_of(k.position * a.turns[col * NA + e], a.amp, c[e], s[e]);
+    d1 = a.rot_start + col * E;
+    d2 = d1 + a.rot / 2;
+  } else {
+    d1 = (col - nc) * E;
+    if (d1 >= a.rot_start) d1 += a.rot;
+  }
+  const int total = a.heads[0] + a.heads[1];
+  for (int h0 = bid_y(); h0 < total; h0 += kRopeHeads * a.slices) {
+    u32x4 r1[kRopeHeads], r2[kRopeHeads];
+#pragma unroll
+    for (int u = 0; u < kRopeHeads; ++u) {
+      const int h = h0 + u * a.slices;
+      if (h >= total) break;
+      const int o = h < a.heads[0] ? 0 : 1, hh = o ? h - a.heads[0] : h;
+      const T* x = (const T*)a.x[o] + k.b * a.xs[o][0] + hh * a.xs[o][1] + k.t * a.xs[o][2];
+      r1[u] = *(const u32x4*)(x + d1);
+      if (!PAIRS && turn) r2[u] = *(const u32x4*)(x + d2);
+    }
+#pragma unroll
+    for (int u = 0; u < kRopeHeads; ++u) {
+      const int h = h0 + u * a.slices;
+      if (h >= total) break;
+      const int o = h < a.heads[0] ? 0 : 1, hh = o ? h - a.heads[0] : h;
+      T* y = (T*)a.y[o] + k.b * a.ys[o][0] + hh * a.ys[o][1] + k.t * a.ys[o][2];
+      if (!turn) {
+        *(u32x4*)(y + d1) = r1[u];
+        continue;
+      }
+      RopePiece<T> p, q;
+      p.unpack(r1[u]);
+      if constexpr (PAIRS) {
+#pragma unroll
+        for (int e = 0; e < NA; ++e) {
+          const float x1 = p.v[2 * e], x2 = p.v[2 * e + 1];
+          p.v[2 * e] = fmaf(x1, c[e], -(x2 * s[e]));
+          p.v[2 * e + 1] = fmaf(x2, c[e], x1 * s[e]);
+        }
+      } else {
+        q.unpack(r2[u]);
+#pragma unroll
+        for (int e = 0; e < NA; ++e) {
+          const float x1 = p.v[e], x2 = q.v[e];
+          p.v[e] = fmaf(x1, c[e], -(x2 * s[e]));
+          q.v[e] = fmaf(x2, c[e], x1 * s[e]);
+        }
+        *(u32x4*)(y + d2) = q.pack();
+      }
+      *(u32x4*)(y + d1) = p.pack();
+    }
+  }
+}
+
+// The same for pieces that are not whole: rotated dims, widths, strides or
+// addresses that 16 bytes do not divide.  One pair or copied dim per thread.
 template <typename T>
 __global__ __launch_bounds__(256) void rope_any(RopeArgs a) {
-  const int np = a.rot / 2, cols = np + (a.in_place ? 0 : a.d - a.rot);
-  const int64_t i = (int64_t)bid_x() * 256 + tid();
-  if (i >= (int64_t)a.n * a.max_len * cols) return;
-  const int col = (int)(i % cols);
-  const RopeToken k = rope_token(a, i / cols);
+  const unsigned np = a.rot / 2, cols = np + (a.in_place ? 0 : a.d - a.rot);
+  const unsigned i = (unsigned)bid_x() * 256u + (unsigned)tid();
+  const unsigned tok = i / cols, col = i % cols;
+  if (tok >= (unsigned)a.n * (unsigned)a.max_len) return;
+  const RopeToken k = rope_token(a, tok);
   if (!k.live) return;
   int d1, d2 = -1;
   float c = 1.f, s = 0.f;
@@ -177,15 +281,28 @@ snap_status launch_rope(const snap_rope_params& r, int dtype, int n_seq, int max
   a.lengths = lengths;
   a.amp = r.amplitude;
   rope_turns(r, a.turns);
-  const int cols = a.rot / 2 + (in_place ? 0 : d - a.rot);
-  const int64_t threads = (int64_t)n_seq * max_len * cols;
+  const int E = dtype == SNAP_F32 ? 4 : 8;
+  bool whole = (d | r.rot_start | (a.pairs ? r.rot_dim : r.rot_dim / 2)) % E == 0;
+  for (int o = 0; o < 2; ++o) {
+    whole = whole && (((uintptr_t)a.x[o] | (uintptr_t)a.y[o]) & 15u) == 0;
+    for (int i = 0; i < 3; ++i) whole = whole && (a.xs[o][i] | a.ys[o][i]) % E == 0;
+  }
+  const int turned = whole ? (a.pairs ? a.rot / E : a.rot / (2 * E)) : a.rot / 2;
+  const int64_t threads = (int64_t)n_seq * max_len * (turned + (in_place ? 0 : (d - a.rot) / (whole ? E : 1)));
+  // heads split over workgroups until 16 waves a CU have work
   const int heads = a.heads[0] + a.heads[1];
-  a.slices = heads < 64 ? heads : 64;
+  const int64_t want = ((int64_t)4096 * 64 + threads - 1) / threads;
+  a.slices = (int)(want > heads ? heads : want);
+  if (a.slices > 65535) a.slices = 65535;
   const dim3 grid((unsigned)((threads + 255) / 256), (unsigned)a.slices);
-  if (dtype == SNAP_BF16)
-    hipLaunchKernelGGL(rope_any<uint16_t>, grid, dim3(256), 0, stream, a);
+  void (*f)(RopeArgs);
+  if (!whole)
+    f = dtype == SNAP_BF16 ? rope_any<uint16_t> : rope_any<float>;
+  else if (a.pairs)
+    f = dtype == SNAP_BF16 ? rope_pieces<uint16_t, true> : rope_pieces<float, true>;
   else
-    hipLaunchKernelGGL(rope_any<float>, grid, dim3(256), 0, stream, a);
+    f = dtype == SNAP_BF16 ? rope_pieces<uint16_t, false> : rope_pieces<float, false>;
+  hipLaunchKernelGGL(f, grid, dim3(256), 0, stream, a);
   return hipGetLastError() == hipSuccess ? SNAP_OK : SNAP_ERR_HIP;
 }
 
