@@ -289,7 +289,7 @@ def snap_advance(pos, slot_ids, stream=None):
                               _stream(stream)))
 
 
-@dataclass
+@dataclass(frozen=True)
 class RopeParams:
     """Rotary positions (snap_rope_params)."""
     rot_start: int
@@ -303,82 +303,85 @@ class RopeParams:
     orig_len: int = 0
     amplitude: float = 1.0
 
+    def __post_init__(self):  # frozen: the structure is built once
+        object.__setattr__(self, "_struct", SnapRopeParams(
+            self.rot_start, self.rot_dim, self.layout, self.rule, self.base, self.factor, self.low_turns,
+            self.high_turns, self.orig_len, self.amplitude))
+
     def c(self) -> SnapRopeParams:
-        return SnapRopeParams(self.rot_start, self.rot_dim, self.layout, self.rule, self.base, self.factor,
-                              self.low_turns, self.high_turns, self.orig_len, self.amplitude)
+        return self._struct
 
 
 def _bad(msg: str):
     raise SnapError(SNAP_ERR_INVALID_ARG, msg)
 
 
-def _want(t, name: str, dtype, shape, device, optional: bool = False):
-    """t is a contiguous tensor of this type, shape and device (the library sees only its address)."""
+def _want(t, name: str, dtype, shape: tuple, index: int):
+    """t is a contiguous tensor of this type, shape and device index (the library sees only its address)."""
     if t is None:
-        if not optional:
-            _bad(f"{name} is None")
-    elif t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
-        _bad(f"{name} must be a contiguous {dtype} {tuple(shape)} tensor on {device} (got {t.dtype} {tuple(t.shape)}, "
-             f"strides {t.stride()}, on {t.device})")
+        _bad(f"{name} is None")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        _bad(f"{name} must be a contiguous {dtype} {tuple(shape)} tensor on device {index} (got {t.dtype} "
+             f"{tuple(t.shape)}, strides {t.stride()}, on {t.device})")
 
 
-class _Device:
-    """The tensors' device for the length of a call, and its stream: a launch goes to the current device."""
+def _launch(index: int, stream, fn, *args):
+    """One library call on the tensors' device (a launch goes to the current one) and its current stream."""
+    import torch
+    if index < 0:
+        _bad("tensors must be on the GPU")
+    if stream is None:
+        stream = torch._C._cuda_getCurrentRawStream(index)
+    if torch.cuda.current_device() == index:
+        status = fn(*args, stream)
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, stream)
+    if status:
+        _check(status)
 
-    def __init__(self, device, stream):
-        import torch
-        if device.type != "cuda":
-            _bad(f"tensors must be on the GPU (got {device})")
-        self.cuda, self.index, self.stream, self.before = torch.cuda, device.index, stream, None
 
-    def __enter__(self):
-        now = self.cuda.current_device()
-        if now != self.index:
-            self.before = now
-            self.cuda.set_device(self.index)
-        return self.cuda.current_stream().cuda_stream if self.stream is None else self.stream
-
-    def __exit__(self, *exc):
-        if self.before is not None:
-            self.cuda.set_device(self.before)
+_i64x3 = ctypes.c_int64 * 3
 
 
 def _rope_heads(x, y, name: str):
     if y is None:
         y = x
-    if x.dim() != 4 or y.shape != x.shape or y.dtype is not x.dtype or y.device != x.device:
-        _bad(f"{name} and its output must be [n, heads, tokens, d] of one shape, type and device "
-             f"(got {tuple(x.shape)} {x.dtype}, {tuple(y.shape)} {y.dtype})")
     xs, ys = x.stride(), y.stride()
+    if len(xs) != 4 or y.shape != x.shape or y.dtype is not x.dtype or y.get_device() != x.get_device():
+        _bad(f"{name} and its output must be [n, heads, tokens, d] of one shape, type and device "
+             f"(got {tuple(x.shape)} {x.dtype} on {x.device}, {tuple(y.shape)} {y.dtype} on {y.device})")
     if xs[3] != 1 or ys[3] != 1:
         _bad(f"{name}: the last dimension must be contiguous")
-    i3 = ctypes.c_int64 * 3
-    return SnapRopeHeads(x.data_ptr(), y.data_ptr(), i3(*xs[:3]), i3(*ys[:3]), x.shape[1])
+    return SnapRopeHeads(x.data_ptr(), y.data_ptr(), _i64x3(*xs[:3]), _i64x3(*ys[:3]), x.shape[1])
 
 
 def snap_rope(r: RopeParams, q, k=None, q_out=None, k_out=None, pos=None, slot_ids=None, lengths=None, stream=None):
     """Rotates q [n, heads, tokens, d] and k (any strides but the last) into q_out / k_out, or in place."""
     import torch
-    if q.dtype is not torch.bfloat16 and q.dtype is not torch.float32:
-        _bad(f"q must be bfloat16 or float32 (got {q.dtype})")
-    dev = q.device
-    hq = _rope_heads(q, q_out, "q")
-    hk = None
+    dtype, index = q.dtype, q.get_device()
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
+        _bad(f"q must be bfloat16 or float32 (got {dtype})")
+    hq, hk = _rope_heads(q, q_out, "q"), None
     n, _, tokens, d = q.shape
     if k is not None:
         hk = _rope_heads(k, k_out, "k")
-        if k.shape[0] != n or k.shape[2] != tokens or k.shape[3] != d or k.dtype is not q.dtype or k.device != dev:
-            _bad(f"q and k differ in more than their heads (got {tuple(q.shape)} {q.dtype}, {tuple(k.shape)} {k.dtype})")
-    if pos is not None:
-        _want(pos, "pos", torch.int32, (pos.numel(),), dev)
-        _want(slot_ids, "slot_ids", torch.int32, (n,), dev)
-    _want(lengths, "lengths", torch.int32, (n,), dev, optional=True)
+        if k.shape[0] != n or k.shape[2] != tokens or k.shape[3] != d or k.dtype is not dtype or k.get_device() != index:
+            _bad(f"q and k differ in more than their heads (got {tuple(q.shape)} {dtype}, {tuple(k.shape)} {k.dtype})")
+    n_slots = 0
+    if pos is None:
+        slot_ids = None
+    else:
+        n_slots = pos.numel()
+        _want(pos, "pos", torch.int32, (n_slots,), index)
+        _want(slot_ids, "slot_ids", torch.int32, (n,), index)
+    if lengths is not None:
+        _want(lengths, "lengths", torch.int32, (n,), index)
     if n == 0 or tokens == 0:
         return
-    with _Device(dev, stream) as st:
-        _check(lib().snap_rope(ctypes.byref(r.c()), SNAP_BF16 if q.dtype is torch.bfloat16 else SNAP_F32, n, tokens, d,
-                               _ptr(pos), 0 if pos is None else pos.numel(), None if pos is None else _ptr(slot_ids),
-                               _ptr(lengths), ctypes.byref(hq), None if hk is None else ctypes.byref(hk), st))
+    _launch(index, stream, lib().snap_rope, ctypes.byref(r.c()), SNAP_BF16 if dtype is torch.bfloat16 else SNAP_F32, n,
+            tokens, d, _ptr(pos), n_slots, _ptr(slot_ids), _ptr(lengths), ctypes.byref(hq),
+            None if hk is None else ctypes.byref(hk))
 
 
 def paged_cache_struct(k, v, page_table, token=None, weight=None, k_scale=None, v_scale=None) -> SnapPagedCache:
@@ -387,71 +390,74 @@ def paged_cache_struct(k, v, page_table, token=None, weight=None, k_scale=None, 
     import torch
     if k.dim() != 4 or k.dtype not in (torch.float32, torch.bfloat16, torch.uint8):
         _bad(f"k must be [n_pages, n_kv_heads, page_size, d] float32, bfloat16 or uint8 (got {tuple(k.shape)} {k.dtype})")
-    dev = k.device
-    _want(k, "k", k.dtype, k.shape, dev)
+    index, pages = k.get_device(), k.shape[:3]
+    _want(k, "k", k.dtype, k.shape, index)
     if v is not None:
         if v.dim() != 4:
             _bad(f"v must be [n_pages, n_kv_heads, page_size, d_v] (got {tuple(v.shape)})")
-        _want(v, "v", k.dtype, k.shape[:3] + v.shape[3:], dev)
+        _want(v, "v", k.dtype, pages + v.shape[3:], index)
     if page_table is None or page_table.dim() != 2:
         _bad("page_table must be [n_slots, max_pages]")
-    _want(page_table, "page_table", torch.int32, page_table.shape, dev)
+    _want(page_table, "page_table", torch.int32, page_table.shape, index)
     slots = int(page_table.shape[0])
-    _want(token, "token", torch.int32, k.shape[:3], dev, optional=True)
-    _want(weight, "weight", torch.float32, k.shape[:3], dev, optional=True)
-    _want(k_scale, "k_scale", torch.float32, (slots, k.shape[1]), dev, optional=True)
-    _want(v_scale, "v_scale", torch.float32, (slots, k.shape[1]), dev, optional=True)
+    for t, name, dtype, shape in ((token, "token", torch.int32, pages), (weight, "weight", torch.float32, pages),
+                                  (k_scale, "k_scale", torch.float32, (slots, pages[1])),
+                                  (v_scale, "v_scale", torch.float32, (slots, pages[1]))):
+        if t is not None:
+            _want(t, name, dtype, shape, index)
     c = SnapPagedCache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(token), _ptr(weight), _ptr(page_table), slots,
                        int(k.shape[0]), int(k.shape[2]), int(page_table.shape[1]))
-    c.device, c.kv_dtype, c.kv_heads, c.widths = dev, k.dtype, int(k.shape[1]), (int(k.shape[3]), None if v is None else int(v.shape[3]))
     c.tensors = (k, v, page_table, token, weight, k_scale, v_scale)
+    c.index, c.slots_shape, c.i32 = index, (slots,), torch.int32
+    c.in_dtype = torch.float32 if k.dtype is torch.float32 else torch.bfloat16
+    c.kind = ({torch.float32: SNAP_F32, torch.bfloat16: SNAP_BF16, torch.uint8: SNAP_FP8_E4M3}[k.dtype], int(k.shape[1]),
+              int(k.shape[3]), None if v is None else int(v.shape[3]))
+    c.rows_max, c.params = c.max_pages * c.page_size, (None, None)
     return c
 
 
-def _paged(p: Params, cache: SnapPagedCache, rows, pos, slot_ids, pos_optional: bool = True) -> int:
-    """Checks what every paged call shares; the number of sequences."""
-    import torch
-    kv = {SNAP_F32: torch.float32, SNAP_BF16: torch.bfloat16, SNAP_FP8_E4M3: torch.uint8}.get(p.kv_dtype)
-    if cache.kv_dtype is not kv or cache.kv_heads != p.n_kv_heads or cache.widths != (
-            p.d_qk, None if p.v_in_k else p.d_v):
-        _bad(f"the cache ({cache.kv_heads} heads, widths {cache.widths}, {cache.kv_dtype}) is not that of the parameters")
-    n = slot_ids.shape[0]
-    _want(slot_ids, "slot_ids", torch.int32, (n,), cache.device)
-    _want(rows, "rows", torch.int32, (cache.n_slots,), cache.device)
-    _want(pos, "pos", torch.int32, (cache.n_slots,), cache.device, optional=pos_optional)
-    return n
+def _paged(p: Params, cache: SnapPagedCache, rows, pos, slot_ids):
+    """Checks what every paged call shares; the number of sequences and the parameters' structure."""
+    values = tuple(vars(p).values())
+    if cache.params[0] != values:  # the same parameters as the last call's: the same structure
+        kind = (p.kv_dtype, p.n_kv_heads, p.d_qk, None if p.v_in_k else p.d_v)
+        if cache.kind != kind:
+            _bad(f"the cache (type, heads, widths {cache.kind}) is not that of the parameters ({kind})")
+        cache.params = (values, p.c())
+    n, index = slot_ids.shape[0], cache.index
+    _want(slot_ids, "slot_ids", cache.i32, (n,), index)
+    _want(rows, "rows", cache.i32, cache.slots_shape, index)
+    if pos is not None:
+        _want(pos, "pos", cache.i32, cache.slots_shape, index)
+    return n, ctypes.byref(cache.params[1])
 
 
-def _in_dtype(p: Params):
-    import torch
-    return torch.float32 if p.in_dtype == SNAP_F32 else torch.bfloat16
-
-
-def _strides(t, name: str, dtype, shape, device):
-    if t.dtype is not dtype or t.shape != shape or t.device != device or t.stride(3) != 1:
-        _bad(f"{name} must be a {dtype} {tuple(shape)} tensor on {device} whose rows are contiguous (got {t.dtype} "
-             f"{tuple(t.shape)}, strides {t.stride()}, on {t.device})")
-    return (ctypes.c_int64 * 3)(*t.stride()[:3])
+def _strides(t, name: str, dtype, shape: tuple, index: int):
+    st = t.stride()
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or st[3] != 1:
+        _bad(f"{name} must be a {dtype} {tuple(shape)} tensor on device {index} whose rows are contiguous (got {t.dtype} "
+             f"{tuple(t.shape)}, strides {st}, on {t.device})")
+    return _i64x3(*st[:3])
 
 
 def snap_paged_append(p: Params, cache: SnapPagedCache, rows, pos, slot_ids, k_new, v_new=None, lengths=None,
                       weight_new=None, stream=None):
     """Stores k_new [n, n_kv_heads, tokens, d_qk] and v_new (any strides but the last) behind the rows held."""
     import torch
-    n, dev = _paged(p, cache, rows, pos, slot_ids), cache.device
+    (n, cp), index, heads = _paged(p, cache, rows, pos, slot_ids), cache.index, p.n_kv_heads
     if k_new.dim() != 4 or (v_new is None) != bool(p.v_in_k):
         _bad("k_new must be [n, n_kv_heads, tokens, d_qk], with v_new unless the values are in the keys")
     tokens = k_new.shape[2]
-    ks = _strides(k_new, "k_new", _in_dtype(p), (n, p.n_kv_heads, tokens, p.d_qk), dev)
-    vs = None if v_new is None else _strides(v_new, "v_new", _in_dtype(p), (n, p.n_kv_heads, tokens, p.d_v), dev)
-    _want(lengths, "lengths", torch.int32, (n,), dev, optional=True)
-    _want(weight_new, "weight_new", torch.float32, (n, p.n_kv_heads, tokens), dev, optional=True)
+    ks = _strides(k_new, "k_new", cache.in_dtype, (n, heads, tokens, p.d_qk), index)
+    vs = None if v_new is None else _strides(v_new, "v_new", cache.in_dtype, (n, heads, tokens, p.d_v), index)
+    if lengths is not None:
+        _want(lengths, "lengths", cache.i32, (n,), index)
+    if weight_new is not None:
+        _want(weight_new, "weight_new", torch.float32, (n, heads, tokens), index)
     if n == 0 or tokens == 0:
         return
-    with _Device(dev, stream) as st:
-        _check(lib().snap_paged_append(ctypes.byref(p.c()), ctypes.byref(cache), _ptr(rows), _ptr(pos), n,
-                                       _ptr(slot_ids), _ptr(lengths), tokens, _ptr(k_new), ks, _ptr(v_new), vs,
-                                       _ptr(weight_new), st))
+    _launch(index, stream, lib().snap_paged_append, cp, ctypes.byref(cache), _ptr(rows), _ptr(pos), n, _ptr(slot_ids),
+            _ptr(lengths), tokens, _ptr(k_new), ks, _ptr(v_new), vs, _ptr(weight_new))
 
 
 def snap_paged_decode_workspace(p: Params, n: int, max_rows: int, weigh: bool = False) -> int:
@@ -462,61 +468,59 @@ def snap_paged_evict_workspace(p: Params, n: int, max_rows: int) -> int:
     return int(lib().snap_paged_evict_workspace(ctypes.byref(p.c()), n, max_rows))
 
 
-def _paged_io(p: Params, n: int, dev, q, out, workspace) -> int:
-    """Checks queries, output and workspace; the output's type code."""
+def _bytes(workspace, index: int) -> int:
+    if workspace.get_device() != index or not workspace.is_contiguous():
+        _bad(f"workspace must be contiguous on device {index} (got {workspace.device})")
+    return workspace.numel() * workspace.element_size()
+
+
+def _paged_io(p: Params, cache: SnapPagedCache, n: int, q, out) -> int:
+    """Checks queries and output; the output's type code."""
     import torch
-    _want(q, "q", _in_dtype(p), (n, p.n_q_heads, p.d_qk), dev)
+    _want(q, "q", cache.in_dtype, (n, p.n_q_heads, p.d_qk), cache.index)
     bf16 = out.dtype is torch.bfloat16
-    _want(out, "out", torch.bfloat16 if bf16 else torch.float32, (n, p.n_q_heads, p.d_v), dev)
-    if workspace.device != dev or not workspace.is_contiguous():
-        _bad(f"workspace must be contiguous on {dev}")
+    _want(out, "out", torch.bfloat16 if bf16 else torch.float32, (n, p.n_q_heads, p.d_v), cache.index)
     return SNAP_BF16 if bf16 else SNAP_F32
 
 
 def snap_paged_decode_attn(p: Params, cache: SnapPagedCache, rows, slot_ids, q, out, workspace, max_rows=None,
                            weigh: bool = False, stream=None):
     """Attention of one new token per sequence (stored already); max_rows bounds their rows (default: the table's)."""
-    n, dev = _paged(p, cache, rows, None, slot_ids), cache.device
-    od = _paged_io(p, n, dev, q, out, workspace)
-    with _Device(dev, stream) as st:
-        _check(lib().snap_paged_decode_attn(ctypes.byref(p.c()), ctypes.byref(cache), _ptr(rows), n, _ptr(slot_ids),
-                                            cache.max_pages * cache.page_size if max_rows is None else max_rows,
-                                            _ptr(q), _ptr(out), od, int(weigh), _ptr(workspace),
-                                            workspace.numel() * workspace.element_size(), st))
+    (n, cp), index = _paged(p, cache, rows, None, slot_ids), cache.index
+    od = _paged_io(p, cache, n, q, out)
+    _launch(index, stream, lib().snap_paged_decode_attn, cp, ctypes.byref(cache), _ptr(rows), n, _ptr(slot_ids),
+            cache.rows_max if max_rows is None else max_rows, _ptr(q), _ptr(out), od, int(weigh), _ptr(workspace),
+            _bytes(workspace, index))
 
 
 def snap_paged_decode_step(p: Params, cache: SnapPagedCache, rows, pos, slot_ids, q, k_new, v_new, out, workspace,
                            max_rows=None, weigh: bool = False, stream=None):
     """Stores one token per sequence (k_new [n, n_kv_heads, 1, d_qk], or without the 1) and attends it."""
-    n, dev = _paged(p, cache, rows, pos, slot_ids), cache.device
-    od = _paged_io(p, n, dev, q, out, workspace)
+    (n, cp), index = _paged(p, cache, rows, pos, slot_ids), cache.index
+    od = _paged_io(p, cache, n, q, out)
     if (v_new is None) != bool(p.v_in_k):
         _bad("v_new must be given unless the values are in the keys")
-    for t, name, d in ((k_new, "k_new", p.d_qk), (v_new, "v_new", p.d_v)):
-        if t is not None:
-            _want(t, name, _in_dtype(p), (n, p.n_kv_heads, 1, d) if t.dim() == 4 else (n, p.n_kv_heads, d), dev)
-    with _Device(dev, stream) as st:
-        _check(lib().snap_paged_decode_step(ctypes.byref(p.c()), ctypes.byref(cache), _ptr(rows), _ptr(pos), n,
-                                            _ptr(slot_ids),
-                                            cache.max_pages * cache.page_size if max_rows is None else max_rows,
-                                            _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), od, int(weigh),
-                                            _ptr(workspace), workspace.numel() * workspace.element_size(), st))
+    heads = (n, p.n_kv_heads) if k_new.dim() == 3 else (n, p.n_kv_heads, 1)
+    _want(k_new, "k_new", cache.in_dtype, heads + (p.d_qk,), index)
+    if v_new is not None:
+        _want(v_new, "v_new", cache.in_dtype, heads + (p.d_v,), index)
+    _launch(index, stream, lib().snap_paged_decode_step, cp, ctypes.byref(cache), _ptr(rows), _ptr(pos), n, _ptr(slot_ids),
+            cache.rows_max if max_rows is None else max_rows, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), od, int(weigh),
+            _ptr(workspace), _bytes(workspace, index))
 
 
 def snap_paged_evict(p: Params, cache: SnapPagedCache, rows, pos, slot_ids, rows_out, workspace, max_rows=None,
                      kept_out=None, stream=None):
     """Cuts slots back to the budget; rows_out [n_slots] gets the rows they then hold."""
-    import torch
-    n, dev = _paged(p, cache, rows, pos, slot_ids, pos_optional=False), cache.device
-    _want(rows_out, "rows_out", torch.int32, (cache.n_slots,), dev)
-    _want(kept_out, "kept_out", torch.int32, (n, p.n_kv_heads, p.budget), dev, optional=True)
-    if workspace.device != dev or not workspace.is_contiguous():
-        _bad(f"workspace must be contiguous on {dev}")
-    with _Device(dev, stream) as st:
-        _check(lib().snap_paged_evict(ctypes.byref(p.c()), ctypes.byref(cache), _ptr(rows), _ptr(pos), _ptr(rows_out), n,
-                                      _ptr(slot_ids),
-                                      cache.max_pages * cache.page_size if max_rows is None else max_rows,
-                                      _ptr(kept_out), _ptr(workspace), workspace.numel() * workspace.element_size(), st))
+    if pos is None:
+        _bad("pos is None")
+    (n, cp), index = _paged(p, cache, rows, pos, slot_ids), cache.index
+    _want(rows_out, "rows_out", cache.i32, cache.slots_shape, index)
+    if kept_out is not None:
+        _want(kept_out, "kept_out", cache.i32, (n, p.n_kv_heads, p.budget), index)
+    _launch(index, stream, lib().snap_paged_evict, cp, ctypes.byref(cache), _ptr(rows), _ptr(pos), _ptr(rows_out), n,
+            _ptr(slot_ids), cache.rows_max if max_rows is None else max_rows, _ptr(kept_out), _ptr(workspace),
+            _bytes(workspace, index))
 
 
 def snap_debug_checks(reset: bool = True) -> int:
