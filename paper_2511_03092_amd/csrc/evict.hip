@@ -1,10 +1,11 @@
 // evict.hip -- eviction from the paged cache by accumulated attention weight.
 //
-//   evict_select  one workgroup per (sequence, KV head): the weight of the last
-//                 row kept (radix select over the weights' bits), then the rows
-//                 to move and where to, in ascending order of both
-//   evict_move    copies those rows; sources lie from the budget on and
-//                 destinations below it, so no row is both
+//   evict_pick     one workgroup per (sequence, KV head): the weight of the last
+//                  row kept (radix select over the weights' bits), then the rows
+//                  to move and where to, in ascending order of both
+//   evict_split_*  the same in two launches, for more rows
+//   evict_move     copies those rows; sources lie from the budget on and
+//                  destinations below it, so no row is both
 #include "snap_internal.h"
 
 namespace snap {
@@ -36,120 +37,472 @@ __device__ __forceinline__ int64_t evict_row(const EvictArgs& a, int slot, int g
 
 // A row's rank among those that are not protected: its weight's bits (weights
 // are not negative, so their bits are in their order; NaN and negative: 0).
-__device__ __forceinline__ uint32_t weight_key(float w) {
-  const uint32_t u = __float_as_uint(w);
-  return u > 0x7f800000u ? 0u : u;
+__device__ __forceinline__ uint32_t weight_key(uint32_t bits) { return bits > 0x7f800000u ? 0u : bits; }
+
+// ---------------------------------------------------------------- selection
+// A row that is to be kept whatever its weight: above every weight's bits.
+constexpr uint32_t kProtected = 0xffffffffu;
+// Past the rows held, in the stored keys: like kProtected it shares no weight's
+// leading bits.
+constexpr uint32_t kAbsent = 0xfffffffeu;
+constexpr int kPickThreads = 1024;
+constexpr int kPickWaves = kPickThreads / 64;
+constexpr int kTileRows = 4 * kPickThreads;  // four neighbouring rows (of one page) a thread
+constexpr int kPickRows = 2 * kTileRows;     // rows that one workgroup selects among
+// The weights' 31 bits in three parts, the leading ones (exponent and three bits
+// more) first.
+constexpr int kParts = 3;
+constexpr int kBins = 2048;
+__device__ __forceinline__ constexpr int part_shift(int part) { return part == 0 ? 20 : (part == 1 ? 10 : 0); }
+__device__ __forceinline__ constexpr int part_bins(int part) { return part == 0 ? 2048 : 1024; }
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+// A unit's rows and counters.
+struct EvictUnit {
+  int unit, slot, g, R, late;
+};
+__device__ __forceinline__ bool evict_unit(const EvictArgs& a, int unit, EvictUnit& u) {
+  const int b = unit / a.Hkv;
+  u.unit = unit;
+  u.g = unit % a.Hkv;
+  u.slot = a.slot_ids[b];
+  if (u.slot < 0 || u.slot >= a.n_slots) return false;
+  const int R = a.rows[u.slot];
+  u.R = R < 0 ? 0 : (R > a.max_rows ? a.max_rows : R);
+  u.late = a.pos[u.slot] - a.recent;
+  return true;
 }
 
-constexpr int kSelThreads1 = 1024;
-constexpr int kSelWaves = kSelThreads1 / 64;
-
-// The number of threads before this one for which pred holds, and of all
-// (every thread calls; red: one int per wave).
-__device__ __forceinline__ int block_rank(bool pred, int* red, int& all) {
-  const int lane = tid() & 63, w = tid() >> 6;
-  const uint64_t m = __builtin_amdgcn_ballot_w64(pred);
-  __syncthreads();
-  if (lane == 0) red[w] = __builtin_popcountll(m);
-  __syncthreads();
-  int before = 0;
-  all = 0;
-  for (int i = 0; i < kSelWaves; ++i) {
-    if (i < w) before += red[i];
-    all += red[i];
+// The keys of this thread's four rows of N tiles from row r0 on (rows past R: 0).
+// No load stands behind a branch: rows that are not there are read at row 0 of page
+// 0, so that every page id, and then every row, is in flight at once.
+template <int N>
+__device__ __forceinline__ void load_keys(const EvictArgs& a, const EvictUnit& u, int r0, uint32_t (&key)[N][4]) {
+  int page[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int r = min(r0 + j * kTileRows + 4 * tid(), u.R - 1);
+    page[j] = a.table[(size_t)u.slot * a.max_pages + (r >> a.page_shift)];
   }
-  return before + __builtin_popcountll(m & ((1ull << lane) - 1));
+  i32x4 tok[N];
+  u32x4 w[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int r = r0 + j * kTileRows + 4 * tid();
+    if (page[j] >= a.n_pages || r >= u.R) page[j] = -1;
+    const int64_t row = page[j] < 0 ? 0 : (((int64_t)page[j] * a.Hkv + u.g) << a.page_shift) + (r & ((1 << a.page_shift) - 1));
+    tok[j] = *(const i32x4*)(a.token + row);
+    w[j] = *(const u32x4*)(a.weight + row);
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      key[j][e] = page[j] < 0 || r0 + j * kTileRows + 4 * tid() + e >= u.R ? 0
+                  : tok[j][e] < a.sink || tok[j][e] >= u.late             ? kProtected
+                                                                          : weight_key(w[j][e]);
 }
 
-__global__ __launch_bounds__(kSelThreads1) void evict_select(EvictArgs a) {
-  __shared__ int hist[256];
-  __shared__ int red[kSelWaves];
-  __shared__ int pick[2];
-  const int unit = bid_x(), b = unit / a.Hkv, g = unit % a.Hkv, t = tid();
-  const int slot = a.slot_ids[b], B = a.budget;
-  if (slot < 0 || slot >= a.n_slots) {
-    if (t == 0) a.count[unit] = 0;
+// Inclusive prefix sum over the wave, by lane shifts within rows of 16 and the rows'
+// last lanes handed on (vector instructions only).
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);  // from 1 lane before
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);  // 2
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);  // 4
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);  // 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // lane 15 of a row to the next: rows 1, 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // lane 31: rows 2, 3
+  return v;
+}
+__device__ __forceinline__ int wave_total(int v) { return __builtin_amdgcn_readlane(wave_scan(v), 63); }
+
+// Sums of N values over the workgroup (every thread calls; red: N ints a wave).
+template <int N>
+__device__ __forceinline__ void block_sums(int (&v)[N], int* red) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = wave_total(v[i]);
+  __syncthreads();
+  if ((tid() & 63) == 0)
+#pragma unroll
+    for (int i = 0; i < N; ++i) red[(tid() >> 6) * N + i] = v[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    v[i] = 0;
+#pragma unroll
+    for (int w = 0; w < kPickWaves; ++w) v[i] += red[w * N + i];
+  }
+}
+
+// The bin of a part's histogram that holds the rem-th largest, and how many are in
+// the bins above it; every thread calls, the histogram is complete and holds rem or
+// more.  out: {bin, above}.
+// c0, c1: this thread's counts, of bin b0 and the one below (c1 = 0: it has one),
+// the threads' bins falling.
+__device__ __forceinline__ void find_bin(int b0, int c0, int c1, int rem, int* red, int* out) {
+  const int t = tid(), lane = t & 63, w = t >> 6;
+  const int v = wave_scan(c0 + c1);
+  __syncthreads();
+  if (lane == 63) red[w] = v;
+  __syncthreads();
+  int before = v - c0 - c1;
+#pragma unroll
+  for (int i = 0; i < kPickWaves; ++i)
+    if (i < w) before += red[i];
+  if (before < rem && rem <= before + c0 + c1) {
+    out[0] = rem <= before + c0 ? b0 : b0 - 1;
+    out[1] = rem <= before + c0 ? before : before + c0;
+  }
+  __syncthreads();
+}
+
+// The same for a histogram of 1024 or 2048 bins in LDS.
+__device__ __forceinline__ void find_bin(const int* hist, int bins, int rem, int* red, int* out) {
+  const int per = bins / kPickThreads, b0 = bins - 1 - per * tid();
+  find_bin(b0, hist[b0], per == 2 ? hist[b0 - 1] : 0, rem, red, out);
+}
+
+// cnt[0 .. n), n <= 128: exclusive prefix sums in place, their total returned;
+// every thread calls.
+__device__ __forceinline__ uint32_t scan128(uint32_t* cnt, int n, uint32_t* total) {
+  __syncthreads();
+  if (tid() < 64) {
+    const int i = 2 * tid();
+    const uint32_t x0 = i < n ? cnt[i] : 0, x1 = i + 1 < n ? cnt[i + 1] : 0;
+    const uint32_t v = wave_scan(x0 + x1);
+    if (i < n) cnt[i] = v - x0 - x1;
+    if (i + 1 < n) cnt[i + 1] = v - x1;
+    if (tid() == 63) *total = v;
+  }
+  __syncthreads();
+  return *total;
+}
+
+// One workgroup a unit, which holds the keys of all its rows in registers (TILES x
+// 4096 of them): the histogram of each part of the weights that share the parts
+// before it leads to the weight of the last row kept; rows of that weight are ranked
+// by their order, then holes below the budget and kept rows behind it.  A rank is
+// the prefix of per-wave counts (ballots) plus the lanes before.  Bound by latency:
+// one read of the rows (8 bytes each), three histograms, two rankings.  Holding eight
+// tiles it takes 33 us for 18k to 32k rows, against 190 and 126 with the rows read
+// again for every 8 bits and a barrier pair for every 1024 ranked; two tiles are
+// where it is even with the launches below.
+template <int TILES>
+__global__ __launch_bounds__(kPickThreads) void evict_pick(EvictArgs a) {
+  __shared__ int hist[kBins];
+  __shared__ uint32_t cnt[TILES * kPickWaves];
+  __shared__ int red[kPickWaves], out[2];
+  __shared__ uint32_t total;
+  const int t = tid(), lane = t & 63, w = t >> 6, B = a.budget;
+  EvictUnit u;
+  if (!evict_unit(a, bid_x(), u)) {
+    if (t == 0) a.count[bid_x()] = 0;
     return;
   }
-  int R = a.rows[slot];
-  R = R < 0 ? 0 : (R > a.max_rows ? a.max_rows : R);
-  if (g == 0 && t == 0) a.rows_out[slot] = R < B ? R : B;
-  int32_t* kept = a.kept_out ? a.kept_out + (int64_t)unit * B : nullptr;
+  const int R = u.R;
+  if (u.g == 0 && t == 0) a.rows_out[u.slot] = R < B ? R : B;
+  int32_t* kept = a.kept_out ? a.kept_out + (int64_t)u.unit * B : nullptr;
   if (R <= B) {
     if (kept)
-      for (int r = t; r < B; r += kSelThreads1) kept[r] = r < R ? r : -1;
-    if (t == 0) a.count[unit] = 0;
+      for (int r = t; r < B; r += kPickThreads) kept[r] = r < R ? r : -1;
+    if (t == 0) a.count[u.unit] = 0;
     return;
   }
-  const int late = a.pos[slot] - a.recent;
-  // state of row r: protected, or its key
-  auto look = [&](int r, uint32_t& key) {
-    key = 0;
-    if (r >= R) return false;
-    const int64_t row = evict_row(a, slot, g, r);
-    if (row < 0) return false;
-    const int tok = a.token[row];
-    key = weight_key(a.weight[row]);
-    return tok < a.sink || tok >= late;
-  };
-  int prot = 0;
-  for (int r0 = 0; r0 < R; r0 += kSelThreads1) {
-    uint32_t key;
-    int all;
-    block_rank(look(r0 + t, key), red, all);
-    prot += all;
-  }
-  int want = B - prot;  // others that are kept
-  uint32_t prefix = 0, known = 0;
-  int rem = want;  // kept among those that share the prefix
-  if (want > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
+  uint32_t key[TILES][4];
+  load_keys<TILES>(a, u, 0, key);
+  int prots[1] = {0};
+#pragma unroll
+  for (int j = 0; j < TILES; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) prots[0] += key[j][e] == kProtected;
+  block_sums(prots, red);
+  const int prot = prots[0];
+  // kept: above T, and of those equal to T the first rem by row
+  uint32_t T = kProtected;
+  int rem = B;
+  if (prot < B) {
+    T = 0;
+    rem = B - prot;
+#pragma unroll
+    for (int part = 0; part < kParts; ++part) {
+      const int sh = part_shift(part), bins = part_bins(part);
+      for (int i = t; i < bins; i += kPickThreads) hist[i] = 0;
       __syncthreads();
-      if (t < 256) hist[t] = 0;
+#pragma unroll
+      for (int j = 0; j < TILES; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t k = key[j][e];
+          const bool same = part == 0 || (k >> part_shift(part ? part - 1 : 0)) == (T >> part_shift(part ? part - 1 : 0));
+          if (k != kProtected && same && j * kTileRows + 4 * t + e < R) atomicAdd(&hist[(k >> sh) & (bins - 1)], 1);
+        }
       __syncthreads();
-      for (int r = t; r < R; r += kSelThreads1) {
-        uint32_t key;
-        if (!look(r, key) && (key & known) == prefix) atomicAdd(&hist[(key >> shift) & 255], 1);
-      }
+      find_bin(hist, bins, rem, red, out);
+      T |= (uint32_t)out[0] << sh;
+      rem -= out[1];
       __syncthreads();
-      if (t == 0) {
-        int above = 0, d = 255;
-        while (d > 0 && above + hist[d] < rem) above += hist[d--];
-        pick[0] = d;
-        pick[1] = above;
-      }
-      __syncthreads();
-      prefix |= (uint32_t)pick[0] << shift;
-      known |= 255u << shift;
-      rem -= pick[1];
     }
   }
-  // rem rows of weight `prefix` are kept, the lower ones
-  int n_prot = 0, n_eq = 0, n_src = 0, n_hole = 0;
-  int32_t* src = a.src + (int64_t)unit * a.max_moves;
-  int32_t* dst = a.dst + (int64_t)unit * a.max_moves;
-  for (int r0 = 0; r0 < R; r0 += kSelThreads1) {
-    const int r = r0 + t;
-    uint32_t key;
-    int all;
-    const bool p = look(r, key);
-    const int prot_before = n_prot + block_rank(p, red, all);
-    n_prot += all;
-    bool keep = p && prot_before < B;
-    const bool eq = want > 0 && r < R && !p && key == prefix;
-    const int eq_before = n_eq + block_rank(eq, red, all);
-    n_eq += all;
-    keep = keep || (want > 0 && r < R && !p && key > prefix) || (eq && eq_before < rem);
-    const bool hole = r < B && !keep, from = r >= B && keep;
-    const int at_hole = n_hole + block_rank(hole, red, all);
-    n_hole += all;
-    const int at_src = n_src + block_rank(from, red, all);
-    n_src += all;
-    if (hole && debug_check(at_hole < a.max_moves, kDbgPagedMove)) dst[at_hole] = r;
-    if (from && debug_check(at_src < a.max_moves, kDbgPagedMove)) src[at_src] = r;
-    if (kept && r < B && keep) kept[r] = r;
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+  // rank the rows of weight T
+#pragma unroll
+  for (int j = 0; j < TILES; ++j) {
+    int c = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      c += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[j][e] == T && j * kTileRows + 4 * t + e < R));
+    if (lane == 0) cnt[j * kPickWaves + w] = c;
   }
-  if (t == 0) a.count[unit] = n_src < n_hole ? n_src : n_hole;
+  scan128(cnt, TILES * kPickWaves, &total);
+  uint32_t keep = 0;  // bit 4 j + e
+#pragma unroll
+  for (int j = 0; j < TILES; ++j) {
+    int before = cnt[j * kPickWaves + w];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      before += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[j][e] == T && j * kTileRows + 4 * t + e < R) & below);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool live = j * kTileRows + 4 * t + e < R, eq = live && key[j][e] == T;
+      if ((live && key[j][e] > T) || (eq && before < rem)) keep |= 1u << (4 * j + e);
+      before += eq;
+    }
+  }
+  // rank the holes below B (low half) and the kept rows from B on (high half)
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < TILES; ++j) {
+    uint32_t c = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int r = j * kTileRows + 4 * t + e;
+      const bool k = (keep >> (4 * j + e)) & 1;
+      c += __builtin_popcountll(__builtin_amdgcn_ballot_w64(r < B && !k));
+      c += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(r >= B && k)) << 16;
+    }
+    if (lane == 0) cnt[j * kPickWaves + w] = c;
+  }
+  const uint32_t all = scan128(cnt, TILES * kPickWaves, &total);
+  int32_t* src = a.src + (int64_t)u.unit * a.max_moves;
+  int32_t* dst = a.dst + (int64_t)u.unit * a.max_moves;
+#pragma unroll
+  for (int j = 0; j < TILES; ++j) {
+    uint32_t before = cnt[j * kPickWaves + w];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int r = j * kTileRows + 4 * t + e;
+      const bool k = (keep >> (4 * j + e)) & 1;
+      before += __builtin_popcountll(__builtin_amdgcn_ballot_w64(r < B && !k) & below);
+      before += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(r >= B && k) & below) << 16;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int r = j * kTileRows + 4 * t + e;
+      const bool k = (keep >> (4 * j + e)) & 1;
+      const int hole = before & 0xffff, from = before >> 16;
+      if (r < B && !k) {
+        if (debug_check(hole < a.max_moves, kDbgPagedMove)) dst[hole] = r;
+        before += 1;
+      } else if (r >= B && k) {
+        if (debug_check(from < a.max_moves, kDbgPagedMove)) src[from] = r;
+        before += 1u << 16;
+      } else if (r < B && kept) {
+        kept[r] = r;
+      }
+    }
+  }
+  if (t == 0) a.count[u.unit] = all & 0xffff;
+}
+
+// ---------------------------------------------------------------- selection, split
+// The same for more rows than one workgroup takes well, in two launches over about
+// 32 splits a unit at most.  The first stores the keys and each split's histogram of
+// the leading bits.  In the second every workgroup finds the weight of the last row
+// kept by itself: it adds the histograms up, reads the unit's keys for each of the
+// other two parts, counts the rows kept before its split, and writes its share of the
+// lists.  Nothing is cleared, added atomically in memory or waited for inside a
+// launch, and the three reads of 4 bytes a row hit the cache.  1 sequence x 8 heads
+// of 32k rows 5.6 + 17 us, 8 x 8 of 18k 7 + 18.
+struct SplitArgs {
+  uint32_t* keys;  // [units][row_pad]
+  int* hist;       // [units][splits][kBins]
+  int* prot;       // [units][splits] protected rows
+  int64_t row_pad;
+  int splits, split_rows;
+};
+
+__global__ __launch_bounds__(kPickThreads) void evict_split_keys(EvictArgs a, SplitArgs p) {
+  __shared__ int hist[kBins];
+  __shared__ int red[kPickWaves];
+  const int t = tid(), split = bid_x(), B = a.budget;
+  EvictUnit u;
+  if (!evict_unit(a, bid_y(), u)) {
+    if (t == 0 && split == 0) a.count[bid_y()] = 0;
+    return;
+  }
+  if (u.g == 0 && t == 0 && split == 0) a.rows_out[u.slot] = u.R < B ? u.R : B;
+  if (u.R <= B) {
+    if (a.kept_out)
+      for (int r = split * kPickThreads + t; r < B; r += p.splits * kPickThreads)
+        a.kept_out[(int64_t)u.unit * B + r] = r < u.R ? r : -1;
+    if (t == 0 && split == 0) a.count[u.unit] = 0;
+    return;
+  }
+  const int64_t at = (int64_t)u.unit * p.splits + split;
+  const int r0 = min((int64_t)split * p.split_rows, (int64_t)u.R), r1 = min((int64_t)r0 + p.split_rows, (int64_t)u.R);
+  for (int i = t; i < kBins; i += kPickThreads) hist[i] = 0;
+  __syncthreads();
+  int prot[1] = {0};
+  for (int r = r0; r < r1; r += kTileRows) {
+    uint32_t key[1][4];
+    load_keys<1>(a, u, r, key);
+    const int mine = r + 4 * t;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (mine + e >= u.R) key[0][e] = kAbsent;
+    if (mine < r1)
+      *(u32x4*)(p.keys + (int64_t)u.unit * p.row_pad + mine) = u32x4{key[0][0], key[0][1], key[0][2], key[0][3]};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (mine + e >= r1) break;
+      if (key[0][e] == kProtected)
+        ++prot[0];
+      else
+        atomicAdd(&hist[key[0][e] >> part_shift(0)], 1);
+    }
+  }
+  block_sums(prot, red);  // and the histogram is complete
+  for (int i = t; i < kBins; i += kPickThreads) p.hist[at * kBins + i] = hist[i];
+  if (t == 0) p.prot[at] = prot[0];
+}
+
+// f(r, keys of rows r .. r + 3) for a unit's stored keys of the rows before `to`,
+// four a thread.  (Held in registers between the scans they take as long: a scan is
+// bound by its compares.)
+template <typename F>
+__device__ __forceinline__ void scan_keys(const uint32_t* keys, int to, F f) {
+#pragma unroll 4
+  for (int r = 4 * tid(); r < to; r += kTileRows) f(r, *(const u32x4*)(keys + r));
+}
+
+__global__ __launch_bounds__(kPickThreads) void evict_split_lists(EvictArgs a, SplitArgs p) {
+  __shared__ int hist[2][part_bins(1)];
+  __shared__ int red[4 * kPickWaves], out[2];
+  const int t = tid(), lane = t & 63, w = t >> 6, split = bid_x(), B = a.budget;
+  EvictUnit u;
+  if (!evict_unit(a, bid_y(), u) || u.R <= B) return;
+  const uint32_t* keys = p.keys + (int64_t)u.unit * p.row_pad;
+  // the splits' histograms of the leading bits, two bins a thread from the top
+  const int* first = p.hist + (int64_t)u.unit * p.splits * kBins + kBins - 2 - 2 * t;
+  int prot[1] = {0}, c0 = 0, c1 = 0;
+  if (t < p.splits) prot[0] = p.prot[(int64_t)u.unit * p.splits + t];
+#pragma unroll 8
+  for (int s = 0; s < p.splits; ++s) {
+    const int2 v = *(const int2*)(first + (int64_t)s * kBins);
+    c0 += v.y;
+    c1 += v.x;
+  }
+  hist[0][t] = hist[1][t] = 0;
+  block_sums(prot, red);
+  // kept: above T, and of those equal to T the first rem by row
+  uint32_t T = kProtected;
+  int rem = B;
+  if (prot[0] < B) {
+    rem = B - prot[0];
+    find_bin(kBins - 1 - 2 * t, c0, c1, rem, red, out);
+    T = (uint32_t)out[0] << part_shift(0);
+    rem -= out[1];
+#pragma unroll
+    for (int part = 1; part < kParts; ++part) {
+      __syncthreads();  // out is read
+      scan_keys(keys, u.R, [&](int, u32x4 k) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (k[e] >> part_shift(part - 1) == T >> part_shift(part - 1))
+            atomicAdd(&hist[part - 1][(k[e] >> part_shift(part)) & (part_bins(part) - 1)], 1);
+      });
+      __syncthreads();
+      find_bin(hist[part - 1], part_bins(part), rem, red, out);
+      T |= (uint32_t)out[0] << part_shift(part);
+      rem -= out[1];
+    }
+  }
+  const int r0 = min((int64_t)split * p.split_rows, (int64_t)u.R), r1 = min((int64_t)r0 + p.split_rows, (int64_t)u.R);
+  // rows above T and equal to it before this split, and below B (for the number of
+  // moves, and where rows from B on go)
+  int c[4] = {0, 0, 0, 0};
+  const bool low = split == 0 || r1 > B;
+  scan_keys(keys, low ? max(r0, B) : r0, [&](int r, u32x4 k) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      c[0] += k[e] > T && r + e < r0;
+      c[1] += k[e] == T && r + e < r0;
+      c[2] += k[e] > T && r + e < B;
+      c[3] += k[e] == T && r + e < B;
+    }
+  });
+  block_sums(c, red);
+  int eq = c[1], kept_before = c[0] + min(rem, c[1]);
+  const int kept_low = c[2] + min(rem, c[3]);  // low only
+  if (t == 0 && split == 0) a.count[u.unit] = B - kept_low;
+  int32_t* kept = a.kept_out ? a.kept_out + (int64_t)u.unit * B : nullptr;
+  int32_t* src = a.src + (int64_t)u.unit * a.max_moves;
+  int32_t* dst = a.dst + (int64_t)u.unit * a.max_moves;
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+  for (int tile = r0; tile < r1; tile += kTileRows) {
+    const int r = tile + 4 * t;
+    const u32x4 k = r < r1 ? *(const u32x4*)(keys + r) : u32x4{0u, 0u, 0u, 0u};
+    int n = 0, before = eq;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint64_t m = __builtin_amdgcn_ballot_w64(r + e < r1 && k[e] == T);
+      n += __builtin_popcountll(m);
+      before += __builtin_popcountll(m & below);
+    }
+    __syncthreads();
+    if (lane == 0) red[w] = n;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPickWaves; ++i) {
+      if (i < w) before += red[i];
+      eq += red[i];
+    }
+    bool keep[4];
+    int rank = kept_before;  // kept rows before this thread's; the holes before row r are r - rank
+    n = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool live = r + e < r1, same = live && k[e] == T;
+      keep[e] = live && (k[e] > T || (same && before < rem));
+      before += same;
+      const uint64_t m = __builtin_amdgcn_ballot_w64(keep[e]);
+      n += __builtin_popcountll(m);
+      rank += __builtin_popcountll(m & below);
+    }
+    __syncthreads();
+    if (lane == 0) red[w] = n;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPickWaves; ++i) {
+      if (i < w) rank += red[i];
+      kept_before += red[i];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (r + e >= r1) break;
+      if (r + e < B) {
+        if (!keep[e]) {
+          if (debug_check(r + e - rank < a.max_moves, kDbgPagedMove)) dst[r + e - rank] = r + e;
+        } else if (kept) {
+          kept[r + e] = r + e;
+        }
+      } else if (keep[e] && debug_check(rank - kept_low < a.max_moves, kDbgPagedMove)) {
+        src[rank - kept_low] = r + e;
+      }
+      rank += keep[e];
+    }
+  }
 }
 
 // block x: share of the moves, y: unit
@@ -190,6 +543,21 @@ EvictGeometry evict_geometry(const snap_params& p, int n, int max_rows) {
   const int behind = max_rows > budget ? max_rows - budget : 0;
   g.max_moves = behind < budget ? behind : budget;
   size_t off = 0;
+  g.splits = 0;
+  if (max_rows > kPickRows) {
+    // a tile each, or more rows where there would be over 32 of them or more
+    // workgroups than CUs: every split reads all of its unit's keys
+    const int most = units >= 256 ? 1 : (256 / units < 32 ? 256 / units : 32);
+    g.split_rows = (int)((max_rows + (int64_t)most * kTileRows - 1) / ((int64_t)most * kTileRows)) * kTileRows;
+    g.splits = (max_rows + g.split_rows - 1) / g.split_rows;
+    g.row_pad = ((size_t)max_rows + 3) & ~(size_t)3;
+    g.off_keys = off;
+    off = align256(off + (size_t)units * g.row_pad * sizeof(uint32_t));
+    g.off_hist = off;
+    off = align256(off + (size_t)units * g.splits * kBins * sizeof(int));
+    g.off_prot = off;
+    off = align256(off + (size_t)units * g.splits * sizeof(int));
+  }
   g.off_count = off;
   off = align256(off + (size_t)units * sizeof(int32_t));
   g.off_src = off;
@@ -232,11 +600,26 @@ snap_status launch_paged_evict(const snap_params& p, const snap_paged_cache& c, 
   a.kbytes = p.d_qk * elt;
   a.vbytes = p.v_in_k ? 0 : p.d_v * elt;
   const int units = n * p.n_kv_heads;
-  hipLaunchKernelGGL(evict_select, dim3(units), dim3(kSelThreads1), 0, stream, a);
+  if (!geo.splits) {
+    hipLaunchKernelGGL(evict_pick<kPickRows / kTileRows>, dim3(units), dim3(kPickThreads), 0, stream, a);
+  } else {
+    unsigned char* base = (unsigned char*)ws;
+    SplitArgs sp;
+    sp.keys = (uint32_t*)(base + geo.off_keys);
+    sp.hist = (int*)(base + geo.off_hist);
+    sp.prot = (int*)(base + geo.off_prot);
+    sp.row_pad = (int64_t)geo.row_pad;
+    sp.splits = geo.splits;
+    sp.split_rows = geo.split_rows;
+    const dim3 grid(geo.splits, units);
+    hipLaunchKernelGGL(evict_split_keys, grid, dim3(kPickThreads), 0, stream, a, sp);
+    if (hipGetLastError() != hipSuccess) return SNAP_ERR_HIP;
+    hipLaunchKernelGGL(evict_split_lists, grid, dim3(kPickThreads), 0, stream, a, sp);
+  }
   if (hipGetLastError() != hipSuccess) return SNAP_ERR_HIP;
   if (geo.max_moves > 0) {
     const int64_t pieces = (int64_t)geo.max_moves * ((a.kbytes + a.vbytes) / 16);
-    const int shares = (int)(pieces < 256 * 64 ? (pieces + 255) / 256 : 64);
+    const int shares = (int)(pieces < 256 * 256 ? (pieces + 255) / 256 : 256);
     hipLaunchKernelGGL(evict_move, dim3(shares, units), dim3(256), 0, stream, a, shares);
     if (hipGetLastError() != hipSuccess) return SNAP_ERR_HIP;
   }

@@ -108,16 +108,17 @@ def fill(c: Paged, slots, lengths, seed, pos=None):
     p = c.p
     st = c.state()
     for s, n in zip(slots, lengths):
-        for r, (page, off) in enumerate(c.places(s, max(0, n))):
-            if not 0 <= page < c.n_pages:
+        pl = [(r, a, o) for r, (a, o) in enumerate(c.places(s, max(0, n))) if 0 <= a < c.n_pages]
+        if not pl:
+            continue
+        r, a, o = (torch.tensor(x, dtype=torch.long) for x in zip(*pl))
+        for name, d in (("k", p.d_qk), ("v", p.d_v)):
+            if st[name] is None:
                 continue
-            for name, d in (("k", p.d_qk), ("v", p.d_v)):
-                if st[name] is None:
-                    continue
-                x = torch.randn((p.n_kv_heads, d), generator=g)
-                st[name][page, :, off] = (x / 0.015).clamp(-448, 448).to(FP8).view(torch.uint8) if c.kv == "fp8" else x.to(KV[c.kv])
-            st["weight"][page, :, off] = torch.rand(p.n_kv_heads, generator=g)
-            st["token"][page, :, off] = r if pos is None else pos[r]
+            x = torch.randn((len(pl), p.n_kv_heads, d), generator=g)
+            st[name][a, :, o] = (x / 0.015).clamp(-448, 448).to(FP8).view(torch.uint8) if c.kv == "fp8" else x.to(KV[c.kv])
+        st["weight"][a, :, o] = torch.rand((len(pl), p.n_kv_heads), generator=g)
+        st["token"][a, :, o] = (r if pos is None else torch.as_tensor(pos)[r]).to(torch.int32)[:, None]
     for name in ("k", "v", "weight", "token"):
         if st[name] is not None:
             getattr(c, name).copy_(st[name])

@@ -250,21 +250,22 @@ def test_append_of_prompts(name, packed):
             assert torch.equal(want[x].view(torch.uint8), after[x].view(torch.uint8)), x
 
 
-def _evict_case(p, kv, page, slots, rows, pos, tokens, weights, max_rows=None, n_slots=None):
-    """Runs an eviction over given tokens and weights [sequence][head][row] and checks every byte."""
+def _evict_case(p, kv, page, slots, rows, pos, tokens, weights, max_rows=None, n_slots=None, table_rows=0):
+    """Runs an eviction over given tokens and weights [sequence][head][row] and checks every byte.  table_rows: the page
+    table has room for so many, and so the call for as many rows."""
     n, B, h = len(slots), p.budget, p.n_kv_heads
     n_slots = n_slots or max(slots) + 1
     cap = [0] * n_slots
     for s, r in zip(slots, rows):
         cap[s] = r
-    c = fill(Paged(p, kv, n_slots, page, cap, 1), slots, rows, 2)
+    c = fill(Paged(p, kv, n_slots, page, cap, 1, max_pages=table_rows // page or None), slots, rows, 2)
     st = c.state()
     for b, s in enumerate(slots):
         c.rows[s], c.pos[s] = rows[b], pos[b]
-        for r, (pg, off) in enumerate(c.places(s, rows[b])):
-            for g in range(h):
-                st["token"][pg, g, off] = int(tokens[b][g][r])
-                st["weight"][pg, g, off] = float(weights[b][g][r])
+        pg, off = (torch.tensor(x, dtype=torch.long) for x in zip(*c.places(s, rows[b]) or [(0, 0)]))
+        for g in range(h if rows[b] else 0):
+            st["token"][pg, g, off] = torch.as_tensor(np.asarray(tokens[b][g]).astype(np.int32))
+            st["weight"][pg, g, off] = torch.as_tensor(np.asarray(weights[b][g]).astype(np.float32))
     c.token.copy_(st["token"])
     c.weight.copy_(st["weight"])
     out = torch.full((n_slots,), -3, dtype=torch.int32, device="cuda")
@@ -285,10 +286,13 @@ def _evict_case(p, kv, page, slots, rows, pos, tokens, weights, max_rows=None, n
             w = np.float32(weights[b][g][:R])
             exp = evict(np.asarray(tokens[b][g][:R]), w, R, pos[b], p.sink, p.recent, B)
             assert np.array_equal(got[b, g], exp), (b, g, np.flatnonzero(got[b, g] != exp)[:5])
-            for r in range(min(R, B)):
+            to = np.flatnonzero((exp >= 0) & (exp != np.arange(B)))
+            if len(to):
+                (tp, to_), (fp, fo) = ((torch.tensor(x, dtype=torch.long) for x in zip(*[pl[i] for i in idx]))
+                                       for idx in (to, exp[to]))
                 for x in ("k", "v", "token", "weight"):
-                    if want[x] is not None and exp[r] != r:
-                        want[x][pl[r][0], g, pl[r][1]] = before[x][pl[exp[r]][0], g, pl[exp[r]][1]]
+                    if want[x] is not None:
+                        want[x][tp, g, to_] = before[x][fp, g, fo]
     for x in ("k", "v", "token", "weight", "rows", "pos"):
         if want[x] is not None:
             assert torch.equal(want[x].contiguous().view(torch.uint8), after[x].contiguous().view(torch.uint8)), x
@@ -297,8 +301,10 @@ def _evict_case(p, kv, page, slots, rows, pos, tokens, weights, max_rows=None, n
     return c
 
 
+# the calls' most rows: what one workgroup selects among, and more (the rows held are the same)
+@pytest.mark.parametrize("table_rows", [0, 1 << 14])
 @pytest.mark.parametrize("name", list(SHAPES))
-def test_evict_ragged(name):
+def test_evict_ragged(name, table_rows):
     """Slots above, at and below the budget, tokens in any order, weights with many ties."""
     p, kv, page = _shape(name, sink=3, recent=9, topk=40)
     rows = [200, 52, 53, 7, 0, 97, 1030]
@@ -308,12 +314,13 @@ def test_evict_ragged(name):
     tokens = [[rng.permutation(r + 30)[:r] for _ in range(p.n_kv_heads)] for r in rows]
     weights = [[np.round(rng.exponential(1.0, r) * 4) / 4 for _ in range(p.n_kv_heads)] for r in rows]
     print(f"\n[case] evict {name}, rows {rows}, budget {p.budget}", flush=True)
-    _evict_case(p, kv, page, slots, rows, pos, tokens, weights, n_slots=9)
+    _evict_case(p, kv, page, slots, rows, pos, tokens, weights, n_slots=9, table_rows=table_rows)
 
 
+@pytest.mark.parametrize("table_rows", [0, 9000 // 32 * 32, 1 << 18])
 @pytest.mark.parametrize("what", ["all-equal", "zeros", "nan-and-negative", "huge-and-tiny", "ascending", "no-topk",
                                   "no-sink", "all-protected", "one-row-over", "max-rows"])
-def test_evict_edges(what):
+def test_evict_edges(what, table_rows):
     over = dict(sink=2, recent=5, topk=30)
     rows, max_rows = 300, None
     if what == "no-topk":
@@ -342,13 +349,25 @@ def test_evict_edges(what):
     elif what == "all-protected":
         tok = [[np.zeros(rows, int) for _ in range(2)]]
     print(f"\n[case] evict {what}", flush=True)
-    _evict_case(p, kv, page, [0], [rows], [rows], tok, [w], max_rows=max_rows)
+    _evict_case(p, kv, page, [0], [rows], [rows], tok, [w], max_rows=max_rows, table_rows=table_rows)
+
+
+@pytest.mark.parametrize("topk", [0, 1, 2, 3, 4091, 4092, 4093, 4094, 4095, 8190, 8999])
+def test_evict_to_budgets_around_the_splits(topk):
+    """Budgets at every remainder of 4 and around whole tiles, rows that end inside one; weights with ties, so that the
+    rows of the last weight kept lie on both sides of the budget."""
+    p, kv, page = _shape("f32-d64", sink=0, recent=1, topk=topk)
+    rng = np.random.default_rng(topk)
+    rows = [9003, topk + 2, 8193]
+    print(f"\n[case] evict {rows} rows to {p.budget}", flush=True)
+    _evict_case(p, kv, page, [1, 0, 2], rows, rows, [[rng.permutation(r) for _ in range(2)] for r in rows],
+                [np.round(rng.exponential(1.0, (2, r)) * 2).astype(np.float32) for r in rows])
 
 
 def test_evict_of_a_long_sequence():
-    """Past the rows that one pass of a workgroup holds, most of them evicted, and most kept."""
+    """Many splits, and splits of several tiles; most rows evicted, and most kept."""
     rng = np.random.default_rng(11)
-    for rows, topk in ((40001, 500), (36007, 33000)):
+    for rows, topk in ((40001, 500), (36007, 33000), (150001, 70003)):
         p = params(4, 2, 64, "bf16", sink=4, recent=100, topk=topk)
         print(f"\n[case] evict {rows} rows to {p.budget}", flush=True)
         _evict_case(p, "bf16", 256, [0], [rows], [rows], [[rng.permutation(rows) for _ in range(2)]],
@@ -517,5 +536,6 @@ def test_debug_build_records_no_failed_invariant_of_the_paged_calls(debug_librar
     for name in ("gqa-bf16", "g3-fp8", "f32-d64", "latent-bf16", "latent-fp8"):
         test_decode_of_ragged_sequences(name, True)
         test_step_is_append_then_attention(name)
-        test_evict_ragged(name)
+        test_evict_ragged(name, 0)
+        test_evict_ragged(name, 1 << 14)
         assert snap.snap_debug_checks(reset=True) == 0, name
