@@ -268,6 +268,45 @@ __device__ __forceinline__ bool paged_item(const PagedArgs& a, int item, PagedIt
   return true;
 }
 
+// The share of wave w of `waves` that take unit `unit` together (none of the rows
+// where there are fewer blocks); the last has the new token.  false: no such slot.
+__device__ __forceinline__ bool paged_unit(const PagedArgs& a, int unit, int w, int waves, PagedItem& it) {
+  it.s = {};
+  it.s.b = unit / a.Hkv;
+  it.g = unit % a.Hkv;
+  int slot;
+  it.s.len = uniform(rows_of(a, it.s.b, slot));
+  it.s.slot = uniform(slot);
+  if (it.s.slot < 0 || it.s.slot >= a.n_slots) return false;
+  it.s.blocks = (it.s.len + kBlockRows - 1) / kBlockRows;
+  it.r0 = min(it.s.len, w * it.s.blocks / waves * kBlockRows);
+  it.r1 = min(it.s.len, (w + 1) * it.s.blocks / waves * kBlockRows);
+  it.rnew = a.k_new && it.s.len > 0 && w == waves - 1 ? uniform(a.rows[it.s.slot]) : -1;
+  return true;
+}
+
+// Adds the softmax weights of rows r .. r + 3 (those before `end`), at index `row` of
+// their page, summed over the unit's heads in order; z: the unit's logits, ml:
+// reference and 1 / sum of every head.  Row rnew has no weight yet.
+__device__ __forceinline__ void add_weights(const PagedArgs& a, const float* z, const float2* ml, int64_t row, int r, int end,
+                                            int rnew) {
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int h = 0; h < a.G; ++h) {
+    const f32x4 y = *(const f32x4*)(z + ((int64_t)(r / kBlockRows) * a.G + h) * kBlockRows + r % kBlockRows);
+    const float2 m = ml[h];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] = fmaf(fast_exp2(y[e] - m.x), m.y, sum[e]);
+  }
+  if (r + 4 <= end && !(rnew >= r && rnew < r + 4)) {
+    f32x4* p = (f32x4*)(a.weight + row);
+    *p = *p + sum;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (r + e < end) a.weight[row + e] = (r + e == rnew ? 0.f : a.weight[row + e]) + sum[e];
+  }
+}
+
 // W: the logits go to the workspace, for the weights.  They are staged in LDS and
 // leave in runs of 16 KB: writes between the streaming reads cost by their number
 // more than by their bytes (8 sequences of 4k to 128k rows, 142 MB of logits beside
@@ -275,18 +314,28 @@ __device__ __forceinline__ bool paged_item(const PagedArgs& a, int item, PagedIt
 // waves a CU leave each 20 KB of LDS.
 constexpr int kZStage = 4096;  // logits that are staged before they leave
 
-template <int D, int KV, bool NT, bool W>
-__global__ __launch_bounds__(64) void paged_gqa(PagedArgs a) {
-  extern __shared__ __align__(16) float zstage[];  // W: kZStage and a block more
+// WAVES > 1: one workgroup takes a whole unit, each wave a share of its blocks, joins
+// them in LDS, writes the output and adds the weights (whose logits stay in LDS): one
+// launch instead of two, for calls so short that launches and dependent loads are
+// most of them.
+template <int D, int KV, bool NT, bool W, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void paged_gqa(PagedArgs a) {
+  // WAVES == 1, W: kZStage logits and a block more; WAVES > 1: [WAVES / 2][G][D] for
+  // the join, then, W, the unit's logits
+  extern __shared__ __align__(16) float zstage[];
   constexpr int E = KV == kKvFp8 ? 1 : (KV == kKvBf16 ? 2 : 4);  // bytes of an element
   constexpr int NK = D * E / 64;                                 // key loads a half
   constexpr int VE = D / 16;                                     // value dims a lane
   constexpr int NQ = KV == kKvFp8 ? 2 * NK : NK;                 // query pieces
   constexpr int NF = KV == kKvF32 ? VE : 1;
   typedef uint32_t VRaw __attribute__((ext_vector_type(VE * E / 4)));
-  const int lane = tid(), l16 = lane & 15, lg = lane >> 4, item = bid_x();
+  const int lane = tid() & 63, w = WAVES == 1 ? 0 : uniform(tid() >> 6), l16 = lane & 15, lg = lane >> 4, item = bid_x();
   PagedItem it;
-  if (!paged_item(a, item, it)) return;
+  if constexpr (WAVES == 1) {
+    if (!paged_item(a, item, it)) return;
+  } else {
+    if (!paged_unit(a, item, w, WAVES, it)) return;
+  }
   const int slot = it.s.slot, g = it.g, r0 = it.r0, r1 = it.r1, b = it.s.b;
   PageIds pages;
   pages.load(a, slot, r0 >> a.page_shift);
@@ -306,7 +355,8 @@ __global__ __launch_bounds__(64) void paged_gqa(PagedArgs a) {
   }
   const float ksc = KV == kKvFp8 ? a.k_scale[(size_t)slot * a.Hkv + g] : 1.f;
   const float vsc = KV == kKvFp8 ? (a.cv ? a.v_scale : a.k_scale)[(size_t)slot * a.Hkv + g] : 1.f;
-  const float xs = a.scale * kLog2e * ksc;
+  float xs = a.scale * kLog2e * ksc;
+  settle(xs);
   // the new token's row in the cache's form: pieces of its input (fp8: the codes,
   // quantised once into LDS, keys in [0, D), values after them)
   __shared__ __align__(16) unsigned char newq[KV == kKvFp8 ? 2 * D : 16];
@@ -324,7 +374,7 @@ __global__ __launch_bounds__(64) void paged_gqa(PagedArgs a) {
         *(u32x2*)(newq + 8 * lane) = bf16_to_codes(*(const u32x4*)(vnew + 16 * (lane - kc)), vsc);
       knew = newq;
       vnew = newq + D;
-      __syncthreads();
+      asm volatile("" ::: "memory");  // one wave's LDS operations take effect in order
     }
   }
 
@@ -353,14 +403,15 @@ __global__ __launch_bounds__(64) void paged_gqa(PagedArgs a) {
   f32x4 acc[VE];
 #pragma unroll
   for (int c = 0; c < VE; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float* z = W ? a.z + (it.s.block0 + (int64_t)g * it.s.blocks) * a.G * kBlockRows : nullptr;
+  float* zunit = zstage + (WAVES / 2) * a.G * D;  // WAVES > 1
+  float* z = W && WAVES == 1 ? a.z + (it.s.block0 + (int64_t)g * it.s.blocks) * a.G * kBlockRows : nullptr;
   int zrow = r0;  // first row staged
 
 #pragma unroll
   for (int j = 0; j < NQ; ++j) settle(q[j]);
   settle(pages.id);
   u32x4 k0[NK], k1[NK];
-  int64_t h0 = pages.row(a, slot, g, r0), h1 = r0 + 16 < r1 ? pages.row(a, slot, g, r0 + 16) : -1;
+  int64_t h0 = r0 < r1 ? pages.row(a, slot, g, r0) : -1, h1 = r0 + 16 < r1 ? pages.row(a, slot, g, r0 + 16) : -1;
   load_k(r0, h0, h1, k0, k1);
   for (int vb = r0; vb < r1; vb += 32) {
     // values of this block, then keys of the next: the second product waits for
@@ -427,12 +478,12 @@ __global__ __launch_bounds__(64) void paged_gqa(PagedArgs a) {
     }
     if constexpr (W) {
       if (hval) {
-        float* st = zstage + (vb - zrow) * a.G + l16 * kBlockRows + 4 * lg;
+        float* st = (WAVES == 1 ? zstage + (vb - zrow) * a.G : zunit + vb * a.G) + l16 * kBlockRows + 4 * lg;
         *(f32x4*)st = f32x4{x[0], x[1], x[2], x[3]} * xs;
         *(f32x4*)(st + 16) = f32x4{x[4], x[5], x[6], x[7]} * xs;
       }
       const int staged = (vb + 32 - zrow) * a.G;
-      if (staged >= kZStage || vb + 32 >= r1) {
+      if (WAVES == 1 && (staged >= kZStage || vb + 32 >= r1)) {
         // one wave, whose LDS operations take effect in order: no barrier (which
         // would also wait for the loads in flight), only the compiler is held
         asm volatile("" ::: "memory");
@@ -513,8 +564,70 @@ __global__ __launch_bounds__(64) void paged_gqa(PagedArgs a) {
         *(u32x4*)((unsigned char*)const_cast<void*>(a.cv) + row * (D * E) + 16 * (lane - kp)) =
             *(const u32x4*)(vnew + 16 * (lane - kp));
       if (lane == 0 && a.token) a.token[row] = a.pos[slot];
-      if (lane == 0 && a.weight) a.weight[row] = 0.f;
+      // (with weights a joined unit's first is written with the sum below)
+      if (lane == 0 && a.weight && !(W && WAVES > 1 && it.rnew < r1)) a.weight[row] = 0.f;
     }
+  }
+  if constexpr (WAVES > 1) {
+    __shared__ float2 mls[WAVES][16];
+    __shared__ float2 joined[16];  // reference and 1 / sum of every head
+    if (lg == 0) mls[w][l16] = make_float2(m, lsum);
+    __syncthreads();
+    float M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) M = fmaxf(M, mls[i][l16].x);
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) {
+      const float2 v = mls[i][l16];
+      if (v.x != -INFINITY) L = fmaf(fast_exp2(v.x - M), v.y, L);
+    }
+    const float inv = L > 0.f ? 1.f / L : 0.f, f = m == -INFINITY ? 0.f : fast_exp2(m - M) * inv * vsc;
+    if (w == 0 && lg == 0) joined[l16] = make_float2(M, inv);
+#pragma unroll
+    for (int c = 0; c < VE; ++c) acc[c] *= f;
+    // the upper half of the waves hand theirs to the lower, until one has the sum
+#pragma unroll
+    for (int half = WAVES / 2; half >= 1; half /= 2) {
+      float* to = zstage + ((w & (half - 1)) * a.G + l16) * D + 4 * lg * VE;
+      if (w >= half && w < 2 * half && hval)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int c = 0; c < VE; c += 4)
+            *(f32x4*)(to + e * VE + c) = f32x4{acc[c][e], acc[c + 1][e], acc[c + 2][e], acc[c + 3][e]};
+      __syncthreads();
+      if (w < half && hval)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int c = 0; c < VE; c += 4) {
+            const f32x4 v = *(const f32x4*)(to + e * VE + c);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[c + i][e] += v[i];
+          }
+      __syncthreads();
+    }
+    if (w == 0 && hval) {
+      const size_t oi = ((size_t)b * a.Hq + g * a.G + l16) * D + 4 * lg * VE;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int c = 0; c < VE; c += 4) {
+          if (a.out_bf16)
+            *(u32x2*)((uint16_t*)a.out + oi + e * VE + c) =
+                u32x2{pack_bf16x2(acc[c][e], acc[c + 1][e]), pack_bf16x2(acc[c + 2][e], acc[c + 3][e])};
+          else
+            *(f32x4*)((float*)a.out + oi + e * VE + c) = f32x4{acc[c][e], acc[c + 1][e], acc[c + 2][e], acc[c + 3][e]};
+        }
+    }
+    if constexpr (W) {
+      const int rnew = a.k_new ? uniform(a.rows[slot]) : -1;
+      for (int r = 4 * tid(); r < it.s.len; r += 4 * 64 * WAVES) {
+        const int64_t row = paged_row(a, slot, g, r);  // four rows of one page
+        if (row >= 0) add_weights(a, zunit, joined, row, r, it.s.len, rnew);
+      }
+    }
+    return;
   }
   if (!hval) return;
   const size_t pi = (size_t)item * a.G + l16;
@@ -838,19 +951,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join(PagedArgs a, int merg
   for (int r = it.r0 + 4 * t; r < it.r1; r += 4 * kJoinThreads) {
     const int64_t row = paged_row(a, it.s.slot, it.g, r);  // four rows of one page
     if (row < 0) continue;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (int h = 0; h < a.G; ++h) {
-      const f32x4 y = *(const f32x4*)(z + ((int64_t)(r / kBlockRows) * a.G + h) * kBlockRows + r % kBlockRows);
-      const float2 ml = sml[h];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] = fmaf(fast_exp2(y[e] - ml.x), ml.y, sum[e]);
-    }
-    if (r + 4 <= it.r1) {
-      f32x4* p = (f32x4*)(a.weight + row);
-      *p = *p + sum;
-    } else {
-      for (int e = 0; r + e < it.r1; ++e) a.weight[row + e] += sum[e];
-    }
+    add_weights(a, z, sml, row, r, it.r1, -1);
   }
 }
 
@@ -956,6 +1057,25 @@ static int resident_items(const snap_params& p, bool weigh) {
 }
 
 // ---------------------------------------------------------------- host side
+// The waves of a workgroup that takes a whole unit of 64- or 128-wide rows in one
+// launch, or 0 where the rows are cut into items: up to 32 KB and 128 rows a wave,
+// twice that where the units fill the card with such workgroups.  A block a wave is
+// 2.2 us of dependent loads (128-wide bf16), the second launch 3 to 4.  Measured, one
+// launch against two, 8 KV heads of 32 query heads, us:
+//   128-wide bf16  1 sequence: 512 rows 11.6 / 11.9, 1024 16.1 / 11.8;
+//                  64 sequences: 1024 49 / 57, 2048 103 / 97
+//   64-wide fp8    1: 1024 rows 10.1 / 11.4, 2048 14.7 / 11.3; 64: 2048 27 / 38
+//   128-wide fp32  1: 64 rows 8.7 / 12.6, 256 13.8 / 12.7; 64: 256 35 / 42, 1024 118 / 110
+constexpr int kJoinedLogits = 6144;  // with weights: beside 32 KB for the join, within 64 KB of LDS
+static int joined_waves(const snap_params& p, int n, int max_rows, bool weigh) {
+  const int G = p.n_q_heads / p.n_kv_heads, rows_pad = (max_rows + kBlockRows - 1) / kBlockRows * kBlockRows;
+  const int elt = p.kv_dtype == SNAP_F32 ? 4 : (p.kv_dtype == SNAP_BF16 ? 2 : 1);
+  const int row_bytes = (p.d_qk + (p.v_in_k ? 0 : p.d_v)) * elt;
+  const int waves = p.kv_dtype == SNAP_F32 && p.d_qk == 128 ? 4 : 8;  // by the registers of a wave
+  const int share = (32768 / row_bytes < 128 ? 32768 / row_bytes : 128) * (n * p.n_kv_heads * waves >= 2048 ? 2 : 1);
+  return p.d_qk == p.d_v && max_rows <= share * waves && !(weigh && (int64_t)rows_pad * G > kJoinedLogits) ? waves : 0;
+}
+
 PagedGeometry paged_geometry(const snap_params& p, int n, int max_rows, bool weigh) {
   PagedGeometry g{};
   const int units = (n > 0 ? n : 1) * p.n_kv_heads, G = p.n_q_heads / p.n_kv_heads;
@@ -1070,13 +1190,26 @@ snap_status launch_paged_decode(const snap_params& p, const snap_paged_cache& c,
     void (*k)(PagedArgs) = kernels[p.kv_dtype == SNAP_FP8_E4M3][nt][weigh];
     hipLaunchKernelGGL(k, dim3(geo.max_items), dim3(256), 0, stream, a);
   } else {
+    const int kv = p.kv_dtype == SNAP_F32 ? kKvF32 : (p.kv_dtype == SNAP_BF16 ? kKvBf16 : kKvFp8);
+    if (const int waves = joined_waves(p, n, max_rows, weigh)) {
+      static constexpr void (*kernels[2][3][2])(PagedArgs) = {  // [width][type][W]
+          {{paged_gqa<64, kKvBf16, false, false, 8>, paged_gqa<64, kKvBf16, false, true, 8>},
+           {paged_gqa<64, kKvFp8, false, false, 8>, paged_gqa<64, kKvFp8, false, true, 8>},
+           {paged_gqa<64, kKvF32, false, false, 8>, paged_gqa<64, kKvF32, false, true, 8>}},
+          {{paged_gqa<128, kKvBf16, false, false, 8>, paged_gqa<128, kKvBf16, false, true, 8>},
+           {paged_gqa<128, kKvFp8, false, false, 8>, paged_gqa<128, kKvFp8, false, true, 8>},
+           {paged_gqa<128, kKvF32, false, false, 4>, paged_gqa<128, kKvF32, false, true, 4>}}};
+      const int rows_pad = (max_rows + kBlockRows - 1) / kBlockRows * kBlockRows;
+      hipLaunchKernelGGL(kernels[p.d_qk == 128][kv][weigh], dim3(n * p.n_kv_heads), dim3(64 * waves),
+                         ((size_t)(waves / 2) * a.G * p.d_v + (weigh ? (size_t)rows_pad * a.G : 0)) * sizeof(float), stream, a);
+      return hipGetLastError() == hipSuccess ? SNAP_OK : SNAP_ERR_HIP;
+    }
     static constexpr void (*kernels[2][3][2][2])(PagedArgs) = {  // [width][type][NT][W]
 #define SNAP_PAGED_GQA(D, KV) \
-  {{paged_gqa<D, KV, false, false>, paged_gqa<D, KV, false, true>}, {paged_gqa<D, KV, true, false>, paged_gqa<D, KV, true, true>}}
+  {{paged_gqa<D, KV, false, false, 1>, paged_gqa<D, KV, false, true, 1>}, {paged_gqa<D, KV, true, false, 1>, paged_gqa<D, KV, true, true, 1>}}
         {SNAP_PAGED_GQA(64, kKvBf16), SNAP_PAGED_GQA(64, kKvFp8), SNAP_PAGED_GQA(64, kKvF32)},
         {SNAP_PAGED_GQA(128, kKvBf16), SNAP_PAGED_GQA(128, kKvFp8), SNAP_PAGED_GQA(128, kKvF32)}};
 #undef SNAP_PAGED_GQA
-    const int kv = p.kv_dtype == SNAP_F32 ? kKvF32 : (p.kv_dtype == SNAP_BF16 ? kKvBf16 : kKvFp8);
     void (*k)(PagedArgs) = kernels[p.d_qk == 128][kv][nt][weigh];
     hipLaunchKernelGGL(k, dim3(geo.max_items), dim3(64),
                        weigh ? (kZStage + kBlockRows * a.G) * sizeof(float) : 0, stream, a);
