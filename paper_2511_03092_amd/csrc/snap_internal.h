@@ -119,6 +119,19 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
+// Inclusive prefix sum over the wave, by lane shifts within rows of 16 and the rows'
+// last lanes handed on (vector instructions only).
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);  // from 1 lane before
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);  // 2
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);  // 4
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);  // 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // lane 15 of a row to the next: rows 1, 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // lane 31: rows 2, 3
+  return v;
+}
+__device__ __forceinline__ int wave_total(int v) { return __builtin_amdgcn_readlane(wave_scan(v), 63); }
+
 // ---------------------------------------------------------------- debug checks
 // Built with SNAP_DEBUG_CHECKS (libsnapstream_debug.so), kernels test the
 // invariants their indexing rests on and record a violated one as a bit of a
