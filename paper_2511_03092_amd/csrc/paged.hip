@@ -24,7 +24,6 @@ namespace snap {
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kBlockRows = 32;  // rows of a block
 // with the SNAP_KV_AUTO hint, calls of at least this many cache bytes (at
 // max_rows) read with streaming loads: half the 256 MB last-level cache
@@ -51,7 +50,7 @@ struct PagedArgs {
   const int32_t* pos;
   int32_t* token;
   int n, Hq, Hkv, G, dk, dv, n_slots, n_pages, page_shift, max_pages, max_rows, waves, target, max_items, out_bf16;
-  float scale;
+  float scale2, scale2_lo;  // scale * log2(e) in two terms, both > 0
 };
 
 // The rows sequence b attends (0 for a slot id out of range).
@@ -185,6 +184,13 @@ __device__ __forceinline__ u32x2 bf16_to_codes(u32x4 raw, float scale) {
     f[2 * i + 1] = bf16_bits_to_f32(raw[i] >> 16) / scale;
   }
   return u32x2{e4m3x4_hw(f[0], f[1], f[2], f[3]), e4m3x4_hw(f[4], f[5], f[6], f[7])};
+}
+
+// Four products as logits in log2 units: the scale's second term keeps its rounding
+// (6e-8 relative, 1e-6 of a probability whose logit is 16) out of them.  It is
+// positive, so a masked product's -inf stays -inf.
+__device__ __forceinline__ f32x4 logits4(const float* x, float xs, float xlo) {
+  return f32x4{fmaf(x[0], xs, x[0] * xlo), fmaf(x[1], xs, x[1] * xlo), fmaf(x[2], xs, x[2] * xlo), fmaf(x[3], xs, x[3] * xlo)};
 }
 
 // Eight probabilities as two bf16 terms (pe is used up).  The second is kept off
@@ -348,7 +354,7 @@ __global__ __launch_bounds__(64 * WAVES) void paged_gqa(PagedArgs a) {
   }
   const float ksc = KV == kKvFp8 ? a.k_scale[(size_t)slot * a.Hkv + g] : 1.f;
   const float vsc = KV == kKvFp8 ? (a.cv ? a.v_scale : a.k_scale)[(size_t)slot * a.Hkv + g] : 1.f;
-  float xs = a.scale * kLog2e * ksc;
+  float xs = a.scale2 * ksc, xlo = fmaxf(a.scale2_lo * ksc, 1e-37f);
   settle(xs);
   // the new token's row in the cache's form: pieces of its input (fp8: the codes,
   // quantised once into LDS, keys in [0, D), values after them)
@@ -435,7 +441,7 @@ __global__ __launch_bounds__(64 * WAVES) void paged_gqa(PagedArgs a) {
       load_k(vb + 32, nh0, nh1, n0, n1);
     }
 
-    f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+    f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f}, f0[4] = {}, f1[4] = {};
 #pragma unroll
     for (int j = 0; j < NK; ++j) {
       if constexpr (KV == kKvBf16) {
@@ -452,12 +458,16 @@ __global__ __launch_bounds__(64 * WAVES) void paged_gqa(PagedArgs a) {
         }
       } else {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < 4; ++u) {  // four sums of D / 4 products: shorter chains of roundings
           const float qq = __uint_as_float(q[j][u]);
-          s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k0[j][u]), qq, s0, 0, 0, 0);
-          s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k1[j][u]), qq, s1, 0, 0, 0);
+          f0[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k0[j][u]), qq, f0[u], 0, 0, 0);
+          f1[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k1[j][u]), qq, f1[u], 0, 0, 0);
         }
       }
+    }
+    if constexpr (KV == kKvF32) {
+      s0 = (f0[0] + f0[1]) + (f0[2] + f0[3]);
+      s1 = (f1[0] + f1[1]) + (f1[2] + f1[3]);
     }
     float x[8];
 #pragma unroll
@@ -472,8 +482,8 @@ __global__ __launch_bounds__(64 * WAVES) void paged_gqa(PagedArgs a) {
     if constexpr (W) {
       if (hval) {
         float* st = (WAVES == 1 ? zstage + (vb - zrow) * a.G : zunit + vb * a.G) + l16 * kBlockRows + 4 * lg;
-        *(f32x4*)st = f32x4{x[0], x[1], x[2], x[3]} * xs;
-        *(f32x4*)(st + 16) = f32x4{x[4], x[5], x[6], x[7]} * xs;
+        *(f32x4*)st = logits4(x, xs, xlo);
+        *(f32x4*)(st + 16) = logits4(x + 4, xs, xlo);
       }
       const int staged = (vb + 32 - zrow) * a.G;
       if (WAVES == 1 && (staged >= kZStage || vb + 32 >= r1)) {
@@ -501,7 +511,7 @@ __global__ __launch_bounds__(64 * WAVES) void paged_gqa(PagedArgs a) {
     }
     float pe[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) pe[i] = fast_exp2(fmaf(x[i], xs, -mref));
+    for (int i = 0; i < 8; ++i) pe[i] = fast_exp2(fmaf(x[i], xs, fmaf(x[i], xlo, -mref)));
     lsum += ((pe[0] + pe[1]) + (pe[2] + pe[3])) + ((pe[4] + pe[5]) + (pe[6] + pe[7]));
     if constexpr (KV == kKvF32) {
 #pragma unroll
@@ -694,7 +704,7 @@ __global__ __launch_bounds__(256, FP8 ? 2 : 1) void paged_latent(PagedArgs a) {
   const unsigned char* cache = (const unsigned char*)a.ck;
   const unsigned char* knew = it.rnew >= 0 ? (const unsigned char*)a.k_new + ((size_t)b * a.Hkv + g) * (D * 2) : nullptr;
   const float ksc = FP8 ? a.k_scale[(size_t)slot * a.Hkv + g] : 1.f;
-  const float xs = a.scale * kLog2e * ksc;
+  const float xs = a.scale2 * ksc, xlo = fmaxf(a.scale2_lo * ksc, 1e-37f);
   // lane group lg feeds the piece 18 lg + t (fp8: half t % 2 of 9 lg + t / 2) of a
   // row to k-step t
   bf16x8 q[18];
@@ -790,7 +800,7 @@ __global__ __launch_bounds__(256, FP8 ? 2 : 1) void paged_latent(PagedArgs a) {
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         if (vb + 16 * k < r1)
-          *(f32x4*)(zb + (k >> 1) * a.G * kBlockRows + 16 * (k & 1)) = f32x4{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]} * xs;
+          *(f32x4*)(zb + (k >> 1) * a.G * kBlockRows + 16 * (k & 1)) = logits4(x + 4 * k, xs, xlo);
     }
     float bm = -INFINITY;
 #pragma unroll
@@ -812,7 +822,7 @@ __global__ __launch_bounds__(256, FP8 ? 2 : 1) void paged_latent(PagedArgs a) {
     for (int kk = 0; kk < 2; ++kk) {
       float pe[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) pe[k] = fast_exp2(fmaf(x[8 * kk + k], xs, -mref));
+      for (int k = 0; k < 8; ++k) pe[k] = fast_exp2(fmaf(x[8 * kk + k], xs, fmaf(x[8 * kk + k], xlo, -mref)));
       lsum += ((pe[0] + pe[1]) + (pe[2] + pe[3])) + ((pe[4] + pe[5]) + (pe[6] + pe[7]));
       bf16x8 p[2];
       two_terms(pe, p);
@@ -1187,7 +1197,7 @@ snap_status launch_paged_decode(const snap_params& p, const snap_paged_cache& c,
   a.target = geo.target;
   a.max_items = geo.max_items;
   a.out_bf16 = out_dtype == SNAP_BF16;
-  a.scale = p.sm_scale > 0.f ? p.sm_scale : 1.0f / sqrtf((float)p.d_qk);
+  split_scale2(p.sm_scale > 0.f ? p.sm_scale : 1.0f / sqrtf((float)p.d_qk), a.scale2, a.scale2_lo);
   a.k_new = k_new;
   a.v_new = v_new;
   a.pos = pos;
