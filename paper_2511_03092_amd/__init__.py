@@ -418,18 +418,18 @@ def paged_cache_struct(k, v, page_table, token=None, weight=None, k_scale=None, 
 
 def _paged(p: Params, cache: SnapPagedCache, rows, pos, slot_ids):
     """Checks what every paged call shares; the number of sequences and the parameters' structure."""
-    values = tuple(vars(p).values())
-    if cache.params[0] != values:  # the same parameters as the last call's: the same structure
+    values, params = tuple(vars(p).values()), cache.params
+    if params[0] != values:  # (the same parameters as the last call's: the same structure)
         kind = (p.kv_dtype, p.n_kv_heads, p.d_qk, None if p.v_in_k else p.d_v)
         if cache.kind != kind:
             _bad(f"the cache (type, heads, widths {cache.kind}) is not that of the parameters ({kind})")
-        cache.params = (values, p.c())
+        cache.params = params = (values, p.c())
     n, index = slot_ids.shape[0], cache.index
     _want(slot_ids, "slot_ids", cache.i32, (n,), index)
     _want(rows, "rows", cache.i32, cache.slots_shape, index)
     if pos is not None:
         _want(pos, "pos", cache.i32, cache.slots_shape, index)
-    return n, ctypes.byref(cache.params[1])
+    return n, ctypes.byref(params[1])
 
 
 def _strides(t, name: str, dtype, shape: tuple, index: int):

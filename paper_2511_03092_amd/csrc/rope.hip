@@ -262,9 +262,10 @@ snap_status launch_rope(const snap_rope_params& r, int dtype, int n_seq, int max
     a.x[o] = op[o]->x;
     a.y[o] = op[o]->y;
     a.heads[o] = op[o]->n_heads;
-    for (int i = 0; i < 3; ++i) {
-      a.xs[o][i] = op[o]->x_stride[i];
-      a.ys[o][i] = op[o]->y_stride[i];
+    const int size[3] = {n_seq, op[o]->n_heads, max_len};
+    for (int i = 0; i < 3; ++i) {  // (a stride along a size of 1 says nothing)
+      a.xs[o][i] = size[i] > 1 ? op[o]->x_stride[i] : 0;
+      a.ys[o][i] = size[i] > 1 ? op[o]->y_stride[i] : 0;
     }
     in_place = in_place && op[o]->x == op[o]->y;
   }

@@ -522,6 +522,125 @@ def test_two_streams_on_their_own_caches():
         assert torch.equal(torch.nan_to_num(c.weight), torch.nan_to_num(w[1]))
 
 
+@pytest.mark.parametrize("name,length", [("gqa-bf16", 60), ("gqa-bf16", 3000), ("f32-d64", 2500), ("d64-fp8", 2500),
+                                         ("latent-bf16", 700), ("latent-fp8", 700)])
+def test_captured_steps_replay(name, length):
+    """A step with weights captured once and replayed, the counters moving inside the graph, beside eager steps of a twin
+    cache that shares the workspace: the same bits after every replay."""
+    p, kv, page = _shape(name)
+    lengths, slots = [length, length // 3], [1, 0]
+    print(f"\n[case] captured paged step {name}, rows {lengths}", flush=True)
+    cap = [length // 3 + 8, length + 8]
+    two = [fill(Paged(p, kv, 2, page, cap, 1), slots, lengths, 2) for _ in range(2)]
+    for c in two:
+        for s, x in zip(slots, lengths):
+            c.rows[s], c.pos[s] = x, x + 9
+    ids, ml = _i32(slots), two[0].c.max_pages * page
+    ws = snap.workspace(snap.snap_paged_decode_workspace(p, 2, ml, True))
+    g = torch.Generator().manual_seed(6)
+    q = _queries(p, kv, 2, 7)
+    kn = torch.randn((2, p.n_kv_heads, 1, p.d_qk), generator=g).to(IN[kv]).cuda()
+    vn = None if p.v_in_k else torch.randn((2, p.n_kv_heads, 1, p.d_v), generator=g).to(IN[kv]).cuda()
+    outs = [torch.empty((2, p.n_q_heads, p.d_v), dtype=IN[kv], device="cuda") for _ in range(2)]
+
+    def step(i):
+        c = two[i]
+        snap.snap_paged_decode_step(p, c.c, c.rows, c.pos, ids, q, kn, vn, outs[i], ws, weigh=True)
+        snap.snap_advance(c.rows, ids)
+        snap.snap_advance(c.pos, ids)
+
+    step(0)
+    step(1)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(0)
+    for i in range(4):
+        q.copy_(_queries(p, kv, 2, 30 + i))
+        graph.replay()
+        torch.cuda.synchronize()
+        step(1)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], outs[1]), i
+        a, b = (c.state() for c in two)
+        for x in ("k", "v", "token", "weight", "rows", "pos"):
+            if a[x] is not None:
+                assert torch.equal(a[x].view(torch.uint8), b[x].view(torch.uint8)), (i, x)
+
+
+@pytest.mark.parametrize("name", ["gqa-bf16", "f32-d64", "latent-fp8", "latent-bf16"])
+@pytest.mark.parametrize("bound", [40, 2000])
+def test_step_past_max_rows_stores_the_token_without_attending_it(name, bound):
+    p, kv, page = _shape(name)
+    held = bound + 7
+    print(f"\n[case] paged step {name}, {held} rows of which {bound} are attended", flush=True)
+    c = fill(Paged(p, kv, 1, page, [held + 1], 1), [0], [held], 2)
+    c.rows[0], c.pos[0] = held, 500
+    before = c.state()
+    g = torch.Generator().manual_seed(5)
+    kn = torch.randn((1, p.n_kv_heads, p.d_qk), generator=g).to(IN[kv]).cuda()
+    vn = None if p.v_in_k else torch.randn((1, p.n_kv_heads, p.d_v), generator=g).to(IN[kv]).cuda()
+    q = _queries(p, kv, 1, 7)
+    out = torch.empty((1, p.n_q_heads, p.d_v), dtype=IN[kv], device="cuda")
+    snap.snap_paged_decode_step(p, c.c, c.rows, c.pos, _i32([0]), q, kn, vn, out,
+                                snap.workspace(snap.snap_paged_decode_workspace(p, 1, bound, True)), max_rows=bound,
+                                weigh=True)
+    torch.cuda.synchronize()
+    pg, off = c.places(0, held + 1)[-1]
+    before["weight"][pg, :, off] = 0
+    _check_decode(c, [0], [bound], q, out, before)
+    assert bool((c.token[pg, :, off] == 500).all())
+    if kv != "fp8":
+        assert torch.equal(c.k[pg, :, off], kn[0])
+
+
+@pytest.mark.parametrize("name,pages", [("gqa-bf16", 40000), ("latent-bf16", 60000)])
+def test_pages_past_four_gigabytes(name, pages):
+    """Pages whose elements lie past 2^31 and whose bytes past 2^32, through all four calls."""
+    p, kv, page = _shape(name, sink=2, recent=20, topk=100)
+    print(f"\n[case] paged calls {name}, {pages} pages of {page} rows", flush=True)
+    h, length, dev = p.n_kv_heads, 300, "cuda"
+    small = fill(Paged(p, kv, 1, page, [length + 1], 1), [0], [length], 2)
+    big = Paged.__new__(Paged)
+    big.p, big.kv, big.page, big.n_slots, big.n_pages, big.max_pages = p, kv, page, 1, pages, small.max_pages
+    big.k_scale = big.v_scale = None
+    big.k = torch.empty((pages, h, page, p.d_qk), dtype=torch.bfloat16, device=dev)
+    big.v = None if p.v_in_k else torch.empty((pages, h, page, p.d_v), dtype=torch.bfloat16, device=dev)
+    big.token = torch.zeros((pages, h, page), dtype=torch.int32, device=dev)
+    big.weight = torch.zeros((pages, h, page), device=dev)
+    assert big.k.numel() > 1 << 31
+    n = small.max_pages
+    ids = [pages - 1 - 3 * j for j in range(n)]
+    big.table = torch.tensor([ids], dtype=torch.int32, device=dev)
+    for x in ("k", "v", "token", "weight"):
+        if getattr(big, x) is not None:
+            getattr(big, x)[ids] = getattr(small, x)[small.table[0].long()]
+    big.rows, big.pos = small.rows.clone(), small.pos.clone()
+    big.handle()
+    ids = _i32([0])
+    g = torch.Generator().manual_seed(5)
+    kn = torch.randn((1, h, 1, p.d_qk), generator=g).to(IN[kv]).cuda()
+    vn = None if p.v_in_k else torch.randn((1, h, 1, p.d_v), generator=g).to(IN[kv]).cuda()
+    q, ml = _queries(p, kv, 1, 7), n * page
+    got = []
+    for c in (small, big):
+        c.rows[0] = c.pos[0] = length
+        ws = snap.workspace(max(snap.snap_paged_decode_workspace(p, 1, ml, True), snap.snap_paged_evict_workspace(p, 1, ml)))
+        out = torch.empty((1, p.n_q_heads, p.d_v), dtype=IN[kv], device=dev)
+        snap.snap_paged_append(p, c.c, c.rows, c.pos, ids, kn, vn)
+        snap.snap_paged_decode_step(p, c.c, c.rows, c.pos, ids, q, kn, vn, out, ws, weigh=True)
+        snap.snap_advance(c.rows, ids)
+        snap.snap_advance(c.pos, ids)
+        rows_out = torch.zeros_like(c.rows)
+        kept = torch.empty((1, h, p.budget), dtype=torch.int32, device=dev)
+        snap.snap_paged_evict(p, c.c, c.rows, c.pos, ids, rows_out, ws, kept_out=kept)
+        torch.cuda.synchronize()
+        pg = c.table[0].long()
+        got.append([out, kept] + [getattr(c, x)[pg] for x in ("k", "v", "token", "weight") if getattr(c, x) is not None])
+    for a, b in zip(*got):
+        assert torch.equal(torch.nan_to_num(a.float()), torch.nan_to_num(b.float()))
+
+
 @pytest.fixture
 def debug_library():
     prev = snap.use_library(snap.DEBUG_LIB_PATH)
