@@ -389,12 +389,18 @@ __global__ __launch_bounds__(64 * WAVES) void paged_gqa(PagedArgs a) {
       }
       return;
     }
+    // A lane whose row is not there reads row 0 of page 0 (its logit is masked), the
+    // new token's its input: the address is chosen, not the load, so that all loads
+    // of the block are in flight together.
+    const int ra = vb + l16, rb = ra + 16;
+    if (h0 < 0 || ra >= r1) p0 = kbase + 16 * lg;
+    else if (KV != kKvFp8 && ra == it.rnew) p0 = knew + 16 * lg;
+    if (h1 < 0 || rb >= r1) p1 = kbase + 16 * lg;
+    else if (KV != kKvFp8 && rb == it.rnew) p1 = knew + 16 * lg;
 #pragma unroll
     for (int j = 0; j < NK; ++j) {
-      k0[j] = k1[j] = u32x4{0u, 0u, 0u, 0u};
-      if (h0 >= 0 && vb + l16 < r1) k0[j] = vb + l16 == it.rnew ? *(const u32x4*)(knew + 16 * lg + 64 * j) : load_as<NT, u32x4>(p0 + 64 * j);
-      if (h1 >= 0 && vb + 16 + l16 < r1)
-        k1[j] = vb + 16 + l16 == it.rnew ? *(const u32x4*)(knew + 16 * lg + 64 * j) : load_as<NT, u32x4>(p1 + 64 * j);
+      k0[j] = load_as<NT, u32x4>(p0 + 64 * j);
+      k1[j] = load_as<NT, u32x4>(p1 + 64 * j);
     }
   };
 
@@ -424,13 +430,13 @@ __global__ __launch_bounds__(64 * WAVES) void paged_gqa(PagedArgs a) {
       for (int i = 0; i < 8; ++i) v[i] = load_as<NT, VRaw>((i < 4 ? p0 : p1) + (i & 3) * (D * E));
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < 8; ++i) {  // as for the keys; a value whose row is not there is zeroed before its product
         const int r = vb + (i < 4 ? 0 : 16) + 4 * lg + (i & 3);
         const int64_t hb = i < 4 ? h0 : h1;
-        v[i] = VRaw{};
-        if (hb >= 0 && r < r1)
-          v[i] = r == it.rnew ? *(const VRaw*)(vnew + l16 * (VE * E))
-                              : load_as<NT, VRaw>(vbase + ((size_t)hb + 4 * lg + (i & 3)) * (D * E) + l16 * (VE * E));
+        const unsigned char* from = vbase + ((size_t)hb + 4 * lg + (i & 3)) * (D * E);
+        if (hb < 0 || r >= r1) from = vbase;
+        else if (KV != kKvFp8 && r == it.rnew) from = vnew;
+        v[i] = load_as<NT, VRaw>(from + l16 * (VE * E));
       }
     }
     u32x4 n0[NK], n1[NK];
@@ -441,6 +447,15 @@ __global__ __launch_bounds__(64 * WAVES) void paged_gqa(PagedArgs a) {
       load_k(vb + 32, nh0, nh1, n0, n1);
     }
 
+    const bool fresh = KV == kKvFp8 && it.rnew >= vb && it.rnew < min(r1, vb + 32);  // its codes are in LDS
+    if (fresh) {
+#pragma unroll
+      for (int j = 0; j < NK; ++j) {
+        const u32x4 c = *(const u32x4*)(newq + 16 * lg + 64 * j);
+        k0[j] = vb + l16 == it.rnew ? c : k0[j];
+        k1[j] = vb + 16 + l16 == it.rnew ? c : k1[j];
+      }
+    }
     f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f}, f0[4] = {}, f1[4] = {};
 #pragma unroll
     for (int j = 0; j < NK; ++j) {
@@ -513,6 +528,14 @@ __global__ __launch_bounds__(64 * WAVES) void paged_gqa(PagedArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) pe[i] = fast_exp2(fmaf(x[i], xs, fmaf(x[i], xlo, -mref)));
     lsum += ((pe[0] + pe[1]) + (pe[2] + pe[3])) + ((pe[4] + pe[5]) + (pe[6] + pe[7]));
+    if (!whole || fresh) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = vb + (i < 4 ? 0 : 16) + 4 * lg + (i & 3);
+        if ((i < 4 ? h0 : h1) < 0 || r >= r1) v[i] = VRaw{};
+        else if (fresh && r == it.rnew) v[i] = *(const VRaw*)(newq + D + l16 * (VE * E));
+      }
+    }
     if constexpr (KV == kKvF32) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
