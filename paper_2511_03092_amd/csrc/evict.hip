@@ -492,7 +492,9 @@ __global__ __launch_bounds__(kPickThreads) void evict_split_lists(EvictArgs a, S
   }
 }
 
-// block x: share of the moves, y: unit
+// block x: share of the moves, y: unit.  8 x 8 units of 1500 moves of 520 bytes (100 MB
+// read and written) 24 us, 4.2 TB/s; few moves are bound by the chain of dependent
+// loads (list, page, row): 8 units of 1300, 9 us.
 __global__ __launch_bounds__(256) void evict_move(EvictArgs a, int shares) {
   const int unit = bid_y(), b = unit / a.Hkv, g = unit % a.Hkv;
   const int n = a.count[unit];

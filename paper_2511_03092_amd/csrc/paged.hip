@@ -149,6 +149,9 @@ __device__ __forceinline__ int64_t paged_row(const PagedArgs& a, int slot, int g
 // a page table.
 // A head's reference maximum moves only when a block's exceeds it by kStaleMax
 // (log2 units), so the accumulators are rescaled on few blocks.
+// HBM bound: 8 sequences of 19k to 128k rows x 8 KV heads, 128-wide bf16 (2.52 GB) 397
+// us, 6.3 TB/s with the join; fp8 209 us, 6.0 TB/s.  Values prefetched a block ahead
+// like the keys change nothing, there or for short sequences.
 // 16-bit and fp8 rows: probabilities enter the products as two bf16 terms of 8
 // bits each, truncated: off by under 2^-16 relative.  One term would be off by up
 // to 2^-8, which the heaviest rows of a head show in the output; the second costs
@@ -308,8 +311,8 @@ __device__ __forceinline__ void put_weights(const PagedArgs& a, int64_t row, int
 
 // W: the logits go to the workspace, for the weights.  They are staged in LDS and
 // leave in runs of 16 KB: writes between the streaming reads cost by their number
-// more than by their bytes (8 sequences of 4k to 128k rows, 142 MB of logits beside
-// 2.28 GB: 512-byte runs 527 us, 1 KB runs 510, 16 KB runs 450, none 397).  Eight
+// more than by their bytes (8 sequences of 19k to 128k rows, 79 MB of logits beside
+// 2.52 GB: 512-byte runs 527 us, 1 KB runs 510, 16 KB runs 455, none 392).  Eight
 // waves a CU leave each 20 KB of LDS.
 constexpr int kZStage = 4096;  // logits that are staged before they leave
 
@@ -682,6 +685,10 @@ __global__ __launch_bounds__(64 * WAVES) void paged_gqa(PagedArgs a) {
 // Rows past the sequence and in pages that are not there are loaded from a row of
 // zeros: their probabilities are zero, and zero times whatever else might stand
 // there need not be.
+// HBM bound in bf16: 16 sequences of 32k rows (604 MB) 100 us, 6.0 TB/s; blocks of 32
+// rows in four stages, the dims of a product split over the waves, take as long.  fp8
+// (302 MB, 16 heads) 70 us: the conversions, and a block's two barriers with two
+// workgroups a CU; the 32-row form takes 82.
 constexpr int kLatRows = 64;
 __device__ const u32x4 kZeroRow[72] = {};
 
@@ -1041,7 +1048,9 @@ __device__ __forceinline__ void store8(const In* src, Out* dst, float scale) {
   }
 }
 
-// block x: tokens 32x .. 32x + 31, y: KV head, z: sequence
+// block x: tokens 32x .. 32x + 31, y: KV head, z: sequence.  HBM bound: four prompts of
+// 32k tokens or fewer out of the packed projection (622 MB) 137 us, 4.5 TB/s (a copy:
+// 4.7).
 constexpr int kAppendTokens = 32;
 template <typename In, typename Out>
 __global__ __launch_bounds__(256) void paged_append(PagedAppendArgs a) {
@@ -1105,22 +1114,28 @@ static int resident_items(const snap_params& p, bool weigh) {
 
 // ---------------------------------------------------------------- host side
 // The waves of a workgroup that takes a whole unit of 64- or 128-wide rows in one
-// launch, or 0 where the rows are cut into items: up to 32 KB and 128 rows a wave,
-// twice that where the units fill the card with such workgroups.  A block a wave is
-// 2.2 us of dependent loads (128-wide bf16), the second launch 3 to 4.  Measured, one
-// launch against two, 8 KV heads of 32 query heads, us:
-//   128-wide bf16  1 sequence: 512 rows 11.6 / 11.9, 1024 16.1 / 11.8;
-//                  64 sequences: 1024 49 / 57, 2048 103 / 97
-//   64-wide fp8    1: 1024 rows 10.1 / 11.4, 2048 14.7 / 11.3; 64: 2048 27 / 38
-//   128-wide fp32  1: 64 rows 8.7 / 12.6, 256 13.8 / 12.7; 64: 256 35 / 42, 1024 118 / 110
+// launch, or 0 where the rows are cut into items.  With few units one launch pays
+// while a wave has four blocks of 64-wide rows, two of 128-wide ones or one of fp32
+// (a further block is about 2 us of dependent work, the second launch 2.5); with
+// enough units to fill the card, while it has eight, or four of 512 bytes a row and
+// more (then also nothing is written for the join).  Measured, one launch / two, 32
+// query heads on 8, us:
+//   rows               256        512        1024       2048
+//   128 bf16   1 x   8.9/11.5  10.8/11.5  15.3/11.3  23.9/11.3   64 x  20/25  29/35  47/55  99/95
+//   128 fp8    1 x   8.6/11.1  10.4/11.3  13.9/11.2  20.4/11.6   64 x  16/20  24/26  33/36  52/57
+//   64 fp8     1 x   8.5/11.1   8.5/11.1  10.7/11.2  15.6/11.3   64 x   9/20  12/22  18/27  28/38
+//   64 fp32    1 x   8.6/11.2  12.1/11.3  18.1/11.3  29.3/11.2   64 x  20/26  30/36  49/56 102/97
+//   128 fp32   1 x  12.6/11.3  18.7/11.3  29.2/11.4  50.1/12.4   64 x  31/37  50/58 106/103
 constexpr int kJoinedLogits = 6144;  // with weights: beside 32 KB for the join, within 64 KB of LDS
 static int joined_waves(const snap_params& p, int n, int max_rows, bool weigh) {
-  const int G = p.n_q_heads / p.n_kv_heads, rows_pad = (max_rows + kBlockRows - 1) / kBlockRows * kBlockRows;
-  const int elt = p.kv_dtype == SNAP_F32 ? 4 : (p.kv_dtype == SNAP_BF16 ? 2 : 1);
-  const int row_bytes = (p.d_qk + (p.v_in_k ? 0 : p.d_v)) * elt;
-  const int waves = p.kv_dtype == SNAP_F32 && p.d_qk == 128 ? 4 : 8;  // by the registers of a wave
-  const int share = (32768 / row_bytes < 128 ? 32768 / row_bytes : 128) * (n * p.n_kv_heads * waves >= 2048 ? 2 : 1);
-  return p.d_qk == p.d_v && max_rows <= share * waves && !(weigh && (int64_t)rows_pad * G > kJoinedLogits) ? waves : 0;
+  if (p.d_qk != p.d_v) return 0;
+  const bool f32 = p.kv_dtype == SNAP_F32;
+  const int blocks = (max_rows + kBlockRows - 1) / kBlockRows;
+  const int waves = f32 && p.d_qk == 128 ? 4 : 8;  // by the registers of a wave
+  const int row_bytes = (p.d_qk + p.d_v) * (f32 ? 4 : (p.kv_dtype == SNAP_BF16 ? 2 : 1));
+  const int share = n * p.n_kv_heads * waves >= 2048 ? (row_bytes >= 512 ? 4 : 8) : (f32 ? 1 : (p.d_qk == 64 ? 4 : 2));
+  const bool fits = !weigh || (int64_t)blocks * kBlockRows * (p.n_q_heads / p.n_kv_heads) <= kJoinedLogits;
+  return blocks <= share * waves && fits ? waves : 0;
 }
 
 PagedGeometry paged_geometry(const snap_params& p, int n, int max_rows, bool weigh) {
@@ -1263,7 +1278,7 @@ snap_status launch_paged_decode(const snap_params& p, const snap_paged_cache& c,
   }
   if (hipGetLastError() != hipSuccess) return SNAP_ERR_HIP;
   // 128-dim slices (8 items at a time), or 32-dim ones (32 at a time) where a unit
-  // has many items: 1 sequence x 8 KV heads of 32k rows, 256 items each, 9.6 -> 6 us
+  // has many items: 1 sequence x 8 KV heads of 32k rows, 256 items each, 9.4 -> 5.8 us
   const bool many = geo.max_items > 32 * n * p.n_kv_heads;
   const int merges = n * p.n_q_heads * (many ? p.d_v / 32 : (p.d_v == 512 ? 4 : 1));
   const dim3 join(merges + (weigh ? geo.max_items : 0));
