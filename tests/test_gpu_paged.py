@@ -101,9 +101,12 @@ def test_decode_of_ragged_sequences(name, weigh):
 
 
 @pytest.mark.parametrize("name,n,length", [("gqa-bf16", 1, 9000), ("g3-fp8", 2, 5001), ("latent-bf16", 1, 6000),
-                                           ("latent-fp8", 1, 4099), ("f32-d64", 1, 3001), ("g1-d64-bf16", 1, 7777)])
+                                           ("latent-fp8", 1, 4099), ("f32-d64", 1, 3001), ("g1-d64-bf16", 1, 7777),
+                                           ("g16-bf16", 1, 384), ("g16-bf16", 1, 385), ("f32-d128-g5", 2, 128),
+                                           ("f32-d128-g5", 1, 129), ("d64-fp8", 1, 768), ("d64-fp8", 1, 1025)])
 @pytest.mark.parametrize("hint", [snap.SNAP_KV_STREAM, snap.SNAP_KV_KEEP])
 def test_decode_of_long_sequences_split_over_the_card(name, n, length, hint):
+    """Sequences cut into many items, and lengths around those that one workgroup takes whole."""
     p, kv, page = _shape(name, kv_reuse=hint)
     lengths = [length - 100 * b for b in range(n)]
     print(f"\n[case] paged decode {name}, lengths {lengths}, load hint {hint}", flush=True)
