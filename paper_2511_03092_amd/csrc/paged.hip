@@ -56,9 +56,9 @@ struct PagedArgs {
 // The rows sequence b attends (0 for a slot id out of range).
 __device__ __forceinline__ int rows_of(const PagedArgs& a, int b, int& slot) {
   slot = a.slot_ids[b];
-  if (slot < 0 || slot >= a.n_slots) return 0;
-  const int r = a.rows[slot];
-  return r < 0 ? 0 : (r >= a.max_rows ? a.max_rows : r + 1);
+  const bool ok = slot >= 0 && slot < a.n_slots;
+  const int r = a.rows[ok ? slot : 0];  // no branch: the loads of several sequences go out together
+  return !ok || r < 0 ? 0 : (r >= a.max_rows ? a.max_rows : r + 1);
 }
 
 // One sequence of the cut: its blocks, items per unit, the items of the
@@ -73,15 +73,17 @@ struct PagedSeq {
 // otherwise sequence `key`.  false: there is none.
 __device__ __forceinline__ bool paged_seq(const PagedArgs& a, int key, bool by_item, PagedSeq& s) {
   const int lane = tid() & 63;
-  int64_t total = 0;
+  int64_t mine = 0;
   int nb0 = 0;
+#pragma unroll 4
   for (int b0 = 0; b0 < a.n; b0 += 64) {
     int slot;
-    const int b = b0 + lane;
-    const int nb = b < a.n ? (rows_of(a, b, slot) + kBlockRows - 1) / kBlockRows : 0;
+    const int b = b0 + lane, len = rows_of(a, min(b, a.n - 1), slot);
+    const int nb = b < a.n ? (len + kBlockRows - 1) / kBlockRows : 0;
     if (b0 == 0) nb0 = nb;
-    total += wave_total(nb);
+    mine += nb;
   }
+  const int64_t total = wave_total((int)(mine & 0xfffff)) + ((int64_t)wave_total((int)(mine >> 20)) << 20);
   // Blocks an item: as few as keep the items within a.waves.  total / waves of
   // them may give more (a unit's last item is short), total / target never does;
   // up to 64 sequences, whose lengths the lanes hold, some between are tried.
@@ -98,12 +100,12 @@ __device__ __forceinline__ bool paged_seq(const PagedArgs& a, int key, bool by_i
     }
   }
   const int C = c64 < 1 ? 1 : (int)c64;
-  int items_before = 0;
+  int items_before = 0, slot_next;
   int64_t blocks_before = 0;
+  int len_next = rows_of(a, min(lane, a.n - 1), slot_next);
   for (int b0 = 0; b0 < a.n; b0 += 64) {
-    int slot = -1;
-    const int b = b0 + lane;
-    const int len = b < a.n ? rows_of(a, b, slot) : 0;
+    const int b = b0 + lane, slot = slot_next, len = b < a.n ? len_next : 0;
+    if (b0 + 64 < a.n) len_next = rows_of(a, min(b + 64, a.n - 1), slot_next);  // while this one is counted
     const int nb = (len + kBlockRows - 1) / kBlockRows;
     const int ni = (nb + C - 1) / C;
     const int si = wave_scan(ni), sb = wave_scan(nb);
