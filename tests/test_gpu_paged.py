@@ -115,12 +115,13 @@ def test_decode_of_long_sequences_split_over_the_card(name, n, length, hint):
     _check_decode(c, list(range(n)), lengths, q, out, before)
 
 
-@pytest.mark.parametrize("name", ["gqa-bf16", "latent-bf16", "f32-d64", "g3-fp8"])
-def test_decode_of_many_short_sequences(name):
-    """More (sequence, KV head) units than work items are wanted, of 1 to 40 rows."""
+@pytest.mark.parametrize("name,n", [("gqa-bf16", 300), ("latent-bf16", 300), ("f32-d64", 300), ("g3-fp8", 300),
+                                    ("latent-bf16", 530), ("latent-fp8", 1030), ("latent-two-heads", 270)])
+def test_decode_of_many_short_sequences(name, n):
+    """More (sequence, KV head) units than work items are wanted, of 0 to 40 rows and one of 700."""
     p, kv, page = _shape(name)
-    n = 300
     lengths = [(7 * b) % 41 for b in range(n)]
+    lengths[n // 2] = 700
     print(f"\n[case] paged decode {name}, {n} sequences of 0 to 40 rows", flush=True)
     c = fill(Paged(p, kv, n, page, lengths, 1), range(n), lengths, 2)
     q, out, before = _decode(c, list(range(n)), lengths, 3, IN[kv], True)
