@@ -167,11 +167,12 @@ __device__ __forceinline__ int64_t paged_row(const PagedArgs& a, int slot, int g
 // HBM bound: 8 sequences of 19k to 128k rows x 8 KV heads, 128-wide bf16 (2.52 GB) 397
 // us, 6.3 TB/s with the join; fp8 209 us, 6.0 TB/s.  Values prefetched a block ahead
 // like the keys change nothing, there or for short sequences.
-// 16-bit and fp8 rows: probabilities enter the products as two bf16 terms of 8
-// bits each, truncated: off by under 2^-16 relative.  One term would be off by up
-// to 2^-8, which the heaviest rows of a head show in the output; the second costs
-// D / 16 matrix instructions a block, which the loads hide.  fp32 rows: fp32
-// matrix instructions throughout.
+// 16-bit and fp8 rows: probabilities enter the products whole, as three bf16 terms
+// of 8 bits.  Two terms, cut off, are off by up to 2^-15 and always to the same side,
+// which fp32 outputs show and bf16 ones as roundings to the other neighbour; the third
+// costs D / 16 matrix instructions a block, mostly hidden by the loads (128-wide fp8,
+// 32 x 8 heads of up to 16384 rows with weights, 123 -> 126 us; bf16 none).  fp32 rows:
+// fp32 matrix instructions throughout.
 constexpr float kStaleMax = 8.f;
 enum { kKvBf16 = 0, kKvFp8 = 1, kKvF32 = 2 };
 
@@ -211,12 +212,12 @@ __device__ __forceinline__ f32x4 logits4(const float* x, float xs, float xlo) {
   return f32x4{fmaf(x[0], xs, x[0] * xlo), fmaf(x[1], xs, x[1] * xlo), fmaf(x[2], xs, x[2] * xlo), fmaf(x[3], xs, x[3] * xlo)};
 }
 
-// Eight probabilities as two bf16 terms (pe is used up).  The second is kept off
-// zero (2^-126), so that an infinite value times it stays infinite, as with the
-// whole probability.
-__device__ __forceinline__ void two_terms(float (&pe)[8], bf16x8 (&p)[2]) {
+// Eight probabilities as three bf16 terms, whose sum they are (pe is used up).  The
+// second and third are kept off zero (2^-126), so that an infinite value times them
+// stays infinite, as with the whole probability.
+__device__ __forceinline__ void three_terms(float (&pe)[8], bf16x8 (&p)[3]) {
 #pragma unroll
-  for (int part = 0; part < 2; ++part) {
+  for (int part = 0; part < 3; ++part) {
     u32x4 pw;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -228,6 +229,21 @@ __device__ __forceinline__ void two_terms(float (&pe)[8], bf16x8 (&p)[2]) {
     }
     p[part] = __builtin_bit_cast(bf16x8, pw);
   }
+}
+
+// The same as two terms, each rounded to nearest: off by at most 2^-18 relative (half a
+// step of half a step), to either side.
+__device__ __forceinline__ void two_terms(float (&pe)[8], bf16x8 (&p)[2]) {
+  u32x4 first, second;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    first[i] = pack_bf16x2(pe[2 * i], pe[2 * i + 1]);
+    pe[2 * i] -= __uint_as_float(first[i] << 16);
+    pe[2 * i + 1] -= __uint_as_float(first[i] & 0xffff0000u);
+    second[i] = pack_bf16x2(pe[2 * i], pe[2 * i + 1]);
+  }
+  p[0] = __builtin_bit_cast(bf16x8, first);
+  p[1] = __builtin_bit_cast(bf16x8, second);
 }
 
 // A loaded value is waited for here.  Before a loop, and behind a branch in one:
@@ -561,8 +577,8 @@ __global__ __launch_bounds__(64 * WAVES) void paged_gqa(PagedArgs a) {
         for (int c = 0; c < NF; ++c)
           acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[i][c]), pe[i], acc[c], 0, 0, 0);
     } else {
-      bf16x8 p[2];
-      two_terms(pe, p);
+      bf16x8 p[3];
+      three_terms(pe, p);
       uint32_t vw[8][VE / 2];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -583,8 +599,9 @@ __global__ __launch_bounds__(64 * WAVES) void paged_gqa(PagedArgs a) {
         u32x4 av;
 #pragma unroll
         for (int i = 0; i < 4; ++i) av[i] = __builtin_amdgcn_perm(vw[2 * i + 1][c >> 1], vw[2 * i][c >> 1], sel);
-        acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, av), p[1], acc[c], 0, 0, 0);
-        acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, av), p[0], acc[c], 0, 0, 0);
+#pragma unroll
+        for (int part = 2; part >= 0; --part)
+          acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, av), p[part], acc[c], 0, 0, 0);
       }
     }
 #pragma unroll
@@ -700,6 +717,11 @@ __global__ __launch_bounds__(64 * WAVES) void paged_gqa(PagedArgs a) {
 // Rows past the sequence and in pages that are not there are loaded from a row of
 // zeros: their probabilities are zero, and zero times whatever else might stand
 // there need not be.
+// Probabilities enter the value product as two bf16 terms rounded to nearest (2^-18):
+// with one wave a SIMD nothing hides a third term's 16 matrix instructions a block (bf16
+// 102.6 -> 107, fp8 72 -> 79 us in the cases below); against the same attention in fp32
+// the bf16 outputs of the bf16 case are 9e-5 off with two terms, 7e-5 with three (mostly
+// roundings to the other neighbour), 2e-4 with two that are cut off.
 // HBM bound in bf16: 16 sequences of 32k rows (604 MB) 100 us, 6.0 TB/s; blocks of 32
 // rows in four stages, the dims of a product split over the waves, take as long.  fp8
 // (302 MB, 16 heads) 70 us: the conversions, and a block's two barriers with two
@@ -888,8 +910,9 @@ __global__ __launch_bounds__(256, FP8 ? 2 : 1) void paged_latent(PagedArgs a) {
         u32x4 av;
 #pragma unroll
         for (int k = 0; k < 4; ++k) av[k] = __builtin_amdgcn_perm(v[2 * k + 1][c >> 1], v[2 * k][c >> 1], sel);
-        acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, av), p[1], acc[c], 0, 0, 0);
-        acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, av), p[0], acc[c], 0, 0, 0);
+#pragma unroll
+        for (int part = 1; part >= 0; --part)
+          acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, av), p[part], acc[c], 0, 0, 0);
       }
     }
     lds_barrier();  // every wave is done with this stage and these products
