@@ -58,9 +58,10 @@ __device__ __forceinline__ constexpr int part_bins(int part) { return part == 0 
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-// A unit's rows and counters.
+// A unit's rows and counters: R rows that the call looks at, `left` the slot's counter
+// after it (a counter below zero stays; rows past max_rows count).
 struct EvictUnit {
-  int unit, slot, g, R, late;
+  int unit, slot, g, R, left, late;
 };
 __device__ __forceinline__ bool evict_unit(const EvictArgs& a, int unit, EvictUnit& u) {
   const int b = unit / a.Hkv;
@@ -68,8 +69,9 @@ __device__ __forceinline__ bool evict_unit(const EvictArgs& a, int unit, EvictUn
   u.g = unit % a.Hkv;
   u.slot = a.slot_ids[b];
   if (u.slot < 0 || u.slot >= a.n_slots) return false;
-  const int R = a.rows[u.slot];
-  u.R = R < 0 ? 0 : (R > a.max_rows ? a.max_rows : R);
+  const int held = a.rows[u.slot];
+  u.R = held < 0 ? 0 : (held > a.max_rows ? a.max_rows : held);
+  u.left = held < a.budget ? held : a.budget;
   u.late = a.pos[u.slot] - a.recent;
   return true;
 }
@@ -188,11 +190,11 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick(EvictArgs a) {
     return;
   }
   const int R = u.R;
-  if (u.g == 0 && t == 0) a.rows_out[u.slot] = R < B ? R : B;
+  if (u.g == 0 && t == 0) a.rows_out[u.slot] = u.left;
   int32_t* kept = a.kept_out ? a.kept_out + (int64_t)u.unit * B : nullptr;
   if (R <= B) {
     if (kept)
-      for (int r = t; r < B; r += kPickThreads) kept[r] = r < R ? r : -1;
+      for (int r = t; r < B; r += kPickThreads) kept[r] = r < u.left ? r : -1;
     if (t == 0) a.count[u.unit] = 0;
     return;
   }
@@ -328,11 +330,11 @@ __global__ __launch_bounds__(kPickThreads) void evict_split_keys(EvictArgs a, Sp
     if (t == 0 && split == 0) a.count[bid_y()] = 0;
     return;
   }
-  if (u.g == 0 && t == 0 && split == 0) a.rows_out[u.slot] = u.R < B ? u.R : B;
+  if (u.g == 0 && t == 0 && split == 0) a.rows_out[u.slot] = u.left;
   if (u.R <= B) {
     if (a.kept_out)
       for (int r = split * kPickThreads + t; r < B; r += p.splits * kPickThreads)
-        a.kept_out[(int64_t)u.unit * B + r] = r < u.R ? r : -1;
+        a.kept_out[(int64_t)u.unit * B + r] = r < u.left ? r : -1;
     if (t == 0 && split == 0) a.count[u.unit] = 0;
     return;
   }
