@@ -457,12 +457,14 @@ size_t snap_paged_evict_workspace(const snap_params* p, int32_t n, int32_t max_r
  * up to B rows in all (equal weights: the lower row; NaN and negative weights
  * count as 0).  Kept rows below B stay where they are; the j-th kept row from B
  * on moves to the j-th row below B that was not kept, with its token and weight.
- * Rows from B on are left as they were.
+ * Rows from B on are left as they were.  A row in a page that is not there is not
+ * kept, and none moves into it: where m rows below B are such, B - m are kept.
  *   rows_out [n_slots] int32: min(rows, B) of the call's slots, so that one below
  *            0 stays so (the same from every layer; rows itself is left, so that
  *            every layer sees it),
  *   kept_out optional [n][n_kv_heads][B] int32: the row whose contents are now
- *            in each row, -1 past the rows held (NULL to skip),
+ *            in each row, -1 past the rows held and where the page is not there
+ *            (NULL to skip),
  *   max_rows (host, at most max_pages * page_size): rows past it are not looked
  *            at: those from B on are not kept, those below B stay where they are,
  *   workspace >= snap_paged_evict_workspace(p, n, max_rows) bytes, 256-byte

@@ -35,21 +35,22 @@ __device__ __forceinline__ int64_t evict_row(const EvictArgs& a, int slot, int g
   return (((int64_t)page * a.Hkv + g) << a.page_shift) + (r & ((1 << a.page_shift) - 1));
 }
 
-// A row's rank among those that are not protected: its weight's bits (weights
-// are not negative, so their bits are in their order; NaN and negative: 0).
-__device__ __forceinline__ uint32_t weight_key(uint32_t bits) { return bits > 0x7f800000u ? 0u : bits; }
+// A row's rank among those that are not protected: one more than its weight's bits
+// (weights are not negative, so their bits are in their order; NaN and negative: 0).
+__device__ __forceinline__ uint32_t weight_key(uint32_t bits) { return bits > 0x7f800000u ? 1u : bits + 1u; }
 
 // ---------------------------------------------------------------- selection
 // A row that is to be kept whatever its weight: above every weight's bits.
 constexpr uint32_t kProtected = 0xffffffffu;
-// Past the rows held, in the stored keys: like kProtected it shares no weight's
-// leading bits.
-constexpr uint32_t kAbsent = 0xfffffffeu;
+// A row past those looked at or in a page that is not there: below every weight's, so
+// that it is never counted to nor kept.  Where such a row lies below the budget there is
+// one place less to keep rows in, and nothing moves into it.
+constexpr uint32_t kAbsent = 0;
 constexpr int kPickThreads = 1024;
 constexpr int kPickWaves = kPickThreads / 64;
 constexpr int kTileRows = 4 * kPickThreads;  // four neighbouring rows (of one page) a thread
 constexpr int kPickRows = 2 * kTileRows;     // rows that one workgroup selects among
-// The weights' 31 bits in three parts, the leading ones (exponent and three bits
+// The keys' 31 bits (but for kProtected) in three parts, the leading ones (exponent and three bits
 // more) first.
 constexpr int kParts = 3;
 constexpr int kBins = 2048;
@@ -76,7 +77,12 @@ __device__ __forceinline__ bool evict_unit(const EvictArgs& a, int unit, EvictUn
   return true;
 }
 
-// The keys of this thread's four rows of N tiles from row r0 on (rows past R: 0).
+// What kept_out says of row r of a unit that is left as it is.
+__device__ __forceinline__ int kept_in_place(const EvictArgs& a, const EvictUnit& u, int r) {
+  return r < u.left && r < a.max_pages << a.page_shift && evict_row(a, u.slot, u.g, r) >= 0 ? r : -1;
+}
+
+// The keys of this thread's four rows of N tiles from row r0 on.
 // No load stands behind a branch: rows that are not there are read at row 0 of page
 // 0, so that every page id, and then every row, is in flight at once.
 template <int N>
@@ -101,7 +107,7 @@ __device__ __forceinline__ void load_keys(const EvictArgs& a, const EvictUnit& u
   for (int j = 0; j < N; ++j)
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      key[j][e] = page[j] < 0 || r0 + j * kTileRows + 4 * tid() + e >= u.R ? 0
+      key[j][e] = page[j] < 0 || r0 + j * kTileRows + 4 * tid() + e >= u.R ? kAbsent
                   : tok[j][e] < a.sink || tok[j][e] >= u.late             ? kProtected
                                                                           : weight_key(w[j][e]);
 }
@@ -181,7 +187,7 @@ template <int TILES>
 __global__ __launch_bounds__(kPickThreads) void evict_pick(EvictArgs a) {
   __shared__ int hist[kBins];
   __shared__ uint32_t cnt[TILES * kPickWaves];
-  __shared__ int red[kPickWaves], out[2];
+  __shared__ int red[2 * kPickWaves], out[2];
   __shared__ uint32_t total;
   const int t = tid(), lane = t & 63, w = t >> 6, B = a.budget;
   EvictUnit u;
@@ -194,25 +200,27 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick(EvictArgs a) {
   int32_t* kept = a.kept_out ? a.kept_out + (int64_t)u.unit * B : nullptr;
   if (R <= B) {
     if (kept)
-      for (int r = t; r < B; r += kPickThreads) kept[r] = r < u.left ? r : -1;
+      for (int r = t; r < B; r += kPickThreads) kept[r] = kept_in_place(a, u, r);
     if (t == 0) a.count[u.unit] = 0;
     return;
   }
   uint32_t key[TILES][4];
   load_keys<TILES>(a, u, 0, key);
-  int prots[1] = {0};
+  int sums[2] = {0, 0};  // protected rows, places below B
 #pragma unroll
   for (int j = 0; j < TILES; ++j)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) prots[0] += key[j][e] == kProtected;
-  block_sums(prots, red);
-  const int prot = prots[0];
+    for (int e = 0; e < 4; ++e) {
+      sums[0] += key[j][e] == kProtected;
+      sums[1] += key[j][e] != kAbsent && j * kTileRows + 4 * t + e < B;
+    }
+  block_sums(sums, red);
   // kept: above T, and of those equal to T the first rem by row
   uint32_t T = kProtected;
-  int rem = B;
-  if (prot < B) {
+  int rem = sums[1];
+  if (sums[0] < rem) {
     T = 0;
-    rem = B - prot;
+    rem -= sums[0];
 #pragma unroll
     for (int part = 0; part < kParts; ++part) {
       const int sh = part_shift(part), bins = part_bins(part);
@@ -224,7 +232,7 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick(EvictArgs a) {
         for (int e = 0; e < 4; ++e) {
           const uint32_t k = key[j][e];
           const bool same = part == 0 || (k >> part_shift(part ? part - 1 : 0)) == (T >> part_shift(part ? part - 1 : 0));
-          if (k != kProtected && same && j * kTileRows + 4 * t + e < R) atomicAdd(&hist[(k >> sh) & (bins - 1)], 1);
+          if (k != kProtected && k != kAbsent && same) atomicAdd(&hist[(k >> sh) & (bins - 1)], 1);
         }
       __syncthreads();
       find_bin(hist, bins, rem, red, out);
@@ -240,7 +248,7 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick(EvictArgs a) {
     int c = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      c += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[j][e] == T && j * kTileRows + 4 * t + e < R));
+      c += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[j][e] == T));
     if (lane == 0) cnt[j * kPickWaves + w] = c;
   }
   scan128(cnt, TILES * kPickWaves, &total);
@@ -250,11 +258,11 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick(EvictArgs a) {
     int before = cnt[j * kPickWaves + w];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      before += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[j][e] == T && j * kTileRows + 4 * t + e < R) & below);
+      before += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[j][e] == T) & below);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const bool live = j * kTileRows + 4 * t + e < R, eq = live && key[j][e] == T;
-      if ((live && key[j][e] > T) || (eq && before < rem)) keep |= 1u << (4 * j + e);
+      const bool eq = key[j][e] == T;
+      if (key[j][e] > T || (eq && before < rem)) keep |= 1u << (4 * j + e);
       before += eq;
     }
   }
@@ -267,7 +275,7 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick(EvictArgs a) {
     for (int e = 0; e < 4; ++e) {
       const int r = j * kTileRows + 4 * t + e;
       const bool k = (keep >> (4 * j + e)) & 1;
-      c += __builtin_popcountll(__builtin_amdgcn_ballot_w64(r < B && !k));
+      c += __builtin_popcountll(__builtin_amdgcn_ballot_w64(r < B && !k && key[j][e] != kAbsent));
       c += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(r >= B && k)) << 16;
     }
     if (lane == 0) cnt[j * kPickWaves + w] = c;
@@ -282,7 +290,7 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick(EvictArgs a) {
     for (int e = 0; e < 4; ++e) {
       const int r = j * kTileRows + 4 * t + e;
       const bool k = (keep >> (4 * j + e)) & 1;
-      before += __builtin_popcountll(__builtin_amdgcn_ballot_w64(r < B && !k) & below);
+      before += __builtin_popcountll(__builtin_amdgcn_ballot_w64(r < B && !k && key[j][e] != kAbsent) & below);
       before += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(r >= B && k) & below) << 16;
     }
 #pragma unroll
@@ -290,7 +298,9 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick(EvictArgs a) {
       const int r = j * kTileRows + 4 * t + e;
       const bool k = (keep >> (4 * j + e)) & 1;
       const int hole = before & 0xffff, from = before >> 16;
-      if (r < B && !k) {
+      if (r < B && key[j][e] == kAbsent) {
+        if (kept) kept[r] = -1;
+      } else if (r < B && !k) {
         if (debug_check(hole < a.max_moves, kDbgPagedMove)) dst[hole] = r;
         before += 1;
       } else if (r >= B && k) {
@@ -316,14 +326,14 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick(EvictArgs a) {
 struct SplitArgs {
   uint32_t* keys;  // [units][row_pad]
   int* hist;       // [units][splits][kBins]
-  int* prot;       // [units][splits] protected rows
+  int2* sums;      // [units][splits] protected rows, rows below the budget that are not there
   int64_t row_pad;
   int splits, split_rows;
 };
 
 __global__ __launch_bounds__(kPickThreads) void evict_split_keys(EvictArgs a, SplitArgs p) {
   __shared__ int hist[kBins];
-  __shared__ int red[kPickWaves];
+  __shared__ int red[2 * kPickWaves];
   const int t = tid(), split = bid_x(), B = a.budget;
   EvictUnit u;
   if (!evict_unit(a, bid_y(), u)) {
@@ -334,7 +344,7 @@ __global__ __launch_bounds__(kPickThreads) void evict_split_keys(EvictArgs a, Sp
   if (u.R <= B) {
     if (a.kept_out)
       for (int r = split * kPickThreads + t; r < B; r += p.splits * kPickThreads)
-        a.kept_out[(int64_t)u.unit * B + r] = r < u.left ? r : -1;
+        a.kept_out[(int64_t)u.unit * B + r] = kept_in_place(a, u, r);
     if (t == 0 && split == 0) a.count[u.unit] = 0;
     return;
   }
@@ -342,28 +352,27 @@ __global__ __launch_bounds__(kPickThreads) void evict_split_keys(EvictArgs a, Sp
   const int r0 = min((int64_t)split * p.split_rows, (int64_t)u.R), r1 = min((int64_t)r0 + p.split_rows, (int64_t)u.R);
   for (int i = t; i < kBins; i += kPickThreads) hist[i] = 0;
   __syncthreads();
-  int prot[1] = {0};
+  int sums[2] = {0, 0};
   for (int r = r0; r < r1; r += kTileRows) {
     uint32_t key[1][4];
     load_keys<1>(a, u, r, key);
     const int mine = r + 4 * t;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (mine + e >= u.R) key[0][e] = kAbsent;
     if (mine < r1)
       *(u32x4*)(p.keys + (int64_t)u.unit * p.row_pad + mine) = u32x4{key[0][0], key[0][1], key[0][2], key[0][3]};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if (mine + e >= r1) break;
       if (key[0][e] == kProtected)
-        ++prot[0];
+        ++sums[0];
+      else if (key[0][e] == kAbsent)
+        sums[1] += mine + e < B;
       else
         atomicAdd(&hist[key[0][e] >> part_shift(0)], 1);
     }
   }
-  block_sums(prot, red);  // and the histogram is complete
+  block_sums(sums, red);  // and the histogram is complete
   for (int i = t; i < kBins; i += kPickThreads) p.hist[at * kBins + i] = hist[i];
-  if (t == 0) p.prot[at] = prot[0];
+  if (t == 0) p.sums[at] = make_int2(sums[0], sums[1]);
 }
 
 // f(r, keys of rows r .. r + 3) for a unit's stored keys of the rows before `to`,
@@ -384,8 +393,9 @@ __global__ __launch_bounds__(kPickThreads) void evict_split_lists(EvictArgs a, S
   const uint32_t* keys = p.keys + (int64_t)u.unit * p.row_pad;
   // the splits' histograms of the leading bits, two bins a thread from the top
   const int* first = p.hist + (int64_t)u.unit * p.splits * kBins + kBins - 2 - 2 * t;
-  int prot[1] = {0}, c0 = 0, c1 = 0;
-  if (t < p.splits) prot[0] = p.prot[(int64_t)u.unit * p.splits + t];
+  int2 sums = {0, 0};  // of split `lane` (there are at most 32)
+  if (lane < p.splits) sums = p.sums[(int64_t)u.unit * p.splits + lane];
+  int c0 = 0, c1 = 0;
 #pragma unroll 8
   for (int s = 0; s < p.splits; ++s) {
     const int2 v = *(const int2*)(first + (int64_t)s * kBins);
@@ -393,12 +403,12 @@ __global__ __launch_bounds__(kPickThreads) void evict_split_lists(EvictArgs a, S
     c1 += v.x;
   }
   hist[0][t] = hist[1][t] = 0;
-  block_sums(prot, red);
+  const int prot = wave_total(sums.x), gone = wave_total(sums.y), gone_before = wave_total(lane < split ? sums.y : 0);
   // kept: above T, and of those equal to T the first rem by row
   uint32_t T = kProtected;
-  int rem = B;
-  if (prot[0] < B) {
-    rem = B - prot[0];
+  int rem = B - gone;
+  if (prot < rem) {
+    rem -= prot;
     find_bin(kBins - 1 - 2 * t, c0, c1, rem, red, out);
     T = (uint32_t)out[0] << part_shift(0);
     rem -= out[1];
@@ -419,7 +429,8 @@ __global__ __launch_bounds__(kPickThreads) void evict_split_lists(EvictArgs a, S
   }
   const int r0 = min((int64_t)split * p.split_rows, (int64_t)u.R), r1 = min((int64_t)r0 + p.split_rows, (int64_t)u.R);
   // rows above T and equal to it before this split, and below B (for the number of
-  // moves, and where rows from B on go)
+  // moves, and where rows from B on go); rows below B that are not there count as kept
+  // where they are
   int c[4] = {0, 0, 0, 0};
   const bool low = split == 0 || r1 > B;
   scan_keys(keys, low ? max(r0, B) : r0, [&](int r, u32x4 k) {
@@ -432,8 +443,8 @@ __global__ __launch_bounds__(kPickThreads) void evict_split_lists(EvictArgs a, S
     }
   });
   block_sums(c, red);
-  int eq = c[1], kept_before = c[0] + min(rem, c[1]);
-  const int kept_low = c[2] + min(rem, c[3]);  // low only
+  int eq = c[1], kept_before = c[0] + min(rem, c[1]) + gone_before;
+  const int kept_low = c[2] + min(rem, c[3]) + gone;  // low only
   if (t == 0 && split == 0) a.count[u.unit] = B - kept_low;
   int32_t* kept = a.kept_out ? a.kept_out + (int64_t)u.unit * B : nullptr;
   int32_t* src = a.src + (int64_t)u.unit * a.max_moves;
@@ -463,7 +474,7 @@ __global__ __launch_bounds__(kPickThreads) void evict_split_lists(EvictArgs a, S
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const bool live = r + e < r1, same = live && k[e] == T;
-      keep[e] = live && (k[e] > T || (same && before < rem));
+      keep[e] = live && (k[e] > T || (same && before < rem) || (k[e] == kAbsent && r + e < B));
       before += same;
       const uint64_t m = __builtin_amdgcn_ballot_w64(keep[e]);
       n += __builtin_popcountll(m);
@@ -484,7 +495,7 @@ __global__ __launch_bounds__(kPickThreads) void evict_split_lists(EvictArgs a, S
         if (!keep[e]) {
           if (debug_check(r + e - rank < a.max_moves, kDbgPagedMove)) dst[r + e - rank] = r + e;
         } else if (kept) {
-          kept[r + e] = r + e;
+          kept[r + e] = k[e] == kAbsent ? -1 : r + e;
         }
       } else if (keep[e] && debug_check(rank - kept_low < a.max_moves, kDbgPagedMove)) {
         src[rank - kept_low] = r + e;
@@ -510,7 +521,7 @@ __global__ __launch_bounds__(256) void evict_move(EvictArgs a, int shares) {
     const int rs = src[j], rd = dst[j];
     if (c == 0 && a.kept_out) a.kept_out[(int64_t)unit * a.budget + rd] = rs;
     const int64_t from = evict_row(a, slot, g, rs), to = evict_row(a, slot, g, rd);
-    if (from < 0 || to < 0) continue;
+    if (from < 0 || to < 0) continue;  // (the selection names no such row)
     if (c < kp)
       *(u32x4*)(a.ck + to * a.kbytes + 16 * c) = *(const u32x4*)(a.ck + from * a.kbytes + 16 * c);
     else
@@ -546,8 +557,8 @@ EvictGeometry evict_geometry(const snap_params& p, int n, int max_rows) {
     off = align256(off + (size_t)units * g.row_pad * sizeof(uint32_t));
     g.off_hist = off;
     off = align256(off + (size_t)units * g.splits * kBins * sizeof(int));
-    g.off_prot = off;
-    off = align256(off + (size_t)units * g.splits * sizeof(int));
+    g.off_sums = off;
+    off = align256(off + (size_t)units * g.splits * sizeof(int2));
   }
   g.off_count = off;
   off = align256(off + (size_t)units * sizeof(int32_t));
@@ -598,7 +609,7 @@ snap_status launch_paged_evict(const snap_params& p, const snap_paged_cache& c, 
     SplitArgs sp;
     sp.keys = (uint32_t*)(base + geo.off_keys);
     sp.hist = (int*)(base + geo.off_hist);
-    sp.prot = (int*)(base + geo.off_prot);
+    sp.sums = (int2*)(base + geo.off_sums);
     sp.row_pad = (int64_t)geo.row_pad;
     sp.splits = geo.splits;
     sp.split_rows = geo.split_rows;

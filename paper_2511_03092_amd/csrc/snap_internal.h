@@ -293,7 +293,7 @@ struct EvictGeometry {
   int max_moves;  // moves of a (sequence, KV head) at most
   // more rows than one workgroup selects among: splits of a unit (0: none)
   int splits, split_rows;
-  size_t row_pad, off_keys, off_hist, off_prot;
+  size_t row_pad, off_keys, off_hist, off_sums;
   size_t off_count, off_src, off_dst, bytes;
 };
 EvictGeometry evict_geometry(const snap_params& p, int n, int max_rows);

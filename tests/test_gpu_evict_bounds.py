@@ -65,3 +65,60 @@ def test_max_rows_below_the_budget_drops_no_row(topk, max_rows, rows):
     for b, r in enumerate(rows):
         assert (kept[b] == np.where(np.arange(B) < min(r, B), np.arange(B), -1)).all(), b
     _same(state, c.state())
+
+
+def _expected(token, weight, there, rows, pos, p):
+    """kept_out of one (slot, head): rows in pages that are not there are neither kept nor filled."""
+    B = p.budget
+    if rows <= B:
+        return np.array([r if r < rows and there[r] else -1 for r in range(B)])
+    r = np.arange(rows)
+    safe = there & ((token < p.sink) | (token >= pos - p.recent))
+    places = int(there[:B].sum())
+    kept = r[safe][:places].tolist()
+    others = sorted(r[there & ~safe].tolist(), key=lambda i: (-weight[i], i))
+    kept = sorted(kept + others[:max(0, places - int(safe.sum()))])
+    out = np.full(B, -1)
+    here = [i for i in kept if i < B]
+    out[here] = here
+    out[np.flatnonzero((out < 0) & there[:B])] = [i for i in kept if i >= B]
+    return out
+
+
+@pytest.mark.parametrize("max_rows", [640, 16384])
+@pytest.mark.parametrize("what", ["below", "behind", "protected", "both", "all-below", "all-behind", "all", "ties",
+                                  "protected-over-places"])
+def test_pages_that_are_not_there(what, max_rows):
+    """Pages of 32 rows missing below the budget of 100, behind it, or with the first and latest tokens: no kept row goes
+    there, and none comes from there."""
+    over = dict(recent=90, topk=7) if what == "protected-over-places" else dict(recent=9, topk=88)
+    p = params(4, 2, 64, "bf16", sink=3, **over)
+    assert p.budget == 100
+    page, rows = 32, [600, 101, 333, 90]
+    gone = {"below": [1], "behind": [4, 9], "protected": [0, 18, 10], "both": [2, 3, 5], "all-below": [0, 1, 2, 3],
+            "all-behind": list(range(4, 19)), "all": list(range(19)), "ties": [1, 3, 4], "protected-over-places": [0, 2]}[what]
+    print(f"\n[case] evict, pages {gone} not there, rows {rows}, at most {max_rows}", flush=True)
+
+    def before(c):
+        g = torch.Generator().manual_seed(9)
+        w = torch.rand(c.weight.shape, generator=g)
+        if what == "ties":
+            w = torch.round(w * 2) / 2  # many zeros among them
+        c.weight.copy_(w)
+        for i, j in enumerate(gone):
+            c.table[:, j] = [-1, c.n_pages, -(1 << 31), (1 << 31) - 1][i % 4]
+
+    c, state, out, kept = _run(p, "bf16", page, [max_rows if b == 0 else x for b, x in enumerate(rows)], rows, max_rows,
+                               before=before)
+    assert out == [min(r, 100) for r in rows]
+    want = {x: state[x].clone() for x in ("k", "v", "token", "weight", "rows", "pos")}
+    for b, R in enumerate(rows):
+        pl = c.places(b, R)
+        for h in range(p.n_kv_heads):
+            (token, there), weight = c.gather("token", b, h, R, state), c.gather("weight", b, h, R, state)[0]
+            exp = _expected(token.numpy(), weight.numpy(), there, R, R + 30, p)
+            assert (kept[b, h] == exp).all(), (b, h, np.flatnonzero(kept[b, h] != exp)[:5])
+            for to in np.flatnonzero((exp >= 0) & (exp != np.arange(100))):
+                for x in ("k", "v", "token", "weight"):
+                    want[x][pl[to][0], h, pl[to][1]] = state[x][pl[exp[to]][0], h, pl[exp[to]][1]]
+    _same(want, c.state())
