@@ -447,7 +447,8 @@ snap_status snap_paged_decode_step(const snap_params* p, const snap_paged_cache*
                                    const void* q, const void* k_new, const void* v_new, void* out, int32_t out_dtype,
                                    int32_t weigh, void* workspace, size_t ws_bytes, void* stream);
 
-/* Bytes of workspace snap_paged_evict needs.  0 on invalid parameters. */
+/* Bytes of workspace snap_paged_evict needs; no fewer than for fewer sequences or
+ * rows.  0 on invalid parameters. */
 size_t snap_paged_evict_workspace(const snap_params* p, int32_t n, int32_t max_rows);
 
 /* Cuts slots back to the budget B = sink + recent + topk, between two steps

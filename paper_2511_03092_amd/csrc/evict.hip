@@ -553,12 +553,17 @@ EvictGeometry evict_geometry(const snap_params& p, int n, int max_rows) {
     g.split_rows = (int)((max_rows + (int64_t)most * kTileRows - 1) / ((int64_t)most * kTileRows)) * kTileRows;
     g.splits = (max_rows + g.split_rows - 1) / g.split_rows;
     g.row_pad = ((size_t)max_rows + 3) & ~(size_t)3;
+    // Room for units * splits histograms, or for more: no call with fewer units or rows
+    // has more splits than `room`, so that a workspace of the largest call serves it.
+    const int tiles = (int)(((int64_t)max_rows + kTileRows - 1) / kTileRows);
+    const size_t each = (size_t)units * (tiles < 32 ? tiles : 32), all = units > 256 ? units : 256;
+    const size_t room = each < all ? each : all;
     g.off_keys = off;
     off = align256(off + (size_t)units * g.row_pad * sizeof(uint32_t));
     g.off_hist = off;
-    off = align256(off + (size_t)units * g.splits * kBins * sizeof(int));
+    off = align256(off + room * kBins * sizeof(int));
     g.off_sums = off;
-    off = align256(off + (size_t)units * g.splits * sizeof(int2));
+    off = align256(off + room * sizeof(int2));
   }
   g.off_count = off;
   off = align256(off + (size_t)units * sizeof(int32_t));
