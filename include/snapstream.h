@@ -421,7 +421,9 @@ snap_status snap_paged_append(const snap_params* p, const snap_paged_cache* cach
                               const int64_t* v_stride, const float* weight_new, void* stream);
 
 /* Bytes of workspace snap_paged_decode_attn / _step need for n sequences of at
- * most max_rows rows (the new one included).  0 on invalid parameters. */
+ * most max_rows rows (the new one included); no fewer than for fewer sequences
+ * or rows, nor with weigh than without.  With weigh it holds the logits: n x
+ * n_q_heads x max_rows x 4 bytes.  0 on invalid parameters. */
 size_t snap_paged_decode_workspace(const snap_params* p, int32_t n, int32_t max_rows, int32_t weigh);
 
 /* Attention of one new token per sequence (already stored) over rows

@@ -1196,7 +1196,12 @@ PagedGeometry paged_geometry(const snap_params& p, int n, int max_rows, bool wei
   g.off_ml = off;
   off = align256(off + (size_t)g.max_items * G * sizeof(float2));
   g.off_z = off;
-  if (weigh) off = align256(off + (size_t)blocks * kBlockRows * G * sizeof(float));
+  if (weigh) {
+    off = align256(off + (size_t)blocks * kBlockRows * G * sizeof(float));
+    // (fewer items may be resident than without weights: room for those calls too)
+    const size_t plain = paged_geometry(p, n, max_rows, false).bytes;
+    if (off < plain) off = plain;
+  }
   g.bytes = off;
   return g;
 }

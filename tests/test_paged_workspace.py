@@ -27,3 +27,19 @@ def _monotone(query):
 def test_eviction_needs_no_more_for_fewer_sequences_or_rows(heads, topk):
     p = params(*heads, topk=topk)
     _monotone(lambda n, r: snap.snap_paged_evict_workspace(p, n, r))
+
+
+@pytest.mark.parametrize("heads", HEADS)
+@pytest.mark.parametrize("weigh", [False, True])
+def test_attention_needs_no_more_for_fewer_sequences_or_rows(heads, weigh):
+    p = params(*heads)
+    _monotone(lambda n, r: snap.snap_paged_decode_workspace(p, n, r, weigh))
+
+
+@pytest.mark.parametrize("heads", HEADS)
+def test_attention_needs_no_more_without_weights(heads):
+    p = params(*heads)
+    for n in COUNTS:
+        for r in ROWS:
+            a, b = (snap.snap_paged_decode_workspace(p, n, r, w) for w in (False, True))
+            assert a <= b, (n, r, a, b)
