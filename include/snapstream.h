@@ -355,7 +355,8 @@ typedef struct {
 } snap_rope_heads;
 
 /* Rotates the heads of q and (unless NULL) of k, both of width d and type
- * dtype (SNAP_F32 or SNAP_BF16), in one launch.  Token t < lengths[b] (max_len
+ * dtype (SNAP_F32 or SNAP_BF16), in one launch (two where one of them is in
+ * place, the other not, and dims are left unrotated).  Token t < lengths[b] (max_len
  * when lengths is NULL; lengths are clamped to [0, max_len]) of sequence b is
  * at position pos[slot_ids[b]] + t, or at t when pos is NULL (slot_ids and
  * n_slots are then not read); tokens past it are neither read nor written, nor
