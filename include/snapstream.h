@@ -344,8 +344,10 @@ typedef struct {
  * elements) of the first three; the d dims of a head are contiguous.  y may be
  * x with the same strides (in place: only the rotated dims are touched);
  * otherwise the memory x spans and the memory y spans must be disjoint.
- * A stride of y is not 0 where its size is more than 1.  What is written for one
- * operand must not be read or written for the other. */
+ * Along sizes of more than 1, from the smallest on, each stride of y reaches past
+ * all that the smaller ones span (so that no outputs share elements: any slice,
+ * permutation or reversal of a tensor).  What is written for one operand must not
+ * be read or written for the other. */
 typedef struct {
   const void* x;
   void* y;

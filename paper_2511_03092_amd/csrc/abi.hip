@@ -7,6 +7,7 @@
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
+#include <stdlib.h>
 
 #include "prefill_order.h"
 #include "snap_internal.h"
@@ -112,7 +113,6 @@ static snap_status check_rope_heads(const snap_rope_heads* h, const char* name, 
   // 2^40 elements reaches nothing that exists
   __int128 lo[2] = {0, 0}, hi[2] = {d, d};
   for (int i = 0; i < 3; ++i) {
-    if (size[i] > 1 && h->y_stride[i] == 0) return fail(SNAP_ERR_INVALID_ARG, "%s: a stride of y is 0", name);
     const int64_t st[2] = {h->x_stride[i], h->y_stride[i]};
     for (int o = 0; o < 2; ++o) {
       if (size[i] > 1 && (st[o] > ((int64_t)1 << 40) || st[o] < -((int64_t)1 << 40)))
@@ -120,6 +120,18 @@ static snap_status check_rope_heads(const snap_rope_heads* h, const char* name, 
       const __int128 reach = size[i] > 1 ? (__int128)(size[i] - 1) * st[o] : 0;
       (reach < 0 ? lo[o] : hi[o]) += reach;
     }
+  }
+  // outputs apart: from the smallest stride of y on, each reaches past all that the
+  // smaller ones span (any slice, permutation or reversal of a tensor is laid out so)
+  __int128 span = d;
+  for (unsigned left = (size[0] > 1) | (size[1] > 1) << 1 | (size[2] > 1) << 2; left;) {
+    int at = -1;
+    for (int i = 0; i < 3; ++i)
+      if (left >> i & 1 && (at < 0 || llabs(h->y_stride[i]) < llabs(h->y_stride[at]))) at = i;
+    left &= ~(1u << at);
+    if (llabs(h->y_stride[at]) < span)
+      return fail(SNAP_ERR_INVALID_ARG, "%s: by the strides of y, outputs share elements", name);
+    span += (__int128)(size[at] - 1) * llabs(h->y_stride[at]);
   }
   bool same = h->x == h->y;
   for (int i = 0; i < 3; ++i) same = same && (size[i] == 1 || h->x_stride[i] == h->y_stride[i]);
