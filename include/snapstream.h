@@ -413,7 +413,8 @@ typedef struct {
  * not finite, as snap_compress's pooled_out is outside the candidates).
  *   k_new [n][n_kv_heads][max_len][d_qk] in_dtype, v_new likewise (NULL when
  *   v_in_k), at strides k_stride / v_stride (host arrays: sequence, head, token
- *   in elements, multiples of 16 bytes; NULL: contiguous),
+ *   in elements, multiples of 16 bytes along sizes of more than 1; NULL:
+ *   contiguous),
  *   weight_new [n][n_kv_heads][max_len] fp32, contiguous.
  * Sequences with rows[slot] < 0 and rows past the page table are skipped.  rows
  * and pos are left as they are; pos may be NULL when the cache has no token

@@ -471,8 +471,9 @@ snap_status snap_paged_append(const snap_params* p, const snap_paged_cache* cach
   if (!p->v_in_k && (!v_new || !aligned16(v_new)))
     return fail(SNAP_ERR_INVALID_ARG, "v_new is NULL or not 16-byte aligned");
   const int per16 = p->in_dtype == SNAP_F32 ? 4 : 8;
-  for (int i = 0; i < 3; ++i)
-    if ((k_stride && k_stride[i] % per16) || (!p->v_in_k && v_stride && v_stride[i] % per16))
+  const int32_t size[3] = {n, p->n_kv_heads, max_len};
+  for (int i = 0; i < 3; ++i)  // (a stride along a size of 1 says nothing)
+    if (size[i] > 1 && ((k_stride && k_stride[i] % per16) || (!p->v_in_k && v_stride && v_stride[i] % per16)))
       return fail(SNAP_ERR_INVALID_ARG, "strides of k_new / v_new must be multiples of 16 bytes");
   st = launch_paged_append(*p, *cache, rows, pos, n, slot_ids, lengths, max_len, k_new, k_stride, v_new, v_stride,
                            weight_new, (hipStream_t)stream);
