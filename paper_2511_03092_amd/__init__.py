@@ -359,6 +359,8 @@ def _rope_heads(x, y, name: str):
 def snap_rope(r: RopeParams, q, k=None, q_out=None, k_out=None, pos=None, slot_ids=None, lengths=None, stream=None):
     """Rotates q [n, heads, tokens, d] and k (any strides but the last) into q_out / k_out, or in place."""
     import torch
+    if q is None:
+        _bad("q is None")
     dtype, index = q.dtype, q.get_device()
     if dtype is not torch.bfloat16 and dtype is not torch.float32:
         _bad(f"q must be bfloat16 or float32 (got {dtype})")
@@ -388,6 +390,8 @@ def paged_cache_struct(k, v, page_table, token=None, weight=None, k_scale=None, 
     """The handle of a paged cache: k [n_pages, n_kv_heads, page_size, d_qk], v likewise (None for a latent cache),
     page_table [n_slots, max_pages], token and weight [n_pages, n_kv_heads, page_size].  It holds the tensors."""
     import torch
+    if k is None:
+        _bad("k is None")
     if k.dim() != 4 or k.dtype not in (torch.float32, torch.bfloat16, torch.uint8):
         _bad(f"k must be [n_pages, n_kv_heads, page_size, d] float32, bfloat16 or uint8 (got {tuple(k.shape)} {k.dtype})")
     index, pages = k.get_device(), k.shape[:3]
@@ -418,6 +422,8 @@ def paged_cache_struct(k, v, page_table, token=None, weight=None, k_scale=None, 
 
 def _paged(p: Params, cache: SnapPagedCache, rows, pos, slot_ids):
     """Checks what every paged call shares; the number of sequences and the parameters' structure."""
+    if cache is None or slot_ids is None:
+        _bad("cache or slot_ids is None")
     values, params = tuple(vars(p).values()), cache.params
     if params[0] != values:  # (the same parameters as the last call's: the same structure)
         kind = (p.kv_dtype, p.n_kv_heads, p.d_qk, None if p.v_in_k else p.d_v)
@@ -445,7 +451,7 @@ def snap_paged_append(p: Params, cache: SnapPagedCache, rows, pos, slot_ids, k_n
     """Stores k_new [n, n_kv_heads, tokens, d_qk] and v_new (any strides but the last) behind the rows held."""
     import torch
     (n, cp), index, heads = _paged(p, cache, rows, pos, slot_ids), cache.index, p.n_kv_heads
-    if k_new.dim() != 4 or (v_new is None) != bool(p.v_in_k):
+    if k_new is None or k_new.dim() != 4 or (v_new is None) != bool(p.v_in_k):
         _bad("k_new must be [n, n_kv_heads, tokens, d_qk], with v_new unless the values are in the keys")
     tokens = k_new.shape[2]
     ks = _strides(k_new, "k_new", cache.in_dtype, (n, heads, tokens, p.d_qk), index)
@@ -469,6 +475,8 @@ def snap_paged_evict_workspace(p: Params, n: int, max_rows: int) -> int:
 
 
 def _bytes(workspace, index: int) -> int:
+    if workspace is None:
+        return 0
     if workspace.get_device() != index or not workspace.is_contiguous():
         _bad(f"workspace must be contiguous on device {index} (got {workspace.device})")
     return workspace.numel() * workspace.element_size()
@@ -478,6 +486,8 @@ def _paged_io(p: Params, cache: SnapPagedCache, n: int, q, out) -> int:
     """Checks queries and output; the output's type code."""
     import torch
     _want(q, "q", cache.in_dtype, (n, p.n_q_heads, p.d_qk), cache.index)
+    if out is None:
+        _bad("out is None")
     bf16 = out.dtype is torch.bfloat16
     _want(out, "out", torch.bfloat16 if bf16 else torch.float32, (n, p.n_q_heads, p.d_v), cache.index)
     return SNAP_BF16 if bf16 else SNAP_F32
@@ -500,7 +510,7 @@ def snap_paged_decode_step(p: Params, cache: SnapPagedCache, rows, pos, slot_ids
     od = _paged_io(p, cache, n, q, out)
     if (v_new is None) != bool(p.v_in_k):
         _bad("v_new must be given unless the values are in the keys")
-    heads = (n, p.n_kv_heads) if k_new.dim() == 3 else (n, p.n_kv_heads, 1)
+    heads = (n, p.n_kv_heads) if k_new is not None and k_new.dim() == 3 else (n, p.n_kv_heads, 1)
     _want(k_new, "k_new", cache.in_dtype, heads + (p.d_qk,), index)
     if v_new is not None:
         _want(v_new, "v_new", cache.in_dtype, heads + (p.d_v,), index)
