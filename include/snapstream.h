@@ -494,7 +494,8 @@ snap_status snap_paged_evict(const snap_params* p, const snap_paged_cache* cache
  * outside the candidates, 16 decode rows past the budget, 32 new token's row
  * outside the sink/ring rows, 64 too many split-K chunks, 128 appended row
  * outside the sink/ring rows, 256 prefill block outside the prompt, 512 paged
- * work item past the workspace, 1024 evicted rows past their move list. */
+ * rows cut into more work items than are launched, 1024 evicted rows past their
+ * move list. */
 snap_status snap_debug_checks(uint32_t* flags, int32_t reset);
 
 /* Static description of a status code. */

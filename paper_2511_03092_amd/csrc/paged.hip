@@ -97,22 +97,8 @@ __device__ __forceinline__ bool paged_seq(const PagedArgs& a, int key, bool by_i
     mine += nb;
   }
   const int64_t total = wave_total((int)(mine & 0xfffff)) + ((int64_t)wave_total((int)(mine >> 20)) << 20);
-  // Blocks an item: as few as keep the items within a.waves.  total / waves of
-  // them may give more (a unit's last item is short), total / target never does;
-  // up to 64 sequences, whose lengths the lanes hold, some between are tried.
-  const int64_t t64 = total * a.Hkv;
-  int64_t c64 = (t64 + a.target - 1) / a.target;
-  if (a.n <= 64) {
-    const int64_t least = (t64 + a.waves - 1) / a.waves, step = (c64 - least) / 4 + 1;
-    for (int64_t c = least; c < c64; c += step) {
-      const int ni = c > 0 ? (nb0 + (int)c - 1) / (int)c : 0;
-      if ((int64_t)a.Hkv * wave_total(ni) <= a.waves) {
-        c64 = c;
-        break;
-      }
-    }
-  }
-  const int C = c64 < 1 ? 1 : (int)c64;
+  const int C = paged_chunk(a.waves, a.target, a.n, a.Hkv, total,
+                            [&](int c) { return wave_total(c > 0 ? (nb0 + c - 1) / c : 0); });  // (up to 64 sequences)
   int items_before = 0, slot_next;
   int64_t blocks_before = 0;
   int len_next = rows_of(a, min(lane, a.n - 1), slot_next);
@@ -134,7 +120,8 @@ __device__ __forceinline__ bool paged_seq(const PagedArgs& a, int key, bool by_i
       s.items = __builtin_amdgcn_readlane(ni, at);
       s.item0 = __builtin_amdgcn_readlane(first, at);
       s.block0 = blocks_before + (int64_t)a.Hkv * __builtin_amdgcn_readlane(sb - nb, at);
-      return true;
+      // (items past the launch would be rows that nothing attends)
+      return debug_check(s.item0 + a.Hkv * s.items <= a.max_items, kDbgPagedItem);
     }
     items_before += a.Hkv * __builtin_amdgcn_readlane(si, 63);
     blocks_before += (int64_t)a.Hkv * __builtin_amdgcn_readlane(sb, 63);
@@ -284,7 +271,6 @@ struct PagedItem {
 };
 __device__ __forceinline__ bool paged_item(const PagedArgs& a, int item, PagedItem& it) {
   if (!paged_seq(a, item, true, it.s)) return false;
-  if (!debug_check(item < a.max_items, kDbgPagedItem)) return false;
   const int local = item - it.s.item0, chunk = local % it.s.items;
   it.g = local / it.s.items;
   it.r0 = (int)((int64_t)chunk * it.s.blocks / it.s.items) * kBlockRows;
@@ -1184,12 +1170,8 @@ static bool whole_units(int units, int waves, int max_rows) { return units >= 2 
 PagedGeometry paged_geometry(const snap_params& p, int n, int max_rows, bool weigh) {
   PagedGeometry g{};
   const int units = (n > 0 ? n : 1) * p.n_kv_heads, G = p.n_q_heads / p.n_kv_heads;
-  g.waves = resident_items(p, weigh);
-  g.target = units < g.waves / 2 ? g.waves - units : g.waves / 2;
   const int64_t blocks = (int64_t)units * ((max_rows + kBlockRows - 1) / kBlockRows);
-  // ceil(blocks / C) a unit, C >= blocks / target: at most target + units items,
-  // and no more than there are blocks
-  g.max_items = (int)(blocks < g.target + units ? blocks : g.target + units);
+  (PagedCut&)g = paged_cut(units, resident_items(p, weigh), blocks);
   size_t off = 0;
   g.off_part = off;
   off = align256(off + (size_t)g.max_items * G * p.d_v * sizeof(float));

@@ -7,6 +7,7 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "paged_cut.h"
 #include "snapstream.h"
 
 namespace snap {
@@ -148,7 +149,7 @@ enum : uint32_t {
   kDbgCombine = 1u << 6,     // more split-K chunks than the combine holds
   kDbgAppend = 1u << 7,      // an appended row outside the sink / ring rows
   kDbgPrefill = 1u << 8,     // a prefill block's positions outside the prompt
-  kDbgPagedItem = 1u << 9,   // a paged work item past the workspace's partials
+  kDbgPagedItem = 1u << 9,   // paged rows cut into more items than are launched
   kDbgPagedMove = 1u << 10,  // an evicted slot's move list past its end
 };
 #ifdef SNAP_DEBUG_CHECKS
@@ -272,10 +273,7 @@ snap_status launch_rope(const snap_rope_params& r, int dtype, int n_seq, int max
 
 // Paged decode: the call's work items (chunks of one (sequence, KV head)'s
 // rows, cut on the device from the rows that are there) and its workspace.
-struct PagedGeometry {
-  int waves;      // items that the card holds at once
-  int target;     // items that the rows are cut into, besides one per unit at most
-  int max_items;  // items at most: target + units
+struct PagedGeometry : PagedCut {
   size_t off_part, off_ml, off_z, bytes;
 };
 PagedGeometry paged_geometry(const snap_params& p, int n, int max_rows, bool weigh);
