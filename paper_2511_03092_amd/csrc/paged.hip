@@ -1163,8 +1163,16 @@ static int joined_waves(const snap_params& p, int n, int max_rows, bool weigh) {
 }
 
 // Units that fill the card twice over and are short are an item each: the card
-// balances them, and no workgroup reads every length to find its own (1000 latent
-// sequences of 100 rows 308 -> 108 us).
+// balances them, and no workgroup reads every length to find its own.  What is lost is
+// the cut of one long sequence among short ones, for which the bound on the rows
+// stands.  Steps of 1000 (latent) and 520 (32 query heads on 8, 128-wide) bf16
+// sequences, us, an item each / cut:
+//   rows                    latent      128-wide
+//   all 100                113 / 314    84 / 150
+//   one of 2048, 2100      186 / 350   186 / 171
+//   one of 4096            265 / 349   289 / 171
+//   all 4096 (600, 520)    573 / 654  1460 / 1524
+//   1 to 4096 (600, 520)   372 / 449   806 / 872
 static bool whole_units(int units, int waves, int max_rows) { return units >= 2 * waves && max_rows <= 4096; }
 
 PagedGeometry paged_geometry(const snap_params& p, int n, int max_rows, bool weigh) {
