@@ -50,8 +50,8 @@ constexpr int kPickThreads = 1024;
 constexpr int kPickWaves = kPickThreads / 64;
 constexpr int kTileRows = 4 * kPickThreads;  // four neighbouring rows (of one page) a thread
 constexpr int kPickRows = 2 * kTileRows;     // rows that one workgroup selects among
-// The keys' 31 bits (but for kProtected) in three parts, the leading ones (exponent and three bits
-// more) first.
+// The keys' 31 bits (but for kProtected) in three parts, the leading ones (exponent and
+// three bits more) first.
 constexpr int kParts = 3;
 constexpr int kBins = 2048;
 __device__ __forceinline__ constexpr int part_shift(int part) { return part == 0 ? 20 : (part == 1 ? 10 : 0); }
@@ -322,7 +322,7 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick(EvictArgs a) {
 // other two parts, counts the rows kept before its split, and writes its share of the
 // lists.  Nothing is cleared, added atomically in memory or waited for inside a
 // launch, and the three reads of 4 bytes a row hit the cache.  1 sequence x 8 heads
-// of 32k rows 5.6 + 17 us, 8 x 8 of 18k 7 + 18.
+// of 32k rows 6.2 + 16.3 us, 8 x 8 of 18k 8.3 + 17.5.
 struct SplitArgs {
   uint32_t* keys;  // [units][row_pad]
   int* hist;       // [units][splits][kBins]
@@ -506,8 +506,8 @@ __global__ __launch_bounds__(kPickThreads) void evict_split_lists(EvictArgs a, S
 }
 
 // block x: share of the moves, y: unit.  8 x 8 units of 1500 moves of 520 bytes (100 MB
-// read and written) 24 us, 4.2 TB/s; few moves are bound by the chain of dependent
-// loads (list, page, row): 8 units of 1300, 9 us.
+// read and written) 23.5 us, 4.2 TB/s; few moves are bound by the chain of dependent
+// loads (list, page, row): 8 units of 3700 (31 MB) 9.1 us, 3.4 TB/s.
 __global__ __launch_bounds__(256) void evict_move(EvictArgs a, int shares) {
   const int unit = bid_y(), b = unit / a.Hkv, g = unit % a.Hkv;
   const int n = a.count[unit];

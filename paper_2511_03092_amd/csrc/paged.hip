@@ -151,8 +151,8 @@ __device__ __forceinline__ int64_t paged_row(const PagedArgs& a, int slot, int g
 // a page table.
 // A head's reference maximum moves only when a block's exceeds it by kStaleMax
 // (log2 units), so the accumulators are rescaled on few blocks.
-// HBM bound: 8 sequences of 19k to 128k rows x 8 KV heads, 128-wide bf16 (2.52 GB) 397
-// us, 6.3 TB/s with the join; fp8 209 us, 6.0 TB/s.  Values prefetched a block ahead
+// HBM bound: 8 sequences of 19k to 128k rows x 8 KV heads, 128-wide bf16 (2.52 GB) 380
+// to 397 us, 6.3 to 6.6 TB/s with the join; fp8 210 us, 6.0 TB/s.  Values prefetched a block ahead
 // like the keys change nothing, there or for short sequences.
 // 16-bit and fp8 rows: probabilities enter the products whole, as three bf16 terms
 // of 8 bits.  Two terms, cut off, are off by up to 2^-15 and always to the same side,
@@ -708,9 +708,9 @@ __global__ __launch_bounds__(64 * WAVES) void paged_gqa(PagedArgs a) {
 // 102.6 -> 107, fp8 72 -> 79 us in the cases below); against the same attention in fp32
 // the bf16 outputs of the bf16 case are 9e-5 off with two terms, 7e-5 with three (mostly
 // roundings to the other neighbour), 2e-4 with two that are cut off.
-// HBM bound in bf16: 16 sequences of 32k rows (604 MB) 100 us, 6.0 TB/s; blocks of 32
+// HBM bound in bf16: 16 sequences of 32k rows (604 MB) 102 us, 5.9 TB/s; blocks of 32
 // rows in four stages, the dims of a product split over the waves, take as long.  fp8
-// (302 MB, 16 heads) 70 us: the conversions, and a block's two barriers with two
+// (302 MB, 16 heads) 74 us: the conversions, and a block's two barriers with two
 // workgroups a CU; the 32-row form takes 82.
 constexpr int kLatRows = 64;
 __device__ const u32x4 kZeroRow[72] = {};

@@ -196,7 +196,9 @@ __global__ __launch_bounds__(256) void rope_pieces(RopeArgs a) {
 }
 
 // The same for pieces that are not whole: rotated dims, widths, strides or
-// addresses that 16 bytes do not divide.  One pair or copied dim per thread.
+// addresses that 16 bytes do not divide.  One pair or copied dim per thread, so bound by
+// the number of accesses: the 32k prompt with 24 of its 128 dims rotated takes 475 us
+// (whole pieces, all 128: 142).
 template <typename T>
 __global__ __launch_bounds__(256) void rope_any(RopeArgs a) {
   const unsigned np = a.rot / 2, cols = np + (a.in_place ? 0 : a.d - a.rot);
