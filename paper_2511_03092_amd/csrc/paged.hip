@@ -1145,11 +1145,12 @@ static int resident_items(const snap_params& p, bool weigh) {
 // more (then also nothing is written for the join).  Measured, one launch / two, 32
 // query heads on 8, us:
 //   rows               256        512        1024       2048
-//   128 bf16   1 x   8.9/11.5  10.8/11.5  15.3/11.3  23.9/11.3   64 x  20/25  29/35  47/55  99/95
-//   128 fp8    1 x   8.6/11.1  10.4/11.3  13.9/11.2  20.4/11.6   64 x  16/20  24/26  33/36  52/57
-//   64 fp8     1 x   8.5/11.1   8.5/11.1  10.7/11.2  15.6/11.3   64 x   9/20  12/22  18/27  28/38
+//   128 bf16   1 x   8.9/11.5  10.8/11.5  15.3/11.3  23.9/11.3   64 x  21/24  30/35  48/55 100/95
+//   128 fp8    1 x   8.7/11.1  10.7/11.3  14.4/11.2  21.2/11.6   64 x  17/21  25/27  34/36  53/56
+//   64 fp8     1 x   8.5/11.1   8.5/11.1  11.2/11.2  16.5/11.3   64 x   9/20  12/22  19/28  28/40
 //   64 fp32    1 x   8.6/11.2  12.1/11.3  18.1/11.3  29.3/11.2   64 x  20/26  30/36  49/56 102/97
 //   128 fp32   1 x  12.6/11.3  18.7/11.3  29.2/11.4  50.1/12.4   64 x  31/37  50/58 106/103
+// (two launches of one sequence are bound by the host; in a graph they take 9.4 to 12.3)
 constexpr int kJoinedLogits = 6144;  // with weights: beside 32 KB for the join, within 64 KB of LDS
 static int joined_waves(const snap_params& p, int n, int max_rows, bool weigh) {
   if (p.d_qk != p.d_v) return 0;
