@@ -17,7 +17,11 @@
  * does both for one layer).  Beside it stand rotary positions for the queries
  * and keys that go in (snap_rope) and a paged cache of growing length, for
  * layers that are not compressed and for sequences that are cut back to the
- * budget later by the attention their rows received (snap_paged_*).
+ * budget later by the attention their rows received (snap_paged_*).  The pages
+ * themselves are handed out and taken back on the device (snap_pages_*), and a
+ * cache that drops nothing holds its rows in blocks, in 8 bits with a scale for
+ * each block and head, and may read only the blocks that matter to a query
+ * (snap_block_*).
  *
  * Conventions shared by every call
  *  - Token positions are 0-based; a prompt of length L holds tokens 0..L-1 and
@@ -41,9 +45,10 @@
  *    (L and min(K, |C|)).
  *  - Batch limits of the launch grids: n_seq * n_kv_heads <= 65535
  *    (snap_compress, snap_prefill, snap_prefill_attn, snap_paged_append,
- *    snap_paged_evict) and n * n_q_heads <= 65535 (snap_decode_attn,
- *    snap_decode_step, snap_paged_decode_attn, snap_paged_decode_step); larger
- *    calls return SNAP_ERR_UNSUPPORTED (split the batch).
+ *    snap_paged_evict, snap_block_append) and n * n_q_heads <= 65535
+ *    (snap_decode_attn, snap_decode_step, snap_paged_decode_attn,
+ *    snap_paged_decode_step, snap_block_decode_attn, snap_block_decode_step);
+ *    larger calls return SNAP_ERR_UNSUPPORTED (split the batch).
  */
 #ifndef SNAPSTREAM_H
 #define SNAPSTREAM_H
@@ -66,7 +71,8 @@ typedef enum {
 typedef enum {
   SNAP_F32 = 0,
   SNAP_BF16 = 1,
-  SNAP_FP8_E4M3 = 2 /* OCP E4M3 (fn): bias 7, max 448, no inf; cache only */
+  SNAP_FP8_E4M3 = 2, /* OCP E4M3 (fn): bias 7, max 448, no inf; cache only */
+  SNAP_INT8 = 3      /* whole numbers -127..127; block caches only          */
 } snap_dtype;
 
 typedef enum {
@@ -482,6 +488,177 @@ snap_status snap_paged_evict(const snap_params* p, const snap_paged_cache* cache
                              const int32_t* pos, int32_t* rows_out, int32_t n, const int32_t* slot_ids,
                              int32_t max_rows, int32_t* kept_out, void* workspace, size_t ws_bytes, void* stream);
 
+/* Stores the tokens of a packed batch by a map (snap_pages_map's): token i < tokens
+ * of the batch goes to row row_of[i] (page * page_size + row of the page) of every
+ * KV head, with token = pos_of[i] and weight 0.  Its scales (fp8) are those of slot
+ * slot_ids[seq_of[i]].
+ *   k_new [tokens][n_kv_heads][d_qk] in_dtype, v_new likewise (NULL when v_in_k),
+ *   at strides k_stride / v_stride (host arrays: token, head in elements, multiples
+ *   of 16 bytes along sizes of more than 1; NULL: contiguous).
+ * A token whose row is outside [0, n_pages * page_size), whose sequence is outside
+ * [0, n) or whose slot is outside [0, n_slots) is not stored.  The rows must be
+ * distinct.  pos_of may be NULL when the cache has no token array. */
+snap_status snap_paged_append_mapped(const snap_params* p, const snap_paged_cache* cache, int32_t n,
+                                     const int32_t* slot_ids, int32_t tokens, const int32_t* seq_of,
+                                     const int32_t* row_of, const int32_t* pos_of, const void* k_new,
+                                     const int64_t* k_stride, const void* v_new, const int64_t* v_stride, void* stream);
+
+/* ---- page tables -----------------------------------------------------------
+ * The pages of a paged or block cache handed out and taken back on the device, so
+ * that a serving step needs no host round trip for them.
+ *   page_table [n_slots][max_pages] int32: as in the caches
+ *   held       [n_slots] int32: the pages that each slot has, entries [0, held)
+ *   free_pages [n_pages] int32: the pages nobody has are entries [0, n_free)
+ *   n_free     [1] int32
+ * All device memory of the caller, filled once: held 0, page_table -1, free_pages
+ * every page, n_free n_pages.  A slot's pages are its own: pages shared between
+ * slots are not counted here and must not be handed back. */
+typedef struct {
+  int32_t* page_table;
+  int32_t* held;
+  int32_t* free_pages;
+  int32_t* n_free;
+  int32_t n_slots;
+  int32_t n_pages;   /* n_pages * page_size < 2^31 */
+  int32_t page_size; /* a power of two, 16..4096 */
+  int32_t max_pages; /* max_pages * page_size <= 2^28 */
+} snap_page_pool;
+
+/* Room for lengths[b] (len when lengths is NULL) more rows behind the rows[slot]
+ * that slot slot_ids[b] holds: the pages it lacks up to then are taken off the end
+ * of the free list and entered behind those it has.  Sequences are served in order
+ * of b, each whole or not at all: b is served when its pages and those of all
+ * sequences before it, served or not, are free together, or when it lacks none;
+ * one that wants more than max_pages is not and does not count.
+ *   short_out [n] int32: the pages b lacks (0: served), optional.
+ * Sequences with a slot id out of range or rows[slot] < 0 are skipped (short 0).
+ * The slots must be distinct.  One workgroup: a call is a few microseconds. */
+snap_status snap_pages_reserve(const snap_page_pool* pool, const int32_t* rows, int32_t n, const int32_t* slot_ids,
+                               const int32_t* lengths, int32_t len, int32_t* short_out, void* stream);
+
+/* Takes back the pages behind the rows[slot] rows that each slot holds (all of them
+ * where that is 0 or less): their entries become -1, and they go to the end of the
+ * free list in the order that undoes snap_pages_reserve.  After an eviction, or with
+ * rows = 0 at a sequence's end.  The slots must be distinct. */
+snap_status snap_pages_release(const snap_page_pool* pool, const int32_t* rows, int32_t n, const int32_t* slot_ids,
+                               void* stream);
+
+/* The map of a packed batch whose sequence b has lengths[b] tokens (negative: none)
+ * behind the rows[slot] it holds, from the page table as it is:
+ *   starts [n + 1] int32: the batch's first token of each sequence, then their sum
+ *          (none above tokens),
+ *   seq_of, row_of, pos_of [tokens] int32: each token's sequence b, its physical row
+ *          (page * page_size + row of the page; -1 where there is no page) and its
+ *          position pos[slot] + t (rows[slot] + t when pos is NULL).
+ * Entries past the batch's tokens are -1, -1 and 0.  A sequence with a slot id out
+ * of range or rows[slot] < 0 has rows -1 and positions 0.  tokens (host) is the
+ * room in the maps; tokens past it are left out.  pool's held and free list are not
+ * read and may be NULL here. */
+snap_status snap_pages_map(const snap_page_pool* pool, const int32_t* rows, const int32_t* pos, int32_t n,
+                           const int32_t* slot_ids, const int32_t* lengths, int32_t tokens, int32_t* starts,
+                           int32_t* seq_of, int32_t* row_of, int32_t* pos_of, void* stream);
+
+/* ---- block cache -----------------------------------------------------------
+ * A paged cache that only grows, whose rows stand in blocks of `block` tokens: in 8
+ * bits with a scale for each block and KV head, formed from the block's own values
+ * (nothing to guess, nothing saturates), or in bf16; with bounds of each block's
+ * keys, a step may read only the blocks that can matter to its queries.
+ *   k, v   [n_pages][n_kv_heads][page_size][d] kv_dtype: SNAP_INT8, SNAP_FP8_E4M3 or
+ *          SNAP_BF16 (inputs are bf16; d_qk = d_v = 64 or 128)
+ *   k_scale, v_scale [n_pages][n_kv_heads][page_size / block] fp32 (8 bits; NULL: bf16)
+ *   k_tail, v_tail   [n_slots][n_kv_heads][block][d] bf16 (8 bits; NULL: bf16): the
+ *          rows of the block that the slot's newest token is in, row r at r % block,
+ *          as they came.  Until a block is whole it has no codes, and while it is the
+ *          newest token's it is attended from here.
+ *   bound  [n_pages][n_kv_heads][page_size / block][2][d] int8, and
+ *   bound_scale [n_pages][n_kv_heads][page_size / block] fp32: of the whole blocks'
+ *          keys, the least (rounded down) and the largest (rounded up) of every dim,
+ *          in units of bound_scale; NULL (both) where nothing is selected
+ * A whole block's scale is s = amax / 127 (int8, and bounds) or amax / 448 (E4M3),
+ * amax the largest magnitude of its finite values, at least 2^-126, 1 where amax is
+ * 0; codes are x / s (fp32 quotient) rounded to nearest even, saturating; NaN is the
+ * code 0 in int8, E4M3's NaN code there, and no bound.  So codes and scales do not
+ * depend on how the tokens were split into calls.
+ * Page ids outside [0, n_pages) are pages that are not there: nothing is stored in
+ * their rows (nor kept in the tail for them), and they receive no attention.  Slots
+ * may share pages of whole blocks that none of them writes to. */
+typedef struct {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  void* k_tail;
+  void* v_tail;
+  void* bound;
+  float* bound_scale;
+  const int32_t* page_table;
+  int32_t n_slots;
+  int32_t n_pages;
+  int32_t page_size; /* a power of two, block..4096 */
+  int32_t max_pages; /* max_pages * page_size <= 2^28 */
+  int32_t block;     /* 32, 64 or 128 */
+} snap_block_cache;
+
+/* Stores new tokens behind the rows[slot] rows held: token t < lengths[b] (max_len
+ * when lengths is NULL) of sequence b in row rows[slot] + t.
+ *   starts NULL: k_new [n][n_kv_heads][max_len][d], v_new likewise, at strides
+ *     (host arrays: sequence, head, token in elements, multiples of 16 bytes along
+ *     sizes of more than 1; NULL: contiguous);
+ *   starts [n + 1] (device int32, as snap_pages_map's): a packed batch of `tokens`
+ *     tokens, k_new [tokens][n_kv_heads][d]; sequence b has tokens starts[b] ..
+ *     starts[b + 1] - 1 (at most max_len of them; starts outside [0, tokens] are
+ *     clamped); lengths is then NULL, and of the strides the sequence's is not read
+ *     (NULL: contiguous).
+ * Sequences with rows[slot] < 0 and rows past the page table are skipped.  rows is
+ * left as it is.  The slots must be distinct. */
+snap_status snap_block_append(const snap_params* p, const snap_block_cache* cache, const int32_t* rows, int32_t n,
+                              const int32_t* slot_ids, const int32_t* lengths, const int32_t* starts, int32_t tokens,
+                              int32_t max_len, const void* k_new, const int64_t* k_stride, const void* v_new,
+                              const int64_t* v_stride, void* stream);
+
+/* Blocks that a selection lists at most for a sequence and KV head:
+ * ceil(sink / block) + ceil((recent - 1) / block) + ceil(topk / block).  0 on invalid
+ * parameters. */
+int32_t snap_block_chosen(const snap_params* p, int32_t block);
+
+/* Bytes of workspace snap_block_decode_attn / _step need for n sequences of at most
+ * max_rows rows (the new one included); no fewer than for fewer sequences or rows.
+ * 0 on invalid parameters. */
+size_t snap_block_decode_workspace(const snap_params* p, int32_t n, int32_t max_rows, int32_t block, int32_t select);
+
+/* Attention of one new token per sequence (already stored), at row r = rows[slot],
+ * over the rows [0, r] of its slot (select = 0): out[b][h] = sum_j softmax_j(sm_scale
+ * q.k_j) v_j, zero for a sequence without rows; blocks before the new token's by
+ * their codes, its own by its rows as they came.
+ * select = 1: over the new token's block and, of the blocks before it,
+ *   those with one of the first `sink` rows or of the last `recent` ones, and
+ *   the ceil(topk / block) others of the largest score (equal scores: the lower
+ *   block),
+ * for each KV head.  The score is an upper bound of what a query of the KV head's
+ * group may have in a block, formed in whole numbers: with a query's codes a_d =
+ * round(q_d / u), u = amax |q_d| / 127 (as a block's scale), and the block's bounds,
+ *   score = bound_scale * max_h u_h * sum_d (a_d > 0 ? a_d largest_d : a_d least_d).
+ * max_rows (host, at most max_pages * page_size) bounds the rows of every sequence;
+ * one that holds more attends those of its whole blocks that lie below max_rows.
+ * select needs bounds and at most 32768 blocks (SNAP_ERR_UNSUPPORTED above).
+ *   q [n][n_q_heads][d] bf16, out [n][n_q_heads][d] out_dtype,
+ *   sel_out [n][n_kv_heads][snap_block_chosen] int32, optional: the blocks selected,
+ *           ascending, then -1 (select = 1; not written otherwise),
+ *   workspace >= snap_block_decode_workspace(...) bytes, 256-byte aligned; its
+ *           contents on entry do not matter. */
+snap_status snap_block_decode_attn(const snap_params* p, const snap_block_cache* cache, const int32_t* rows, int32_t n,
+                                   const int32_t* slot_ids, int32_t max_rows, const void* q, void* out,
+                                   int32_t out_dtype, int32_t select, int32_t* sel_out, void* workspace,
+                                   size_t ws_bytes, void* stream);
+
+/* snap_block_append of one token per sequence (k_new, v_new [n][n_kv_heads][d],
+ * contiguous) followed by snap_block_decode_attn: the same results and cache
+ * contents.  The slots of the call are distinct. */
+snap_status snap_block_decode_step(const snap_params* p, const snap_block_cache* cache, const int32_t* rows, int32_t n,
+                                   const int32_t* slot_ids, int32_t max_rows, const void* q, const void* k_new,
+                                   const void* v_new, void* out, int32_t out_dtype, int32_t select, int32_t* sel_out,
+                                   void* workspace, size_t ws_bytes, void* stream);
+
 /* Device-side checks of the debug build (libsnapstream_debug.so, built with
  * SNAP_DEBUG_CHECKS): its kernels test the invariants their indexing rests on
  * (keys inside the prompt, kept tokens inside the candidates, rows inside the
@@ -495,7 +672,7 @@ snap_status snap_paged_evict(const snap_params* p, const snap_paged_cache* cache
  * outside the sink/ring rows, 64 too many split-K chunks, 128 appended row
  * outside the sink/ring rows, 256 prefill block outside the prompt, 512 paged
  * rows cut into more work items than are launched, 1024 evicted rows past their
- * move list. */
+ * move list, 2048 more blocks selected than a list holds. */
 snap_status snap_debug_checks(uint32_t* flags, int32_t reset);
 
 /* Static description of a status code. */

@@ -9,6 +9,8 @@ Functions keep the C names (include/snapstream.h):
     snap_compress, snap_prefill, snap_prefill_attn, snap_cache_append, snap_decode_attn, snap_decode_step,
     snap_decode_step_noalloc, snap_advance, snap_debug_checks,
     snap_rope, snap_paged_append, snap_paged_decode_attn, snap_paged_decode_step, snap_paged_evict,
+    snap_paged_append_mapped, snap_pages_reserve, snap_pages_release, snap_pages_map,
+    snap_block_append, snap_block_decode_attn, snap_block_decode_step, snap_block_chosen, snap_block_decode_workspace,
     snap_paged_decode_workspace, snap_paged_evict_workspace, snap_compress_workspace, snap_prefill_workspace, snap_decode_workspace, snap_status_str
 """
 from __future__ import annotations
@@ -23,7 +25,7 @@ LIB_PATH = os.path.join(_HERE, "libsnapstream.so")
 DEBUG_LIB_PATH = os.path.join(_HERE, "libsnapstream_debug.so")
 
 SNAP_OK, SNAP_ERR_INVALID_ARG, SNAP_ERR_UNSUPPORTED, SNAP_ERR_WORKSPACE, SNAP_ERR_HIP = range(5)
-SNAP_F32, SNAP_BF16, SNAP_FP8_E4M3 = 0, 1, 2
+SNAP_F32, SNAP_BF16, SNAP_FP8_E4M3, SNAP_INT8 = 0, 1, 2, 3
 SNAP_POOL_MAX, SNAP_POOL_AVG = 0, 1
 SNAP_NORM_CAND, SNAP_NORM_ROW = 0, 1
 SNAP_FP8_SCALES_GIVEN, SNAP_FP8_SCALES_AMAX = 0, 1
@@ -36,7 +38,9 @@ EXPORTED = ["snap_compress_workspace", "snap_decode_workspace", "snap_prefill_wo
             "snap_decode_attn", "snap_decode_step", "snap_decode_step_noalloc", "snap_advance", "snap_debug_checks",
             "snap_rope", "snap_paged_append", "snap_paged_decode_workspace", "snap_paged_decode_attn",
             "snap_paged_decode_step", "snap_paged_evict_workspace", "snap_paged_evict",
-            "snap_status_str", "snap_last_error"]
+            "snap_paged_append_mapped", "snap_pages_reserve", "snap_pages_release", "snap_pages_map",
+            "snap_block_append", "snap_block_chosen", "snap_block_decode_workspace", "snap_block_decode_attn",
+            "snap_block_decode_step", "snap_status_str", "snap_last_error"]
 
 
 class SnapParams(ctypes.Structure):
@@ -69,6 +73,18 @@ class SnapPagedCache(ctypes.Structure):
                 ("v_scale", ctypes.c_void_p), ("token", ctypes.c_void_p), ("weight", ctypes.c_void_p),
                 ("page_table", ctypes.c_void_p), ("n_slots", ctypes.c_int32), ("n_pages", ctypes.c_int32),
                 ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
+
+
+class SnapPagePool(ctypes.Structure):
+    _fields_ = [("page_table", ctypes.c_void_p), ("held", ctypes.c_void_p), ("free_pages", ctypes.c_void_p),
+                ("n_free", ctypes.c_void_p), ("n_slots", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
+
+
+class SnapBlockCache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "k_tail", "v_tail", "bound", "bound_scale",
+                                               "page_table")] + [
+        (n, ctypes.c_int32) for n in ("n_slots", "n_pages", "page_size", "max_pages", "block")]
 
 
 class SnapError(RuntimeError):
@@ -152,6 +168,25 @@ def load(path: str) -> ctypes.CDLL:
     L.snap_paged_evict_workspace.restype = sz
     L.snap_paged_evict.argtypes = [P, PC, vp, vp, vp, i32, vp, i32, vp, vp, sz, vp]
     L.snap_paged_evict.restype = ctypes.c_int
+    L.snap_paged_append_mapped.argtypes = [P, PC, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.snap_paged_append_mapped.restype = ctypes.c_int
+    PP, BC = ctypes.POINTER(SnapPagePool), ctypes.POINTER(SnapBlockCache)
+    L.snap_pages_reserve.argtypes = [PP, vp, i32, vp, vp, i32, vp, vp]
+    L.snap_pages_reserve.restype = ctypes.c_int
+    L.snap_pages_release.argtypes = [PP, vp, i32, vp, vp]
+    L.snap_pages_release.restype = ctypes.c_int
+    L.snap_pages_map.argtypes = [PP, vp, vp, i32, vp, vp, i32, vp, vp, vp, vp, vp]
+    L.snap_pages_map.restype = ctypes.c_int
+    L.snap_block_append.argtypes = [P, BC, vp, i32, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
+    L.snap_block_append.restype = ctypes.c_int
+    L.snap_block_chosen.argtypes = [P, i32]
+    L.snap_block_chosen.restype = i32
+    L.snap_block_decode_workspace.argtypes = [P, i32, i32, i32, i32]
+    L.snap_block_decode_workspace.restype = sz
+    L.snap_block_decode_attn.argtypes = [P, BC, vp, i32, vp, i32, vp, vp, i32, i32, vp, vp, sz, vp]
+    L.snap_block_decode_attn.restype = ctypes.c_int
+    L.snap_block_decode_step.argtypes = [P, BC, vp, i32, vp, i32, vp, vp, vp, vp, i32, i32, vp, vp, sz, vp]
+    L.snap_block_decode_step.restype = ctypes.c_int
     L.snap_debug_checks.argtypes = [ctypes.POINTER(ctypes.c_uint32), i32]
     L.snap_debug_checks.restype = ctypes.c_int
     return L
@@ -420,30 +455,36 @@ def paged_cache_struct(k, v, page_table, token=None, weight=None, k_scale=None, 
     return c
 
 
-def _paged(p: Params, cache: SnapPagedCache, rows, pos, slot_ids):
-    """Checks what every paged call shares; the number of sequences and the parameters' structure."""
-    if cache is None or slot_ids is None:
-        _bad("cache or slot_ids is None")
+def _params_of(p: Params, cache):
+    """The parameters' structure, that of the last call while their values stay, after a check against the cache."""
     values, params = tuple(vars(p).values()), cache.params
-    if params[0] != values:  # (the same parameters as the last call's: the same structure)
+    if params[0] != values:
         kind = (p.kv_dtype, p.n_kv_heads, p.d_qk, None if p.v_in_k else p.d_v)
         if cache.kind != kind:
             _bad(f"the cache (type, heads, widths {cache.kind}) is not that of the parameters ({kind})")
         cache.params = params = (values, p.c())
+    return ctypes.byref(params[1])
+
+
+def _paged(p: Params, cache, rows, pos, slot_ids):
+    """Checks what every paged call shares; the number of sequences and the parameters' structure."""
+    if cache is None or slot_ids is None:
+        _bad("cache or slot_ids is None")
+    cp = _params_of(p, cache)
     n, index = slot_ids.shape[0], cache.index
     _want(slot_ids, "slot_ids", cache.i32, (n,), index)
     _want(rows, "rows", cache.i32, cache.slots_shape, index)
     if pos is not None:
         _want(pos, "pos", cache.i32, cache.slots_shape, index)
-    return n, ctypes.byref(params[1])
+    return n, cp
 
 
 def _strides(t, name: str, dtype, shape: tuple, index: int):
     st = t.stride()
-    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or st[3] != 1:
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or st[-1] != 1:
         _bad(f"{name} must be a {dtype} {tuple(shape)} tensor on device {index} whose rows are contiguous (got {t.dtype} "
              f"{tuple(t.shape)}, strides {st}, on {t.device})")
-    return _i64x3(*st[:3])
+    return _i64x3(*st[:-1])
 
 
 def snap_paged_append(p: Params, cache: SnapPagedCache, rows, pos, slot_ids, k_new, v_new=None, lengths=None,
@@ -531,6 +572,200 @@ def snap_paged_evict(p: Params, cache: SnapPagedCache, rows, pos, slot_ids, rows
     _launch(index, stream, lib().snap_paged_evict, cp, ctypes.byref(cache), _ptr(rows), _ptr(pos), _ptr(rows_out), n,
             _ptr(slot_ids), cache.rows_max if max_rows is None else max_rows, _ptr(kept_out), _ptr(workspace),
             _bytes(workspace, index))
+
+
+def snap_paged_append_mapped(p: Params, cache: SnapPagedCache, slot_ids, seq_of, row_of, pos_of, k_new, v_new=None,
+                             stream=None):
+    """Stores the tokens of a packed batch, k_new [tokens, n_kv_heads, d_qk] and v_new (any strides but the last), by the
+    map that snap_pages_map made of it."""
+    if cache is None or slot_ids is None:
+        _bad("cache or slot_ids is None")
+    cp, index, heads, n = _params_of(p, cache), cache.index, p.n_kv_heads, slot_ids.shape[0]
+    _want(slot_ids, "slot_ids", cache.i32, (n,), index)
+    if k_new is None or k_new.dim() != 3 or (v_new is None) != bool(p.v_in_k):
+        _bad("k_new must be [tokens, n_kv_heads, d_qk], with v_new unless the values are in the keys")
+    tokens = k_new.shape[0]
+    ks = _strides(k_new, "k_new", cache.in_dtype, (tokens, heads, p.d_qk), index)
+    vs = None if v_new is None else _strides(v_new, "v_new", cache.in_dtype, (tokens, heads, p.d_v), index)
+    for t, name in ((seq_of, "seq_of"), (row_of, "row_of"), (pos_of, "pos_of")):
+        if t is None or t.dim() != 1 or t.shape[0] < tokens:
+            _bad(f"{name} must have an entry for each of the {tokens} tokens")
+        _want(t, name, cache.i32, t.shape, index)
+    if n == 0 or tokens == 0:
+        return
+    _launch(index, stream, lib().snap_paged_append_mapped, cp, ctypes.byref(cache), n, _ptr(slot_ids), tokens, _ptr(seq_of),
+            _ptr(row_of), _ptr(pos_of), _ptr(k_new), ks, _ptr(v_new), vs)
+
+
+def page_pool_struct(page_table, held=None, free_pages=None, n_free=None, page_size: int = 64) -> SnapPagePool:
+    """The handle of a page pool: page_table [n_slots, max_pages], held [n_slots], free_pages [n_pages] and n_free [1], all
+    int32 (for snap_pages_map alone the table does; every page id it holds is then taken as one).  It holds the tensors."""
+    import torch
+    if page_table is None or page_table.dim() != 2:
+        _bad("page_table must be [n_slots, max_pages]")
+    index, slots = page_table.get_device(), int(page_table.shape[0])
+    _want(page_table, "page_table", torch.int32, page_table.shape, index)
+    if (held is None) != (free_pages is None) or (held is None) != (n_free is None):
+        _bad("held, free_pages and n_free come together")
+    pages = 0x7fffffff // max(1, page_size)
+    if held is not None:
+        _want(held, "held", torch.int32, (slots,), index)
+        if free_pages.dim() != 1:
+            _bad("free_pages must be [n_pages]")
+        pages = int(free_pages.shape[0])
+        _want(free_pages, "free_pages", torch.int32, (pages,), index)
+        _want(n_free, "n_free", torch.int32, (1,), index)
+    c = SnapPagePool(_ptr(page_table), _ptr(held), _ptr(free_pages), _ptr(n_free), slots, pages, page_size,
+                     int(page_table.shape[1]))
+    c.tensors, c.index, c.slots_shape, c.i32 = (page_table, held, free_pages, n_free), index, (slots,), torch.int32
+    return c
+
+
+def _pool(pool: SnapPagePool, rows, slot_ids) -> int:
+    """Checks what the page-table calls share; the number of sequences."""
+    if pool is None or slot_ids is None:
+        _bad("pool or slot_ids is None")
+    n = slot_ids.shape[0]
+    _want(slot_ids, "slot_ids", pool.i32, (n,), pool.index)
+    _want(rows, "rows", pool.i32, pool.slots_shape, pool.index)
+    return n
+
+
+def snap_pages_reserve(pool: SnapPagePool, rows, slot_ids, lengths, short_out=None, stream=None):
+    """Pages for lengths (int32 [n], or one number for all) more rows of each sequence; short_out [n]: the pages it lacks."""
+    n, index = _pool(pool, rows, slot_ids), pool.index
+    one = lengths if isinstance(lengths, int) else 0
+    lengths = None if isinstance(lengths, int) else lengths
+    if lengths is not None or one < 0:
+        _want(lengths, "lengths", pool.i32, (n,), index)
+    if short_out is not None:
+        _want(short_out, "short_out", pool.i32, (n,), index)
+    _launch(index, stream, lib().snap_pages_reserve, ctypes.byref(pool), _ptr(rows), n, _ptr(slot_ids), _ptr(lengths), one,
+            _ptr(short_out))
+
+
+def snap_pages_release(pool: SnapPagePool, rows, slot_ids, stream=None):
+    """Hands back the pages behind the rows that each slot holds."""
+    n = _pool(pool, rows, slot_ids)
+    _launch(pool.index, stream, lib().snap_pages_release, ctypes.byref(pool), _ptr(rows), n, _ptr(slot_ids))
+
+
+def snap_pages_map(pool: SnapPagePool, rows, slot_ids, lengths, starts, seq_of, row_of, pos_of, pos=None, stream=None):
+    """The map of a packed batch: starts [n + 1]; each token's sequence, physical row and position (one length)."""
+    n, index = _pool(pool, rows, slot_ids), pool.index
+    _want(lengths, "lengths", pool.i32, (n,), index)
+    if pos is not None:
+        _want(pos, "pos", pool.i32, pool.slots_shape, index)
+    _want(starts, "starts", pool.i32, (n + 1,), index)
+    if seq_of is None or seq_of.dim() != 1:
+        _bad("seq_of must be [tokens]")
+    tokens = seq_of.shape[0]
+    for t, name in ((seq_of, "seq_of"), (row_of, "row_of"), (pos_of, "pos_of")):
+        _want(t, name, pool.i32, (tokens,), index)
+    _launch(index, stream, lib().snap_pages_map, ctypes.byref(pool), _ptr(rows), _ptr(pos), n, _ptr(slot_ids), _ptr(lengths),
+            tokens, _ptr(starts), _ptr(seq_of), _ptr(row_of), _ptr(pos_of))
+
+
+def block_cache_struct(k, v, page_table, block: int, k_scale=None, v_scale=None, k_tail=None, v_tail=None, bound=None,
+                       bound_scale=None) -> SnapBlockCache:
+    """The handle of a block cache: k, v [n_pages, n_kv_heads, page_size, d] int8 (SNAP_INT8), uint8 (E4M3 codes) or
+    bfloat16; scales [n_pages, n_kv_heads, page_size / block], tails [n_slots, n_kv_heads, block, d] (8 bits); bound
+    [n_pages, n_kv_heads, page_size / block, 2, d] int8 with its scale (for select).  It holds the tensors."""
+    import torch
+    if k is None or k.dim() != 4 or k.dtype not in (torch.bfloat16, torch.int8, torch.uint8):
+        _bad("k must be [n_pages, n_kv_heads, page_size, d] bfloat16, int8 or uint8")
+    index, pages, d = k.get_device(), k.shape[:3], int(k.shape[3])
+    _want(k, "k", k.dtype, k.shape, index)
+    _want(v, "v", k.dtype, k.shape, index)
+    if page_table is None or page_table.dim() != 2:
+        _bad("page_table must be [n_slots, max_pages]")
+    _want(page_table, "page_table", torch.int32, page_table.shape, index)
+    if block not in (32, 64, 128) or pages[2] % block:
+        _bad(f"block must be 32, 64 or 128 and divide the pages' {pages[2]} rows (got {block})")
+    slots, each = int(page_table.shape[0]), (pages[0], pages[1], pages[2] // block)
+    for t, name, dtype, shape in ((k_scale, "k_scale", torch.float32, each), (v_scale, "v_scale", torch.float32, each),
+                                  (k_tail, "k_tail", torch.bfloat16, (slots, pages[1], block, d)),
+                                  (v_tail, "v_tail", torch.bfloat16, (slots, pages[1], block, d)),
+                                  (bound, "bound", torch.int8, each + (2, d)),
+                                  (bound_scale, "bound_scale", torch.float32, each)):
+        if t is not None:
+            _want(t, name, dtype, shape, index)
+    c = SnapBlockCache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(k_tail), _ptr(v_tail), _ptr(bound),
+                       _ptr(bound_scale), _ptr(page_table), slots, int(pages[0]), int(pages[2]), int(page_table.shape[1]), block)
+    c.tensors = (k, v, page_table, k_scale, v_scale, k_tail, v_tail, bound, bound_scale)
+    c.index, c.slots_shape, c.i32, c.in_dtype = index, (slots,), torch.int32, torch.bfloat16
+    c.kind = ({torch.bfloat16: SNAP_BF16, torch.uint8: SNAP_FP8_E4M3, torch.int8: SNAP_INT8}[k.dtype], int(pages[1]), d, d)
+    c.rows_max, c.params = c.max_pages * c.page_size, (None, None)
+    return c
+
+
+def snap_block_append(p: Params, cache: SnapBlockCache, rows, slot_ids, k_new, v_new, lengths=None, starts=None,
+                      max_len=None, stream=None):
+    """Stores k_new and v_new (any strides but the last) behind the rows held: [n, n_kv_heads, tokens, d], or with starts
+    [n + 1] a packed batch [tokens, n_kv_heads, d] whose sequences have at most max_len tokens (default: all of them)."""
+    (n, cp), index, heads = _paged(p, cache, rows, None, slot_ids), cache.index, p.n_kv_heads
+    dims = 4 if starts is None else 3
+    if k_new is None or v_new is None or k_new.dim() != dims:
+        _bad("k_new and v_new must be [n, n_kv_heads, tokens, d], or [tokens, n_kv_heads, d] with starts")
+    if starts is None:
+        tokens = k_new.shape[2]
+        shape, longest = (n, heads, tokens, p.d_qk), tokens
+        if max_len is not None:
+            _bad("max_len goes with starts")
+    else:
+        tokens = k_new.shape[0]
+        shape, longest = (tokens, heads, p.d_qk), tokens if max_len is None else max_len
+        _want(starts, "starts", cache.i32, (n + 1,), index)
+        if lengths is not None:
+            _bad("a packed batch (starts) takes no lengths")
+    ks, vs = (_strides(x, name, cache.in_dtype, shape, index) for x, name in ((k_new, "k_new"), (v_new, "v_new")))
+    if starts is not None:
+        ks, vs = (_i64x3(0, x[1], x[0]) for x in (ks, vs))
+    if lengths is not None:
+        _want(lengths, "lengths", cache.i32, (n,), index)
+    if n == 0 or tokens == 0:
+        return
+    _launch(index, stream, lib().snap_block_append, cp, ctypes.byref(cache), _ptr(rows), n, _ptr(slot_ids), _ptr(lengths),
+            _ptr(starts), tokens, longest, _ptr(k_new), ks, _ptr(v_new), vs)
+
+
+def snap_block_chosen(p: Params, block: int) -> int:
+    return int(lib().snap_block_chosen(ctypes.byref(p.c()), block))
+
+
+def snap_block_decode_workspace(p: Params, n: int, max_rows: int, block: int, select: bool = False) -> int:
+    return int(lib().snap_block_decode_workspace(ctypes.byref(p.c()), n, max_rows, block, int(select)))
+
+
+def _block_io(p: Params, cache: SnapBlockCache, n: int, q, out, select, sel_out) -> int:
+    if sel_out is not None:
+        if not select:
+            _bad("sel_out goes with select")
+        _want(sel_out, "sel_out", cache.i32, (n, p.n_kv_heads, snap_block_chosen(p, cache.block)), cache.index)
+    return _paged_io(p, cache, n, q, out)
+
+
+def snap_block_decode_attn(p: Params, cache: SnapBlockCache, rows, slot_ids, q, out, workspace, max_rows=None,
+                           select: bool = False, sel_out=None, stream=None):
+    """Attention of one new token per sequence (stored already) over every block, or those that are selected."""
+    (n, cp), index = _paged(p, cache, rows, None, slot_ids), cache.index
+    od = _block_io(p, cache, n, q, out, select, sel_out)
+    _launch(index, stream, lib().snap_block_decode_attn, cp, ctypes.byref(cache), _ptr(rows), n, _ptr(slot_ids),
+            cache.rows_max if max_rows is None else max_rows, _ptr(q), _ptr(out), od, int(select), _ptr(sel_out),
+            _ptr(workspace), _bytes(workspace, index))
+
+
+def snap_block_decode_step(p: Params, cache: SnapBlockCache, rows, slot_ids, q, k_new, v_new, out, workspace, max_rows=None,
+                           select: bool = False, sel_out=None, stream=None):
+    """Stores one token per sequence (k_new [n, n_kv_heads, 1, d], or without the 1) and attends."""
+    (n, cp), index = _paged(p, cache, rows, None, slot_ids), cache.index
+    od = _block_io(p, cache, n, q, out, select, sel_out)
+    heads = (n, p.n_kv_heads) if k_new is not None and k_new.dim() == 3 else (n, p.n_kv_heads, 1)
+    _want(k_new, "k_new", cache.in_dtype, heads + (p.d_qk,), index)
+    _want(v_new, "v_new", cache.in_dtype, heads + (p.d_v,), index)
+    _launch(index, stream, lib().snap_block_decode_step, cp, ctypes.byref(cache), _ptr(rows), n, _ptr(slot_ids),
+            cache.rows_max if max_rows is None else max_rows, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), od, int(select),
+            _ptr(sel_out), _ptr(workspace), _bytes(workspace, index))
 
 
 def snap_debug_checks(reset: bool = True) -> int:

@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsnapstream.so")
 DEBUG_LIB = os.path.join(HERE, "libsnapstream_debug.so")
 SOURCES = ["abi.hip", "compress.hip", "decode.hip", "prefill.hip", "noalloc.hip",
-           "rope.hip", "paged.hip", "evict.hip"]
+           "rope.hip", "paged.hip", "evict.hip", "pages.hip", "blocks.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 

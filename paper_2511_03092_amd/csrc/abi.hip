@@ -36,6 +36,8 @@ static bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 // Largest second launch-grid dimension (workgroups along y): per-(sequence,
 // KV head) and per-(sequence, query head) grids must fit it.
 constexpr int kMaxGridY = 65535;
+// Sequences of one call of the page-table operators.
+constexpr int kMaxSequences = 1 << 20;
 
 // Parameter checks shared by every call.
 static snap_status check_params(const snap_params* p) {
@@ -188,6 +190,82 @@ static snap_status check_paged_decode(const snap_params* p, const snap_paged_cac
   const size_t need = paged_geometry(*p, n, max_rows, weigh != 0).bytes;
   if (!workspace || ((uintptr_t)workspace & 255u) || ws_bytes < need)
     return fail(SNAP_ERR_WORKSPACE, "workspace needs %zu bytes, 256-byte aligned (got %zu)", need, ws_bytes);
+  return SNAP_OK;
+}
+
+// Checks of the parameters and the cache that the block calls share.
+static snap_status check_block(const snap_params* p, const snap_block_cache* c) {
+  if (!p) return fail(SNAP_ERR_INVALID_ARG, "params is NULL");
+  snap_params as = *p;
+  if (as.kv_dtype == SNAP_INT8) as.kv_dtype = SNAP_FP8_E4M3;  // (the other calls have no such cache)
+  snap_status st = check_params(&as);
+  if (st != SNAP_OK) return st;
+  if (p->fp8_qk) return fail(SNAP_ERR_UNSUPPORTED, "the block cache has no fp8 query products (fp8_qk)");
+  if (p->in_dtype != SNAP_BF16) return fail(SNAP_ERR_UNSUPPORTED, "the block cache takes bf16 inputs");
+  if (p->v_in_k || p->d_qk != p->d_v) return fail(SNAP_ERR_UNSUPPORTED, "the block cache holds 64- or 128-wide keys and values");
+  if (!c) return fail(SNAP_ERR_INVALID_ARG, "cache is NULL");
+  if (c->n_slots < 1 || c->n_pages < 1 || c->max_pages < 1)
+    return fail(SNAP_ERR_INVALID_ARG, "cache n_slots, n_pages and max_pages must be >= 1 (got %d, %d, %d)", c->n_slots,
+                c->n_pages, c->max_pages);
+  if (c->block != 32 && c->block != 64 && c->block != 128)
+    return fail(SNAP_ERR_UNSUPPORTED, "block must be 32, 64 or 128 (got %d)", c->block);
+  if (c->page_size < c->block || c->page_size > 4096 || (c->page_size & (c->page_size - 1)))
+    return fail(SNAP_ERR_UNSUPPORTED, "page_size must be a power of two in [block, 4096] (got %d)", c->page_size);
+  if ((long long)c->max_pages * c->page_size > (1 << 28))
+    return fail(SNAP_ERR_INVALID_ARG, "max_pages * page_size exceeds 2^28 rows");
+  if ((long long)c->n_pages * (c->page_size / c->block) * p->n_kv_heads > 0x7fffffffll)
+    return fail(SNAP_ERR_UNSUPPORTED, "the cache has more than 2^31 - 1 blocks of all KV heads");
+  if (!c->page_table) return fail(SNAP_ERR_INVALID_ARG, "cache page_table is NULL");
+  if (!c->k || !aligned16(c->k) || !c->v || !aligned16(c->v))
+    return fail(SNAP_ERR_INVALID_ARG, "cache k or v is NULL or not 16-byte aligned");
+  if (p->kv_dtype != SNAP_BF16) {
+    if (!c->k_scale || !c->v_scale) return fail(SNAP_ERR_INVALID_ARG, "an 8-bit cache needs k_scale and v_scale");
+    if (!c->k_tail || !aligned16(c->k_tail) || !c->v_tail || !aligned16(c->v_tail))
+      return fail(SNAP_ERR_INVALID_ARG, "an 8-bit cache needs k_tail and v_tail, 16-byte aligned");
+  }
+  if (!c->bound != !c->bound_scale || !aligned16(c->bound))
+    return fail(SNAP_ERR_INVALID_ARG, "bound and bound_scale come together, bound 16-byte aligned");
+  return SNAP_OK;
+}
+
+// Checks of snap_block_decode_attn and, but for the new token, of
+// snap_block_decode_step (n > 0).
+static snap_status check_block_decode(const snap_params* p, const snap_block_cache* c, const int32_t* rows, int32_t n,
+                                      const int32_t* slot_ids, int32_t max_rows, const void* q, void* out,
+                                      int32_t out_dtype, int32_t select, void* workspace, size_t ws_bytes) {
+  if (max_rows < 1 || (long long)max_rows > (long long)c->max_pages * c->page_size)
+    return fail(SNAP_ERR_INVALID_ARG, "max_rows must be in [1, max_pages * page_size = %lld] (got %d)",
+                (long long)c->max_pages * c->page_size, max_rows);
+  if ((long long)n * p->n_q_heads > kMaxGridY)
+    return fail(SNAP_ERR_UNSUPPORTED, "n * n_q_heads must be at most %d", kMaxGridY);
+  if (!rows || !slot_ids) return fail(SNAP_ERR_INVALID_ARG, "rows/slot_ids NULL");
+  if (!q || !aligned16(q)) return fail(SNAP_ERR_INVALID_ARG, "q is NULL or not 16-byte aligned");
+  if (!out || !aligned16(out)) return fail(SNAP_ERR_INVALID_ARG, "out is NULL or not 16-byte aligned");
+  if (out_dtype != SNAP_F32 && out_dtype != SNAP_BF16) return fail(SNAP_ERR_INVALID_ARG, "out_dtype must be F32 or BF16");
+  if (select != 0 && select != 1) return fail(SNAP_ERR_INVALID_ARG, "select must be 0 or 1");
+  if (select && !c->bound) return fail(SNAP_ERR_INVALID_ARG, "select needs the cache's bound and bound_scale");
+  if (select && max_rows / c->block > kBlockMost)
+    return fail(SNAP_ERR_UNSUPPORTED, "select takes at most %d blocks of a sequence (got %d)", kBlockMost, max_rows / c->block);
+  const size_t need = block_geometry(*p, n, max_rows, c->block, select != 0).bytes;
+  if (!workspace || ((uintptr_t)workspace & 255u) || ws_bytes < need)
+    return fail(SNAP_ERR_WORKSPACE, "workspace needs %zu bytes, 256-byte aligned (got %zu)", need, ws_bytes);
+  return SNAP_OK;
+}
+
+static snap_status check_pool(const snap_page_pool* c, bool counts) {
+  if (!c) return fail(SNAP_ERR_INVALID_ARG, "pool is NULL");
+  if (c->n_slots < 1 || c->n_pages < 1 || c->max_pages < 1)
+    return fail(SNAP_ERR_INVALID_ARG, "pool n_slots, n_pages and max_pages must be >= 1 (got %d, %d, %d)", c->n_slots,
+                c->n_pages, c->max_pages);
+  if (c->page_size < 16 || c->page_size > 4096 || (c->page_size & (c->page_size - 1)))
+    return fail(SNAP_ERR_UNSUPPORTED, "page_size must be a power of two in [16, 4096] (got %d)", c->page_size);
+  if ((long long)c->max_pages * c->page_size > (1 << 28))
+    return fail(SNAP_ERR_INVALID_ARG, "max_pages * page_size exceeds 2^28 rows");
+  if ((long long)c->n_pages * c->page_size > 0x7fffffffll)
+    return fail(SNAP_ERR_UNSUPPORTED, "n_pages * page_size must be below 2^31");
+  if (!c->page_table) return fail(SNAP_ERR_INVALID_ARG, "pool page_table is NULL");
+  if (counts && (!c->held || !c->free_pages || !c->n_free))
+    return fail(SNAP_ERR_INVALID_ARG, "pool held, free_pages or n_free is NULL");
   return SNAP_OK;
 }
 
@@ -556,6 +634,159 @@ snap_status snap_paged_evict(const snap_params* p, const snap_paged_cache* cache
   return st;
 }
 
+snap_status snap_paged_append_mapped(const snap_params* p, const snap_paged_cache* cache, int32_t n,
+                                     const int32_t* slot_ids, int32_t tokens, const int32_t* seq_of,
+                                     const int32_t* row_of, const int32_t* pos_of, const void* k_new,
+                                     const int64_t* k_stride, const void* v_new, const int64_t* v_stride,
+                                     void* stream) {
+  g_err[0] = 0;
+  snap_status st = check_params(p);
+  if (st != SNAP_OK) return st;
+  if ((st = check_paged(p, cache)) != SNAP_OK) return st;
+  if (n < 0 || tokens < 0) return fail(SNAP_ERR_INVALID_ARG, "n and tokens must be >= 0");
+  if (n == 0 || tokens == 0) return SNAP_OK;
+  if (tokens > (1 << 28)) return fail(SNAP_ERR_INVALID_ARG, "tokens must be at most 2^28");
+  if (p->n_kv_heads > kMaxGridY) return fail(SNAP_ERR_UNSUPPORTED, "n_kv_heads must be at most %d", kMaxGridY);
+  if ((long long)cache->n_pages * cache->page_size > 0x7fffffffll)
+    return fail(SNAP_ERR_UNSUPPORTED, "n_pages * page_size must be below 2^31");
+  if (!slot_ids || !seq_of || !row_of) return fail(SNAP_ERR_INVALID_ARG, "slot_ids/seq_of/row_of NULL");
+  if (cache->token && !pos_of) return fail(SNAP_ERR_INVALID_ARG, "a cache with a token array needs pos_of");
+  if (!k_new || !aligned16(k_new)) return fail(SNAP_ERR_INVALID_ARG, "k_new is NULL or not 16-byte aligned");
+  if (!p->v_in_k && (!v_new || !aligned16(v_new)))
+    return fail(SNAP_ERR_INVALID_ARG, "v_new is NULL or not 16-byte aligned");
+  const int per16 = p->in_dtype == SNAP_F32 ? 4 : 8;
+  const int32_t size[2] = {tokens, p->n_kv_heads};
+  for (int i = 0; i < 2; ++i)
+    if (size[i] > 1 && ((k_stride && k_stride[i] % per16) || (!p->v_in_k && v_stride && v_stride[i] % per16)))
+      return fail(SNAP_ERR_INVALID_ARG, "strides of k_new / v_new must be multiples of 16 bytes");
+  st = launch_paged_append_mapped(*p, *cache, n, slot_ids, tokens, seq_of, row_of, pos_of, k_new, k_stride, v_new,
+                                  v_stride, (hipStream_t)stream);
+  if (st == SNAP_ERR_HIP) set_error("kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+  return st;
+}
+
+snap_status snap_pages_reserve(const snap_page_pool* pool, const int32_t* rows, int32_t n, const int32_t* slot_ids,
+                               const int32_t* lengths, int32_t len, int32_t* short_out, void* stream) {
+  g_err[0] = 0;
+  snap_status st = check_pool(pool, true);
+  if (st != SNAP_OK) return st;
+  if (n < 0 || n > kMaxSequences) return fail(SNAP_ERR_INVALID_ARG, "n must be in [0, %d]", kMaxSequences);
+  if (!lengths && len < 0) return fail(SNAP_ERR_INVALID_ARG, "len must be >= 0");
+  if (n == 0) return SNAP_OK;
+  if (!rows || !slot_ids) return fail(SNAP_ERR_INVALID_ARG, "rows/slot_ids NULL");
+  st = launch_pages_reserve(*pool, rows, n, slot_ids, lengths, len, short_out, (hipStream_t)stream);
+  if (st == SNAP_ERR_HIP) set_error("kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+  return st;
+}
+
+snap_status snap_pages_release(const snap_page_pool* pool, const int32_t* rows, int32_t n, const int32_t* slot_ids,
+                               void* stream) {
+  g_err[0] = 0;
+  snap_status st = check_pool(pool, true);
+  if (st != SNAP_OK) return st;
+  if (n < 0 || n > kMaxSequences) return fail(SNAP_ERR_INVALID_ARG, "n must be in [0, %d]", kMaxSequences);
+  if (n == 0) return SNAP_OK;
+  if (!rows || !slot_ids) return fail(SNAP_ERR_INVALID_ARG, "rows/slot_ids NULL");
+  st = launch_pages_release(*pool, rows, n, slot_ids, (hipStream_t)stream);
+  if (st == SNAP_ERR_HIP) set_error("kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+  return st;
+}
+
+snap_status snap_pages_map(const snap_page_pool* pool, const int32_t* rows, const int32_t* pos, int32_t n,
+                           const int32_t* slot_ids, const int32_t* lengths, int32_t tokens, int32_t* starts,
+                           int32_t* seq_of, int32_t* row_of, int32_t* pos_of, void* stream) {
+  g_err[0] = 0;
+  snap_status st = check_pool(pool, false);
+  if (st != SNAP_OK) return st;
+  if (n < 0 || n > kMaxSequences) return fail(SNAP_ERR_INVALID_ARG, "n must be in [0, %d]", kMaxSequences);
+  if (tokens < 0 || tokens > (1 << 28)) return fail(SNAP_ERR_INVALID_ARG, "tokens must be in [0, 2^28]");
+  if (n > 0 && (!rows || !slot_ids || !lengths)) return fail(SNAP_ERR_INVALID_ARG, "rows/slot_ids/lengths NULL");
+  if (!starts || (tokens > 0 && (!seq_of || !row_of || !pos_of)))
+    return fail(SNAP_ERR_INVALID_ARG, "starts/seq_of/row_of/pos_of NULL");
+  st = launch_pages_map(*pool, rows, pos, n, slot_ids, lengths, tokens, starts, seq_of, row_of, pos_of,
+                        (hipStream_t)stream);
+  if (st == SNAP_ERR_HIP) set_error("kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+  return st;
+}
+
+snap_status snap_block_append(const snap_params* p, const snap_block_cache* cache, const int32_t* rows, int32_t n,
+                              const int32_t* slot_ids, const int32_t* lengths, const int32_t* starts, int32_t tokens,
+                              int32_t max_len, const void* k_new, const int64_t* k_stride, const void* v_new,
+                              const int64_t* v_stride, void* stream) {
+  g_err[0] = 0;
+  snap_status st = check_block(p, cache);
+  if (st != SNAP_OK) return st;
+  if (n < 0) return fail(SNAP_ERR_INVALID_ARG, "n must be >= 0");
+  if (n == 0) return SNAP_OK;
+  if (max_len < 1 || max_len > (1 << 28)) return fail(SNAP_ERR_INVALID_ARG, "max_len must be in [1, 2^28]");
+  if ((long long)n * p->n_kv_heads > kMaxGridY)
+    return fail(SNAP_ERR_UNSUPPORTED, "n * n_kv_heads must be at most %d", kMaxGridY);
+  if (!rows || !slot_ids) return fail(SNAP_ERR_INVALID_ARG, "rows/slot_ids NULL");
+  if (starts && lengths) return fail(SNAP_ERR_INVALID_ARG, "a packed batch (starts) takes no lengths");
+  if (starts && tokens < 0) return fail(SNAP_ERR_INVALID_ARG, "tokens must be >= 0");
+  if (!k_new || !aligned16(k_new)) return fail(SNAP_ERR_INVALID_ARG, "k_new is NULL or not 16-byte aligned");
+  if (!v_new || !aligned16(v_new)) return fail(SNAP_ERR_INVALID_ARG, "v_new is NULL or not 16-byte aligned");
+  const int32_t size[3] = {starts ? 1 : n, p->n_kv_heads, starts ? tokens : max_len};
+  for (int i = 0; i < 3; ++i)
+    if (size[i] > 1 && ((k_stride && k_stride[i] % 8) || (v_stride && v_stride[i] % 8)))
+      return fail(SNAP_ERR_INVALID_ARG, "strides of k_new / v_new must be multiples of 16 bytes");
+  st = launch_block_append(*p, *cache, rows, n, slot_ids, lengths, starts, tokens, max_len, k_new, k_stride, v_new,
+                           v_stride, (hipStream_t)stream);
+  if (st == SNAP_ERR_HIP) set_error("kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+  return st;
+}
+
+int32_t snap_block_chosen(const snap_params* p, int32_t block) {
+  if (!p || (block != 32 && block != 64 && block != 128)) return 0;
+  if (p->sink < 0 || p->recent < 1 || p->topk < 0 || (long long)p->sink + p->recent + p->topk > (1 << 24)) return 0;
+  return block_chosen(*p, block);
+}
+
+size_t snap_block_decode_workspace(const snap_params* p, int32_t n, int32_t max_rows, int32_t block, int32_t select) {
+  if (!p || n < 0 || max_rows < 1 || max_rows > (1 << 28) || (block != 32 && block != 64 && block != 128)) return 0;
+  snap_params as = *p;
+  if (as.kv_dtype == SNAP_INT8) as.kv_dtype = SNAP_FP8_E4M3;
+  if (check_params(&as) != SNAP_OK || p->d_qk != p->d_v) return 0;
+  if ((long long)n * p->n_q_heads > kMaxGridY) return 0;
+  return block_geometry(*p, n, max_rows, block, select != 0).bytes;
+}
+
+snap_status snap_block_decode_attn(const snap_params* p, const snap_block_cache* cache, const int32_t* rows, int32_t n,
+                                   const int32_t* slot_ids, int32_t max_rows, const void* q, void* out,
+                                   int32_t out_dtype, int32_t select, int32_t* sel_out, void* workspace,
+                                   size_t ws_bytes, void* stream) {
+  g_err[0] = 0;
+  snap_status st = check_block(p, cache);
+  if (st != SNAP_OK) return st;
+  if (n < 0) return fail(SNAP_ERR_INVALID_ARG, "n must be >= 0");
+  if (n == 0) return SNAP_OK;
+  st = check_block_decode(p, cache, rows, n, slot_ids, max_rows, q, out, out_dtype, select, workspace, ws_bytes);
+  if (st != SNAP_OK) return st;
+  st = launch_block_decode(*p, *cache, rows, n, slot_ids, max_rows, q, nullptr, nullptr, out, out_dtype, select != 0,
+                           sel_out, workspace, (hipStream_t)stream);
+  if (st == SNAP_ERR_HIP) set_error("kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+  return st;
+}
+
+snap_status snap_block_decode_step(const snap_params* p, const snap_block_cache* cache, const int32_t* rows, int32_t n,
+                                   const int32_t* slot_ids, int32_t max_rows, const void* q, const void* k_new,
+                                   const void* v_new, void* out, int32_t out_dtype, int32_t select, int32_t* sel_out,
+                                   void* workspace, size_t ws_bytes, void* stream) {
+  g_err[0] = 0;
+  snap_status st = check_block(p, cache);
+  if (st != SNAP_OK) return st;
+  if (n < 0) return fail(SNAP_ERR_INVALID_ARG, "n must be >= 0");
+  if (n == 0) return SNAP_OK;
+  st = check_block_decode(p, cache, rows, n, slot_ids, max_rows, q, out, out_dtype, select, workspace, ws_bytes);
+  if (st != SNAP_OK) return st;
+  if (!k_new || !aligned16(k_new)) return fail(SNAP_ERR_INVALID_ARG, "k_new is NULL or not 16-byte aligned");
+  if (!v_new || !aligned16(v_new)) return fail(SNAP_ERR_INVALID_ARG, "v_new is NULL or not 16-byte aligned");
+  st = launch_block_decode(*p, *cache, rows, n, slot_ids, max_rows, q, k_new, v_new, out, out_dtype, select != 0,
+                           sel_out, workspace, (hipStream_t)stream);
+  if (st == SNAP_ERR_HIP) set_error("kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+  return st;
+}
+
 snap_status snap_debug_checks(uint32_t* flags, int32_t reset) {
   g_err[0] = 0;
   if (!flags) return fail(SNAP_ERR_INVALID_ARG, "flags is NULL");
@@ -564,10 +795,11 @@ snap_status snap_debug_checks(uint32_t* flags, int32_t reset) {
   if (hipDeviceSynchronize() != hipSuccess) return fail(SNAP_ERR_HIP, "hipDeviceSynchronize failed");
   const uint32_t c = debug_flags_compress(reset != 0), d = debug_flags_decode(reset != 0),
                  f = debug_flags_prefill(reset != 0), g = debug_flags_paged(reset != 0),
-                 e = debug_flags_evict(reset != 0);
-  if (c == 0xffffffffu || d == 0xffffffffu || f == 0xffffffffu || g == 0xffffffffu || e == 0xffffffffu)
+                 e = debug_flags_evict(reset != 0), h = debug_flags_blocks(reset != 0);
+  if (c == 0xffffffffu || d == 0xffffffffu || f == 0xffffffffu || g == 0xffffffffu || e == 0xffffffffu ||
+      h == 0xffffffffu)
     return fail(SNAP_ERR_HIP, "reading the check words failed");
-  *flags = c | d | f | g | e;
+  *flags = c | d | f | g | e | h;
   return SNAP_OK;
 #else
   (void)reset;

@@ -1,0 +1,823 @@
+// blocks.hip -- the block cache: rows in blocks of 32, 64 or 128 tokens, in 8 bits with
+// a scale for each block and KV head, or in bf16, and attention of one new token over
+// all of them or over those that a score selects.
+//
+//   block_append  a wave for each block of new keys or values
+//   block_select  one workgroup for each (sequence, KV head): the blocks' scores from
+//                 their bounds, and the best of them
+//   block_attn    one wave for each work item: a share of a unit's blocks, or the
+//                 newest token's own block (with the token stored)
+//   block_join    the items of a (sequence, query head) -> out
+#include <math.h>
+
+#include "snap_internal.h"
+
+namespace snap {
+
+namespace {
+
+enum { kRowsBf16 = 0, kRowsFp8 = 1, kRowsInt8 = 2 };
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
+struct BlockArgs {
+  const void* q;  // [n][Hq][d]
+  unsigned char* ck;
+  unsigned char* cv;
+  float* ks;
+  float* vs;
+  unsigned char* kt;
+  unsigned char* vt;
+  int8_t* bound;
+  float* bscale;
+  const int32_t* rows;
+  const int32_t* slot_ids;
+  const int32_t* table;
+  float* part;     // [items][G][d]
+  float2* ml;      // [items][G]  (max in log2 units, sum)
+  int32_t* list;   // [units][list_ld] selected blocks, ascending; NULL: all
+  int32_t* count;  // [units]
+  int32_t* sel_out;
+  void* out;
+  const void* k_new;  // a step's token, [n][Hkv][d]; NULL: the launch only attends
+  const void* v_new;
+  int n, Hq, Hkv, G, n_slots, n_pages, page_shift, block_shift, max_pages, max_rows, per_unit, chosen, list_ld, out_bf16;
+  int sink, recent, best;  // selection: rows, rows, blocks
+  float scale2, scale2_lo;
+};
+
+// One sequence of a call: the row of its newest token, its whole blocks before that
+// one's, and whether that one's is attended.
+struct BlockSeq {
+  int slot, row, blocks;
+  bool tail;
+};
+__device__ __forceinline__ BlockSeq block_seq(const BlockArgs& a, int b) {
+  BlockSeq s;
+  s.slot = a.slot_ids[b];
+  const bool ok = s.slot >= 0 && s.slot < a.n_slots;
+  s.row = ok ? a.rows[s.slot] : -1;
+  s.row = uniform(s.row);
+  s.slot = uniform(s.slot);
+  if (!ok) s.row = -1;
+  s.tail = s.row >= 0 && s.row < a.max_rows;
+  s.blocks = s.row < 0 ? 0 : (s.tail ? s.row : a.max_rows) >> a.block_shift;
+  return s;
+}
+
+// Index of a block of (slot, KV head g) among the blocks of all pages, or -1 when its
+// page is not there.
+__device__ __forceinline__ int block_at(const BlockArgs& a, int slot, int g, int block) {
+  const int per = a.page_shift - a.block_shift, p = block >> per;
+  if (p >= a.max_pages) return -1;
+  const int page = a.table[(size_t)slot * a.max_pages + p];
+  if (page < 0 || page >= a.n_pages) return -1;
+  return (int)((((int64_t)page * a.Hkv + g) << per) + (block & ((1 << per) - 1)));
+}
+
+// ---------------------------------------------------------------- codes
+constexpr float kLeastScale = 0x1p-126f;
+__device__ __forceinline__ float block_scale(uint32_t amax_bf16, float top) {
+  const float s = bf16_bits_to_f32(amax_bf16) / top;
+  return amax_bf16 == 0 ? 1.f : fmaxf(s, kLeastScale);
+}
+
+// Four values over a scale as int8 codes (NaN: 0, by its bits: the build lets float
+// compares assume none).
+__device__ __forceinline__ uint32_t int8x4(const float* x, float scale) {
+  uint32_t w = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float y = fminf(fmaxf(__builtin_rintf(x[i] / scale), -127.f), 127.f);
+    const uint32_t c = (__float_as_uint(x[i]) & 0x7fffffffu) > 0x7f800000u ? 0u : (uint32_t)(int)y & 0xffu;
+    w |= c << (8 * i);
+  }
+  return w;
+}
+
+// 8 bf16 -> 8 codes
+template <int KIND>
+__device__ __forceinline__ u32x2 codes8(u32x4 raw, float scale) {
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = bf16_bits_to_f32(raw[i] & 0xffffu);
+    f[2 * i + 1] = bf16_bits_to_f32(raw[i] >> 16);
+  }
+  if constexpr (KIND == kRowsInt8) {
+    return u32x2{int8x4(f, scale), int8x4(f + 4, scale)};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] /= scale;
+    return u32x2{e4m3x4_hw(f[0], f[1], f[2], f[3]), e4m3x4_hw(f[4], f[5], f[6], f[7])};
+  }
+}
+
+// Largest finite magnitude of bf16 pieces, as bits.
+__device__ __forceinline__ uint32_t amax8(u32x4 x, uint32_t m) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t lo = x[i] & 0x7fffu, hi = (x[i] >> 16) & 0x7fffu;
+    m = max(m, lo < 0x7f80u ? lo : 0u);
+    m = max(m, hi < 0x7f80u ? hi : 0u);
+  }
+  return m;
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t m) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
+  return m;
+}
+
+// bf16 in an order of whole numbers (and back: its own inverse)
+__device__ __forceinline__ int in_order(int h) { return (short)h < 0 ? (short)(h ^ 0x7fff) : (short)h; }
+struct Bounds8 {
+  int lo[8], hi[8];
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      lo[i] = 0x7fff;
+      hi[i] = -0x8000;
+    }
+  }
+  __device__ __forceinline__ void add(u32x4 x) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t h = (x[i >> 1] >> (16 * (i & 1))) & 0xffffu;
+      const int k = in_order((int)h);
+      const bool nan = (h & 0x7fffu) > 0x7f80u;
+      lo[i] = nan ? lo[i] : min(lo[i], k);
+      hi[i] = nan ? hi[i] : max(hi[i], k);
+    }
+  }
+  __device__ __forceinline__ void join(int from) {  // with lane ^ from
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      lo[i] = min(lo[i], __shfl_xor(lo[i], from));
+      hi[i] = max(hi[i], __shfl_xor(hi[i], from));
+    }
+  }
+  // codes outwards, 8 bytes each
+  __device__ __forceinline__ void codes(float scale, u32x2& least, u32x2& largest) const {
+    least = largest = u32x2{0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const bool none = lo[i] > hi[i];
+      const float l = bf16_bits_to_f32((uint32_t)in_order(lo[i]) & 0xffffu) / scale;
+      const float h = bf16_bits_to_f32((uint32_t)in_order(hi[i]) & 0xffffu) / scale;
+      const int cl = none ? 0 : (int)fminf(fmaxf(__builtin_floorf(l), -127.f), 127.f);
+      const int ch = none ? 0 : (int)fminf(fmaxf(__builtin_ceilf(h), -127.f), 127.f);
+      least[i >> 2] |= ((uint32_t)cl & 0xffu) << (8 * (i & 3));
+      largest[i >> 2] |= ((uint32_t)ch & 0xffu) << (8 * (i & 3));
+    }
+  }
+};
+
+// A whole block's codes, scale and bounds written by one wave, from the rows that
+// row(r) points to (bf16, read twice).  keys: it is the keys' side.
+template <int D, int KIND, typename Row>
+__device__ __forceinline__ void put_block(const BlockArgs& a, int at, bool keys, Row row) {
+  constexpr int P = D / 8, R = 64 / P;  // pieces of a row, rows a wave takes at once
+  const int lane = tid() & 63, col = lane % P, r0 = lane / P, B = 1 << a.block_shift;
+  const bool bounds = keys && a.bound;
+  if (KIND == kRowsBf16 && !bounds) return;
+  uint32_t m = 0;
+  Bounds8 bd;
+  bd.init();
+  for (int r = r0; r < B; r += R) {
+    const u32x4 x = *((const u32x4*)row(r) + col);
+    m = amax8(x, m);
+    if (bounds) bd.add(x);
+  }
+  m = wave_max(m);
+  if constexpr (KIND != kRowsBf16) {
+    const float s = block_scale(m, KIND == kRowsInt8 ? 127.f : 448.f);
+    unsigned char* to = (keys ? a.ck : a.cv) + ((size_t)at << a.block_shift) * D + 8 * col;
+    for (int r = r0; r < B; r += R) *(u32x2*)(to + (size_t)r * D) = codes8<KIND>(*((const u32x4*)row(r) + col), s);
+    if (lane == 0) (keys ? a.ks : a.vs)[at] = s;
+  }
+  if (bounds) {
+#pragma unroll
+    for (int o = P; o < 64; o <<= 1) bd.join(o);
+    const float s = block_scale(m, 127.f);
+    u32x2 least, largest;
+    bd.codes(s, least, largest);
+    if (lane < P) {
+      *(u32x2*)(a.bound + (size_t)at * 2 * D + 8 * col) = least;
+      *(u32x2*)(a.bound + (size_t)at * 2 * D + D + 8 * col) = largest;
+    }
+    if (lane == 0) a.bscale[at] = s;
+  }
+}
+
+// ---------------------------------------------------------------- append
+struct BlockAppend {
+  BlockArgs c;
+  const int32_t* lengths;
+  const int32_t* starts;
+  int64_t ks[3], vs[3];  // bytes
+  int tokens, max_len;
+};
+
+// Wave w of workgroup x takes block 2 x + w / 2 of the sequence's new ones, keys (w even)
+// or values.  The wave of the first block, which may read the tail's old rows, writes the
+// last one's afterwards, so that no other wave's writes meet those reads.
+template <int D, int KIND>
+__global__ __launch_bounds__(256) void block_append(BlockAppend p) {
+  const BlockArgs& a = p.c;
+  constexpr int P = D / 8, R = 64 / P;
+  const int w = uniform(tid() >> 6), lane = tid() & 63, col = lane % P, r0 = lane / P;
+  const int g = bid_y(), b = __builtin_amdgcn_workgroup_id_z(), j = 2 * bid_x() + (w >> 1), B = 1 << a.block_shift;
+  const bool keys = !(w & 1);
+  const int slot = uniform(a.slot_ids[b]);
+  if (slot < 0 || slot >= a.n_slots) return;
+  const int row0 = uniform(a.rows[slot]);
+  if (row0 < 0) return;
+  int len, t0 = 0;
+  if (p.starts) {
+    t0 = min(max(uniform(p.starts[b]), 0), p.tokens);
+    len = min(max(uniform(p.starts[b + 1]), 0), p.tokens) - t0;
+  } else {
+    len = p.lengths ? uniform(p.lengths[b]) : p.max_len;
+  }
+  len = min(len, p.max_len);
+  const int64_t room = ((int64_t)a.max_pages << a.page_shift) - row0;
+  if (len > room) len = room < 0 ? 0 : (int)room;
+  if (len <= 0) return;
+  const int first = row0 >> a.block_shift, skip = row0 & (B - 1), last = (skip + len - 1) >> a.block_shift;
+  if (j > last) return;
+  const int64_t* st = keys ? p.ks : p.vs;
+  const unsigned char* in = (const unsigned char*)(keys ? a.k_new : a.v_new) + (p.starts ? 0 : b * st[0]) + g * st[1];
+  unsigned char* tail = KIND == kRowsBf16 ? nullptr : (keys ? a.kt : a.vt) + ((((size_t)slot * a.Hkv + g) << a.block_shift) * D) * 2;
+  // rows [from, upto) of block i come from the input
+  auto block = [&](int i) {
+    const int at = uniform(block_at(a, slot, g, first + i));
+    if (at < 0) return;
+    const int from = i ? 0 : skip, upto = min(B, skip + len - i * B);
+    unsigned char* old = KIND == kRowsBf16 ? (keys ? a.ck : a.cv) + ((size_t)at << a.block_shift) * D * 2 : tail;
+    auto row = [&](int r) -> const unsigned char* {
+      return r < from ? old + (size_t)r * D * 2 : in + (t0 + (int64_t)i * B + r - skip) * st[2];
+    };
+    if (upto == B && i == j) put_block<D, KIND>(a, at, keys, row);
+    if (KIND == kRowsBf16 || i == last)
+      for (int r = r0; r < upto; r += R)
+        if (r >= from) *((u32x4*)(old + (size_t)r * D * 2) + col) = *((const u32x4*)row(r) + col);
+  };
+  if (KIND == kRowsBf16) {
+    block(j);
+  } else {
+    if (j != last || j == 0) block(j);
+    else if (skip + len == (last + 1) * B) {  // a whole last block: its codes here, its tail rows by the first block's wave
+      const int at = uniform(block_at(a, slot, g, first + j));
+      if (at >= 0) put_block<D, KIND>(a, at, keys, [&](int r) { return in + (t0 + (int64_t)j * B + r - skip) * st[2]; });
+    }
+    if (j == 0 && last > 0) block(last);
+  }
+}
+
+// ---------------------------------------------------------------- selection
+constexpr int kSelThreadsB = 1024, kSelWaves = kSelThreadsB / 64;
+constexpr uint32_t kForced = 0xffffffffu;  // above every score's key; 0, below them: no such block
+
+// A score's bits in the order of whole numbers, within [1, kForced - 1].
+__device__ __forceinline__ uint32_t score_key(float s) {
+  const uint32_t u = __float_as_uint(s + 0.f);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// The scores are products of 8-bit whole numbers on the matrix units, exact in 32 bits,
+// so that the choice does not depend on the order of sums.
+template <int D>
+__global__ __launch_bounds__(kSelThreadsB) void block_select(BlockArgs a) {
+  constexpr int NK = 2 * D / 64;
+  extern __shared__ __align__(16) uint32_t key[];  // one a block
+  __shared__ __align__(16) int8_t qa[16][2 * D];
+  __shared__ float qu[16];
+  __shared__ int hist[256], cnt[kSelWaves], out[2];
+  const int t = tid(), lane = t & 63, w = uniform(t >> 6), l16 = lane & 15, lg = lane >> 4, unit = bid_x();
+  const int b = unit / a.Hkv, g = unit % a.Hkv, B = 1 << a.block_shift;
+  const BlockSeq s = block_seq(a, b);
+  int32_t* list = a.list + (size_t)unit * a.list_ld;
+  int32_t* sel = a.sel_out ? a.sel_out + (size_t)unit * a.chosen : nullptr;
+  // blocks [0, f0) and [f1, nb) are selected whatever their scores
+  const int nb = s.blocks, f0 = min(nb, (int)(((int64_t)a.sink + B - 1) >> a.block_shift));
+  int f1 = s.row + 1 - a.recent;
+  f1 = max(f0, min(nb, f1 <= 0 ? 0 : f1 >> a.block_shift));
+  const bool scored = f1 - f0 > a.best && a.best > 0;
+  if (scored) {
+    {
+      const int h = w;
+      const bool ok = h < a.G;
+      float x[D / 64];
+      uint32_t m = 0;
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        const uint32_t v = ok ? ((const uint16_t*)a.q)[((size_t)b * a.Hq + g * a.G + h) * D + i * 64 + lane] : 0u;
+        x[i] = bf16_bits_to_f32(v);
+        const uint32_t mag = v & 0x7fffu;
+        m = max(m, mag < 0x7f80u ? mag : 0u);
+      }
+      const float u = block_scale(wave_max(m), 127.f);
+      if (lane == 0) qu[h] = u;
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        const float z[4] = {x[i], 0.f, 0.f, 0.f};
+        const int c = (int)(int8_t)(int8x4(z, u) & 0xffu);
+        qa[h][i * 64 + lane] = (int8_t)min(c, 0);
+        qa[h][D + i * 64 + lane] = (int8_t)max(c, 0);
+      }
+    }
+    __syncthreads();
+    i32x4 q[NK];
+#pragma unroll
+    for (int i = 0; i < NK; ++i) q[i] = *(const i32x4*)(&qa[l16][64 * i + 16 * lg]);
+    const float u = qu[l16];
+    for (int j0 = f0 + 16 * w; j0 < f1; j0 += 16 * kSelWaves) {
+      const int j = min(j0 + l16, f1 - 1), at = block_at(a, s.slot, g, j);
+      const float bs = at < 0 ? 0.f : a.bscale[at];
+      const int8_t* from = a.bound + (size_t)max(at, 0) * 2 * D + 16 * lg;
+      i32x4 c = {0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < NK; ++i) c = __builtin_amdgcn_mfma_i32_16x16x64_i8(*(const i32x4*)(from + 64 * i), q[i], c, 0, 0, 0);
+      float best[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        best[e] = l16 < a.G ? (float)c[e] * u : -INFINITY;
+#pragma unroll
+        for (int o = 8; o >= 1; o >>= 1) best[e] = fmaxf(best[e], __shfl_xor(best[e], o));
+      }
+      // lane (l16 < 4, lg) keeps block 4 lg + l16's; its scale and place are lane 4 lg + l16's
+      const int from_lane = 4 * lg + (l16 & 3);
+      const float mine = l16 == 0 ? best[0] : (l16 == 1 ? best[1] : (l16 == 2 ? best[2] : best[3]));
+      const float scale = __shfl(bs, from_lane);
+      const int place = __shfl(at, from_lane);
+      if (l16 < 4 && j0 + from_lane < f1) key[j0 + from_lane] = place < 0 ? 0u : score_key(mine * scale);
+    }
+  } else {
+    for (int j = f0 + t; j < f1; j += kSelThreadsB) key[j] = a.best > 0 && block_at(a, s.slot, g, j) >= 0 ? kForced : 0u;
+  }
+  for (int i = t; i < f0 + nb - f1; i += kSelThreadsB) {
+    const int j = i < f0 ? i : f1 + i - f0;
+    key[j] = block_at(a, s.slot, g, j) >= 0 ? kForced : 0u;
+  }
+  // the score of the last one taken, T, and how many of that score are
+  uint32_t T = 0;
+  int rem = a.best;
+  if (scored) {
+    for (int sh = 24; sh >= 0; sh -= 8) {
+      __syncthreads();
+      if (t < 256) hist[t] = 0;
+      __syncthreads();
+      for (int j = f0 + t; j < f1; j += kSelThreadsB) {
+        const uint32_t k = key[j];
+        if (k != 0 && (sh == 24 || (k >> (sh + 8)) == (T >> (sh + 8)))) atomicAdd(&hist[(k >> sh) & 255], 1);
+      }
+      __syncthreads();
+      if (w == 0) {  // lane's four bins, the largest first
+        int c[4], sum = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          c[i] = hist[255 - 4 * lane - i];
+          sum += c[i];
+        }
+        int before = wave_scan(sum) - sum;
+        const int total = wave_total(sum);
+        if (total < rem && lane == 0) {  // fewer than wanted are there at all: everything is taken
+          out[0] = -1;
+          out[1] = 0;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (before < rem && before + c[i] >= rem) {
+            out[0] = 255 - 4 * lane - i;
+            out[1] = before;
+          }
+          before += c[i];
+        }
+      }
+      __syncthreads();
+      if (out[0] < 0) {
+        T = 1;  // keys are 1 at least; only equal ones would be counted
+        rem = 0x7fffffff;
+        break;
+      }
+      T |= (uint32_t)out[0] << sh;
+      rem -= out[1];
+    }
+  } else {
+    T = 1;
+  }
+  __syncthreads();
+  // taken in order: above T, and the first `rem` of T; wave w ranks its share of the blocks
+  const int share = ((nb + kSelWaves - 1) / kSelWaves + 63) & ~63, a0 = min(nb, w * share), a1 = min(nb, a0 + share);
+  int eq = 0;
+  for (int j = a0 + lane; j - lane < a1; j += 64) eq += __builtin_popcountll(__builtin_amdgcn_ballot_w64(j < a1 && key[j] == T));
+  if (lane == 0) cnt[w] = eq;
+  __syncthreads();
+  int eq_before = 0;
+  for (int i = 0; i < w; ++i) eq_before += cnt[i];
+  __syncthreads();
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+  int taken = 0, e0 = eq_before;
+  for (int j = a0 + lane; j - lane < a1; j += 64) {
+    const uint32_t k = j < a1 ? key[j] : 0u;
+    const uint64_t me = __builtin_amdgcn_ballot_w64(j < a1 && k == T);
+    const bool take = k != 0 && (k > T || (k == T && e0 + __builtin_popcountll(me & below) < rem));
+    taken += __builtin_popcountll(__builtin_amdgcn_ballot_w64(take));
+    e0 += __builtin_popcountll(me);
+  }
+  if (lane == 0) cnt[w] = taken;
+  __syncthreads();
+  int at = 0, total = 0;
+  for (int i = 0; i < kSelWaves; ++i) {
+    if (i < w) at += cnt[i];
+    total += cnt[i];
+  }
+  e0 = eq_before;
+  for (int j = a0 + lane; j - lane < a1; j += 64) {
+    const uint32_t k = j < a1 ? key[j] : 0u;
+    const uint64_t me = __builtin_amdgcn_ballot_w64(j < a1 && k == T);
+    const bool take = k != 0 && (k > T || (k == T && e0 + __builtin_popcountll(me & below) < rem));
+    const uint64_t tm = __builtin_amdgcn_ballot_w64(take);
+    const int i = at + __builtin_popcountll(tm & below);
+    if (take && debug_check(i < a.list_ld, kDbgBlockList)) {
+      list[i] = j;
+      if (sel) sel[i] = j;
+    }
+    at += __builtin_popcountll(tm);
+    e0 += __builtin_popcountll(me);
+  }
+  if (t == 0) a.count[unit] = min(total, a.list_ld);
+  if (sel)
+    for (int i = total + t; i < a.chosen; i += kSelThreadsB) sel[i] = -1;
+}
+
+// ---------------------------------------------------------------- attention
+constexpr float kStaleMax = 8.f;
+
+// Eight probabilities as three bf16 terms, whose sum they are (pe is used up).
+__device__ __forceinline__ void three_terms(float (&pe)[8], bf16x8 (&p)[3]) {
+#pragma unroll
+  for (int part = 0; part < 3; ++part) {
+    u32x4 pw;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float lo = part ? fmaxf(pe[2 * i], 0x1p-126f) : pe[2 * i];
+      const float hi = part ? fmaxf(pe[2 * i + 1], 0x1p-126f) : pe[2 * i + 1];
+      pe[2 * i] -= __uint_as_float(__float_as_uint(pe[2 * i]) & 0xffff0000u);
+      pe[2 * i + 1] -= __uint_as_float(__float_as_uint(pe[2 * i + 1]) & 0xffff0000u);
+      pw[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+    }
+    p[part] = __builtin_bit_cast(bf16x8, pw);
+  }
+}
+
+// 4 codes -> 4 bf16 (exact)
+template <int KIND>
+__device__ __forceinline__ u32x2 bf16x4(uint32_t c) {
+  if constexpr (KIND == kRowsFp8) {
+    return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, 1.0f, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, 1.0f, true))};
+  } else {
+    uint32_t f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = __float_as_uint((float)(int)(int8_t)(c >> (8 * i)));
+    return u32x2{__builtin_amdgcn_perm(f[1], f[0], 0x07060302u), __builtin_amdgcn_perm(f[3], f[2], 0x07060302u)};
+  }
+}
+
+template <int D>
+struct Soft {
+  static constexpr int VE = D / 16;  // value dims a lane
+  float m = -INFINITY, mref = 0.f, lsum = 0.f;
+  f32x4 acc[VE];
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int c = 0; c < VE; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  // products x of eight rows at xs a unit (xlo: its low part), values vw (two bf16 a
+  // word) at vs
+  __device__ __forceinline__ void add(const float (&x)[8], float xs, float xlo, const uint32_t (&vw)[8][VE / 2], float vs) {
+    float bm = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+    bm = fmaxf(bm, __shfl_xor(bm, 16));
+    bm = fmaxf(bm, __shfl_xor(bm, 32));
+    bm *= xs;
+    const bool up = bm > m + kStaleMax;
+    if (wave_any(up)) {
+      const float mnew = up ? bm : m, alpha = up ? fast_exp2(m - mnew) : 1.f;
+#pragma unroll
+      for (int c = 0; c < VE; ++c) acc[c] *= alpha;
+      lsum *= alpha;
+      m = mnew;
+      mref = m == -INFINITY ? 0.f : m;
+    }
+    float pe[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) pe[i] = fast_exp2(fmaf(x[i], xs, fmaf(x[i], xlo, -mref)));
+    lsum += ((pe[0] + pe[1]) + (pe[2] + pe[3])) + ((pe[4] + pe[5]) + (pe[6] + pe[7]));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) pe[i] *= vs;
+    bf16x8 p[3];
+    three_terms(pe, p);
+#pragma unroll
+    for (int c = 0; c < VE; ++c) {
+      const uint32_t sel = (c & 1) ? 0x07060302u : 0x05040100u;
+      u32x4 av;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) av[i] = __builtin_amdgcn_perm(vw[2 * i + 1][c >> 1], vw[2 * i][c >> 1], sel);
+#pragma unroll
+      for (int part = 2; part >= 0; --part)
+        acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, av), p[part], acc[c], 0, 0, 0);
+    }
+  }
+};
+
+template <int D, int KIND>
+__global__ __launch_bounds__(64) void block_attn(BlockArgs a) {
+  constexpr int E = KIND == kRowsBf16 ? 2 : 1, VE = D / 16;
+  constexpr int NK = D * E / 64;
+  typedef uint32_t VRaw __attribute__((ext_vector_type(VE * E / 4)));
+  typedef uint32_t VTail __attribute__((ext_vector_type(VE * 2 / 4)));
+  const int lane = tid() & 63, l16 = lane & 15, lg = lane >> 4, item = bid_x(), units = a.n * a.Hkv, B = 1 << a.block_shift;
+  const bool own_block = item < units;
+  const int unit = own_block ? item : (item - units) / a.per_unit, chunk = own_block ? 0 : (item - units) % a.per_unit;
+  const int b = unit / a.Hkv, g = unit % a.Hkv;
+  const BlockSeq s = block_seq(a, b);
+  const bool hval = l16 < a.G;
+  const unsigned char* qp = (const unsigned char*)a.q + ((size_t)b * a.Hq + g * a.G + (hval ? l16 : 0)) * D * 2;
+  Soft<D> o;
+  o.init();
+  if (own_block) {
+    const int T = s.row >> a.block_shift, at = s.row < 0 ? -1 : uniform(block_at(a, s.slot, g, T));
+    if (at >= 0) {
+      const int newest = s.row & (B - 1);
+      const size_t t0 = (((size_t)s.slot * a.Hkv + g) << a.block_shift) * D * 2, p0 = ((size_t)at << a.block_shift) * D * 2;
+      unsigned char* kb = KIND == kRowsBf16 ? a.ck + p0 : a.kt + t0;
+      unsigned char* vb = KIND == kRowsBf16 ? a.cv + p0 : a.vt + t0;
+      const unsigned char* kn = a.k_new ? (const unsigned char*)a.k_new + (size_t)unit * D * 2 : kb + newest * (D * 2);
+      const unsigned char* vn = a.k_new ? (const unsigned char*)a.v_new + (size_t)unit * D * 2 : vb + newest * (D * 2);
+      if (s.tail) {
+        u32x4 q[D / 32];
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) q[j] = hval ? *(const u32x4*)(qp + 64 * j + 16 * lg) : u32x4{0u, 0u, 0u, 0u};
+        for (int r0 = 0; r0 <= newest; r0 += 32) {
+          const int ra = r0 + l16, rb = ra + 16;
+          const unsigned char* pa = ra >= newest ? kn : kb + ra * (D * 2);  // (rows past the newest are masked)
+          const unsigned char* pb = rb >= newest ? kn : kb + rb * (D * 2);
+          f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int j = 0; j < D / 32; ++j) {
+            s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, *(const u32x4*)(pa + 64 * j + 16 * lg)),
+                                                         __builtin_bit_cast(bf16x8, q[j]), s0, 0, 0, 0);
+            s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, *(const u32x4*)(pb + 64 * j + 16 * lg)),
+                                                         __builtin_bit_cast(bf16x8, q[j]), s1, 0, 0, 0);
+          }
+          float x[8];
+          uint32_t vw[8][VE / 2];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int r = r0 + (i < 4 ? 0 : 16) + 4 * lg + (i & 3);
+            x[i] = r <= newest ? (i < 4 ? s0[i & 3] : s1[i & 3]) : -INFINITY;
+            VTail v = *(const VTail*)((r >= newest ? vn : vb + r * (D * 2)) + l16 * (VE * 2));
+            if (r > newest) v = VTail{};
+#pragma unroll
+            for (int u = 0; u < VE / 2; ++u) vw[i][u] = v[u];
+          }
+          o.add(x, a.scale2, a.scale2_lo, vw, 1.f);
+        }
+      }
+      if (a.k_new && s.row < a.max_pages << a.page_shift) {
+        // the token's row, and the block's codes and bounds when it is the last of one
+        if (lane < D / 8) *((u32x4*)(kb + newest * (D * 2)) + lane) = *((const u32x4*)kn + lane);
+        else if (lane < D / 4) *((u32x4*)(vb + newest * (D * 2)) + lane - D / 8) = *((const u32x4*)vn + lane - D / 8);
+        if (newest == B - 1) {
+          put_block<D, KIND>(a, at, true, [&](int r) { return r == newest ? kn : kb + r * (D * 2); });
+          put_block<D, KIND>(a, at, false, [&](int r) { return r == newest ? vn : vb + r * (D * 2); });
+        }
+      }
+    }
+  } else {
+    const int32_t* list = a.list ? a.list + (size_t)unit * a.list_ld : nullptr;
+    const int nb = a.list ? uniform(a.count[unit]) : s.blocks;
+    const int e0 = (int)((int64_t)chunk * nb / a.per_unit), e1 = (int)((int64_t)(chunk + 1) * nb / a.per_unit);
+    u32x4 q[D / 32];
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+      const int off = KIND == kRowsBf16 ? 64 * j + 16 * lg : (64 * (j / 2) + 16 * lg + 8 * (j & 1)) * 2;
+      q[j] = hval ? *(const u32x4*)(qp + off) : u32x4{0u, 0u, 0u, 0u};
+    }
+    for (int e = e0; e < e1; ++e) {
+      const int at = uniform(block_at(a, s.slot, g, list ? list[e] : e));
+      if (at < 0) continue;
+      const float ksc = KIND == kRowsBf16 ? 1.f : a.ks[at], vsc = KIND == kRowsBf16 ? 1.f : a.vs[at];
+      const float xs = a.scale2 * ksc, xlo = a.scale2_lo * ksc;
+      for (int r0 = 0; r0 < B; r0 += 32) {
+        const size_t p0 = (((size_t)at << a.block_shift) + r0) * (D * E);
+        const unsigned char* kp = a.ck + p0 + l16 * (D * E) + 16 * lg;
+        const unsigned char* vp = a.cv + p0 + 4 * lg * (D * E) + l16 * (VE * E);
+        f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < NK; ++j) {
+          const u32x4 k0 = *(const u32x4*)(kp + 64 * j), k1 = *(const u32x4*)(kp + 16 * (D * E) + 64 * j);
+          if constexpr (KIND == kRowsBf16) {
+            s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k0), __builtin_bit_cast(bf16x8, q[j]), s0, 0, 0, 0);
+            s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k1), __builtin_bit_cast(bf16x8, q[j]), s1, 0, 0, 0);
+          } else {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const bf16x8 qq = __builtin_bit_cast(bf16x8, q[2 * j + u]);
+              const u32x2 a0 = bf16x4<KIND>(k0[2 * u]), a1 = bf16x4<KIND>(k0[2 * u + 1]);
+              const u32x2 b0 = bf16x4<KIND>(k1[2 * u]), b1 = bf16x4<KIND>(k1[2 * u + 1]);
+              s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{a0[0], a0[1], a1[0], a1[1]}), qq, s0, 0, 0, 0);
+              s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{b0[0], b0[1], b1[0], b1[1]}), qq, s1, 0, 0, 0);
+            }
+          }
+        }
+        const float x[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
+        uint32_t vw[8][VE / 2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const VRaw v = *(const VRaw*)(vp + ((i < 4 ? 0 : 16) + (i & 3)) * (D * E));
+          if constexpr (KIND == kRowsBf16) {
+#pragma unroll
+            for (int u = 0; u < VE / 2; ++u) vw[i][u] = v[u];
+          } else {
+#pragma unroll
+            for (int u = 0; u < VE / 4; ++u) {
+              const u32x2 c = bf16x4<KIND>(v[u]);
+              vw[i][2 * u] = c[0];
+              vw[i][2 * u + 1] = c[1];
+            }
+          }
+        }
+        o.add(x, xs, xlo, vw, vsc);
+      }
+    }
+  }
+  o.lsum += __shfl_xor(o.lsum, 16);
+  o.lsum += __shfl_xor(o.lsum, 32);
+  if (!hval) return;
+  const size_t pi = (size_t)item * a.G + l16;
+  if (lg == 0) a.ml[pi] = make_float2(o.m, o.lsum);
+  float* dst = a.part + pi * D + 4 * lg * VE;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+#pragma unroll
+    for (int c = 0; c < VE; c += 4)
+      *(f32x4*)(dst + e * VE + c) = f32x4{o.acc[c][e], o.acc[c + 1][e], o.acc[c + 2][e], o.acc[c + 3][e]};
+}
+
+// ---------------------------------------------------------------- join
+template <int D>
+__global__ __launch_bounds__(D) void block_join(BlockArgs a) {
+  const int bh = bid_x(), b = bh / a.Hq, qh = bh % a.Hq, g = qh / a.G, h = qh % a.G, units = a.n * a.Hkv, unit = b * a.Hkv + g;
+  const int t = tid();
+  auto item = [&](int i) { return (size_t)(i == 0 ? unit : units + unit * a.per_unit + i - 1) * a.G + h; };
+  float M = -INFINITY, L = 0.f, o = 0.f;
+  for (int i = 0; i <= a.per_unit; ++i) M = fmaxf(M, a.ml[item(i)].x);
+  for (int i = 0; i <= a.per_unit; ++i) {
+    const float2 v = a.ml[item(i)];
+    if (v.x == -INFINITY) continue;
+    const float f = fast_exp2(v.x - M);
+    L = fmaf(f, v.y, L);
+    o = fmaf(f, a.part[item(i) * D + t], o);
+  }
+  o = L > 0.f ? o / L : 0.f;
+  if (a.out_bf16)
+    ((uint16_t*)a.out)[(size_t)bh * D + t] = (uint16_t)f32_to_bf16_bits(o);
+  else
+    ((float*)a.out)[(size_t)bh * D + t] = o;
+}
+
+inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+inline int log2_of(int x) { return 31 - __builtin_clz((unsigned)x); }
+int kind_of(int kv_dtype) { return kv_dtype == SNAP_BF16 ? kRowsBf16 : (kv_dtype == SNAP_INT8 ? kRowsInt8 : kRowsFp8); }
+
+BlockArgs block_args(const snap_params& p, const snap_block_cache& c, const int32_t* rows, int n, const int32_t* slot_ids,
+                     const void* k_new, const void* v_new) {
+  BlockArgs a = {};
+  a.ck = (unsigned char*)c.k;
+  a.cv = (unsigned char*)c.v;
+  a.ks = c.k_scale;
+  a.vs = c.v_scale;
+  a.kt = (unsigned char*)c.k_tail;
+  a.vt = (unsigned char*)c.v_tail;
+  a.bound = (int8_t*)c.bound;
+  a.bscale = c.bound_scale;
+  a.rows = rows;
+  a.slot_ids = slot_ids;
+  a.table = c.page_table;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.n = n;
+  a.Hq = p.n_q_heads;
+  a.Hkv = p.n_kv_heads;
+  a.G = p.n_q_heads / p.n_kv_heads;
+  a.n_slots = c.n_slots;
+  a.n_pages = c.n_pages;
+  a.page_shift = log2_of(c.page_size);
+  a.block_shift = log2_of(c.block);
+  a.max_pages = c.max_pages;
+  return a;
+}
+
+}  // namespace
+
+SNAP_DEBUG_READER(debug_flags_blocks)
+
+// ---------------------------------------------------------------- host side
+int block_chosen(const snap_params& p, int block) {
+  return (p.sink + block - 1) / block + (p.recent - 1 + block - 1) / block + (p.topk + block - 1) / block;
+}
+
+constexpr int kResident = 2048;
+BlockGeometry block_geometry(const snap_params& p, int n, int max_rows, int block, bool select) {
+  BlockGeometry g{};
+  const int units = (n > 0 ? n : 1) * p.n_kv_heads, G = p.n_q_heads / p.n_kv_heads;
+  g.blocks = max_rows / block;
+  g.chosen = block_chosen(p, block);
+  const int most = g.blocks < 1 ? 1 : g.blocks, read = select && g.chosen < most ? (g.chosen < 1 ? 1 : g.chosen) : most;
+  g.list_ld = g.chosen < most ? g.chosen : most;
+  g.per_unit = kResident / units;
+  if (g.per_unit < 1) g.per_unit = 1;
+  if (g.per_unit > read) g.per_unit = read;
+  // a bound that does not fall as sequences or rows grow
+  const int64_t codes = (int64_t)units * most < (units > kResident ? units : kResident) ? (int64_t)units * most
+                                                                                        : (units > kResident ? units : kResident);
+  const size_t items = (size_t)units + (size_t)codes;
+  size_t off = 0;
+  g.off_part = off;
+  off = align256(off + items * G * p.d_v * sizeof(float));
+  g.off_ml = off;
+  off = align256(off + items * G * sizeof(float2));
+  g.off_list = off;
+  if (select) off = align256(off + (size_t)units * g.list_ld * sizeof(int32_t));
+  g.off_count = off;
+  if (select) off = align256(off + (size_t)units * sizeof(int32_t));
+  g.bytes = off;
+  return g;
+}
+
+snap_status launch_block_append(const snap_params& p, const snap_block_cache& c, const int32_t* rows, int n,
+                                const int32_t* slot_ids, const int32_t* lengths, const int32_t* starts, int tokens,
+                                int max_len, const void* k_new, const int64_t* k_stride, const void* v_new,
+                                const int64_t* v_stride, hipStream_t stream) {
+  BlockAppend a = {};
+  a.c = block_args(p, c, rows, n, slot_ids, k_new, v_new);
+  a.lengths = lengths;
+  a.starts = starts;
+  a.tokens = tokens;
+  a.max_len = max_len;
+  const int64_t d = p.d_qk, h = p.n_kv_heads;
+  const int64_t kd[3] = {h * max_len * d, starts ? d : max_len * d, starts ? h * d : d};
+  for (int i = 0; i < 3; ++i) {
+    a.ks[i] = 2 * (k_stride ? k_stride[i] : kd[i]);
+    a.vs[i] = 2 * (v_stride ? v_stride[i] : kd[i]);
+  }
+  const int blocks = (int)(((int64_t)max_len + 2 * c.block - 2) / c.block);
+  static constexpr void (*kernels[2][3])(BlockAppend) = {
+      {block_append<64, kRowsBf16>, block_append<64, kRowsFp8>, block_append<64, kRowsInt8>},
+      {block_append<128, kRowsBf16>, block_append<128, kRowsFp8>, block_append<128, kRowsInt8>}};
+  hipLaunchKernelGGL(kernels[p.d_qk == 128][kind_of(p.kv_dtype)], dim3((blocks + 1) / 2, p.n_kv_heads, n), dim3(256), 0, stream, a);
+  return hipGetLastError() == hipSuccess ? SNAP_OK : SNAP_ERR_HIP;
+}
+
+snap_status launch_block_decode(const snap_params& p, const snap_block_cache& c, const int32_t* rows, int n,
+                                const int32_t* slot_ids, int max_rows, const void* q, const void* k_new, const void* v_new,
+                                void* out, int out_dtype, bool select, int32_t* sel_out, void* ws, hipStream_t stream) {
+  const BlockGeometry geo = block_geometry(p, n, max_rows, c.block, select);
+  BlockArgs a = block_args(p, c, rows, n, slot_ids, k_new, v_new);
+  a.q = q;
+  a.part = (float*)((unsigned char*)ws + geo.off_part);
+  a.ml = (float2*)((unsigned char*)ws + geo.off_ml);
+  a.out = out;
+  a.max_rows = max_rows;
+  a.per_unit = geo.per_unit;
+  a.chosen = geo.chosen;
+  a.list_ld = geo.list_ld;
+  a.out_bf16 = out_dtype == SNAP_BF16;
+  split_scale2(p.sm_scale > 0.f ? p.sm_scale : 1.0f / sqrtf((float)p.d_qk), a.scale2, a.scale2_lo);
+  const int units = n * p.n_kv_heads;
+  if (select) {
+    a.list = (int32_t*)((unsigned char*)ws + geo.off_list);
+    a.count = (int32_t*)((unsigned char*)ws + geo.off_count);
+    a.sel_out = sel_out;
+    a.sink = p.sink;
+    a.recent = p.recent;
+    a.best = (p.topk + c.block - 1) / c.block;
+    const size_t lds = (size_t)(geo.blocks < 1 ? 1 : geo.blocks) * sizeof(uint32_t);
+    hipLaunchKernelGGL((p.d_qk == 128 ? block_select<128> : block_select<64>), dim3(units), dim3(kSelThreadsB), lds, stream, a);
+    if (hipGetLastError() != hipSuccess) return SNAP_ERR_HIP;
+  }
+  static constexpr void (*kernels[2][3])(BlockArgs) = {
+      {block_attn<64, kRowsBf16>, block_attn<64, kRowsFp8>, block_attn<64, kRowsInt8>},
+      {block_attn<128, kRowsBf16>, block_attn<128, kRowsFp8>, block_attn<128, kRowsInt8>}};
+  hipLaunchKernelGGL(kernels[p.d_qk == 128][kind_of(p.kv_dtype)], dim3(units + units * geo.per_unit), dim3(64), 0, stream, a);
+  if (hipGetLastError() != hipSuccess) return SNAP_ERR_HIP;
+  hipLaunchKernelGGL((p.d_qk == 128 ? block_join<128> : block_join<64>), dim3(n * p.n_q_heads), dim3(p.d_qk), 0, stream, a);
+  return hipGetLastError() == hipSuccess ? SNAP_OK : SNAP_ERR_HIP;
+}
+
+}  // namespace snap

@@ -1,7 +1,8 @@
 // paged.hip -- the paged cache: storing new tokens, and attention of one new
 // token per sequence over every row its slot holds.
 //
-//   paged_append   stores the tokens of a prompt or of a step
+//   paged_append   stores the tokens of a prompt or of a step (paged_append_mapped: of
+//                  a packed batch, by its map)
 //   paged_gqa      64- and 128-wide rows: one wave per work item on the matrix
 //                  units
 //   paged_latent   latent rows: four waves per work item, through LDS
@@ -1115,6 +1116,48 @@ __global__ __launch_bounds__(256) void paged_append(PagedAppendArgs a) {
   }
 }
 
+// A packed batch by its map: tokens 32x .. 32x + 31, y: KV head.
+struct PagedMapArgs {
+  const void* k_new;
+  const void* v_new;
+  void* ck;
+  void* cv;
+  const float* k_scale;
+  const float* v_scale;
+  int32_t* token;
+  float* weight;
+  const int32_t* slot_ids;
+  const int32_t* seq_of;
+  const int32_t* row_of;
+  const int32_t* pos_of;
+  int64_t ks[2], vs[2];
+  int64_t rows;  // of all pages, for one KV head
+  int n, tokens, Hkv, dk, dv, n_slots, page_shift;
+};
+template <typename In, typename Out>
+__global__ __launch_bounds__(256) void paged_append_mapped(PagedMapArgs a) {
+  const int g = bid_y(), kc = a.dk / 8, vc = a.v_new ? a.dv / 8 : 0, t0 = bid_x() * kAppendTokens;
+  for (int i = tid(); i < kAppendTokens * (kc + vc); i += 256) {
+    const int t = t0 + i / (kc + vc), c = i % (kc + vc);
+    if (t >= a.tokens) break;
+    const int r = a.row_of[t], b = a.seq_of[t];
+    if (r < 0 || r >= a.rows || b < 0 || b >= a.n) continue;
+    const int slot = a.slot_ids[b];
+    if (slot < 0 || slot >= a.n_slots) continue;
+    const int64_t row = (((int64_t)(r >> a.page_shift) * a.Hkv + g) << a.page_shift) + (r & ((1 << a.page_shift) - 1));
+    if (c < kc)
+      store8<In, Out>((const In*)a.k_new + t * a.ks[0] + g * a.ks[1] + 8 * c, (Out*)a.ck + row * a.dk + 8 * c,
+                      sizeof(Out) == 1 ? a.k_scale[(size_t)slot * a.Hkv + g] : 1.f);
+    else
+      store8<In, Out>((const In*)a.v_new + t * a.vs[0] + g * a.vs[1] + 8 * (c - kc), (Out*)a.cv + row * a.dv + 8 * (c - kc),
+                      sizeof(Out) == 1 ? a.v_scale[(size_t)slot * a.Hkv + g] : 1.f);
+    if (c == 0) {
+      if (a.token) a.token[row] = a.pos_of[t];
+      if (a.weight) a.weight[row] = 0.f;
+    }
+  }
+}
+
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 inline int log2_of(int x) { return 31 - __builtin_clz((unsigned)x); }
 
@@ -1237,6 +1280,46 @@ snap_status launch_paged_append(const snap_params& p, const snap_paged_cache& c,
     hipLaunchKernelGGL((paged_append<uint16_t, uint16_t>), grid, dim3(256), 0, stream, a);
   else
     hipLaunchKernelGGL((paged_append<float, float>), grid, dim3(256), 0, stream, a);
+  return hipGetLastError() == hipSuccess ? SNAP_OK : SNAP_ERR_HIP;
+}
+
+snap_status launch_paged_append_mapped(const snap_params& p, const snap_paged_cache& c, int n, const int32_t* slot_ids,
+                                       int tokens, const int32_t* seq_of, const int32_t* row_of, const int32_t* pos_of,
+                                       const void* k_new, const int64_t* k_stride, const void* v_new,
+                                       const int64_t* v_stride, hipStream_t stream) {
+  PagedMapArgs a = {};
+  a.k_new = k_new;
+  a.v_new = p.v_in_k ? nullptr : v_new;
+  a.ck = c.k;
+  a.cv = p.v_in_k ? nullptr : c.v;
+  a.k_scale = c.k_scale;
+  a.v_scale = c.v_scale;
+  a.token = c.token;
+  a.weight = c.weight;
+  a.slot_ids = slot_ids;
+  a.seq_of = seq_of;
+  a.row_of = row_of;
+  a.pos_of = pos_of;
+  a.rows = (int64_t)c.n_pages * c.page_size;
+  a.n = n;
+  a.tokens = tokens;
+  a.Hkv = p.n_kv_heads;
+  a.dk = p.d_qk;
+  a.dv = p.d_v;
+  a.n_slots = c.n_slots;
+  a.page_shift = log2_of(c.page_size);
+  const int64_t kd[2] = {(int64_t)p.n_kv_heads * p.d_qk, p.d_qk}, vd[2] = {(int64_t)p.n_kv_heads * p.d_v, p.d_v};
+  for (int i = 0; i < 2; ++i) {
+    a.ks[i] = k_stride ? k_stride[i] : kd[i];
+    a.vs[i] = v_stride ? v_stride[i] : vd[i];
+  }
+  const dim3 grid((tokens + kAppendTokens - 1) / kAppendTokens, p.n_kv_heads);
+  if (p.kv_dtype == SNAP_FP8_E4M3)
+    hipLaunchKernelGGL((paged_append_mapped<uint16_t, uint8_t>), grid, dim3(256), 0, stream, a);
+  else if (p.kv_dtype == SNAP_BF16)
+    hipLaunchKernelGGL((paged_append_mapped<uint16_t, uint16_t>), grid, dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL((paged_append_mapped<float, float>), grid, dim3(256), 0, stream, a);
   return hipGetLastError() == hipSuccess ? SNAP_OK : SNAP_ERR_HIP;
 }
 

@@ -1,0 +1,269 @@
+// pages.hip -- page tables on the device: pages handed out to sequences that grow,
+// taken back, and the map of a packed batch's tokens to their rows.
+//
+//   pages_reserve   one workgroup: what each sequence lacks, served in order by
+//                   prefix sums, the pages copied off the end of the free list
+//   pages_release   one workgroup: the reverse
+//   pages_map       a workgroup for every kMapTokens tokens, each after its own
+//                   prefix sums of the lengths
+//
+// All are bound by latency: a handful of dependent loads, no more than 12 bytes a
+// token written.
+#include "snap_internal.h"
+
+namespace snap {
+
+namespace {
+
+constexpr int kPoolThreads = 1024;
+constexpr int kPoolWaves = kPoolThreads / 64;
+
+struct PoolArgs {
+  int32_t* table;
+  int32_t* held;
+  int32_t* free_pages;
+  int32_t* n_free;
+  const int32_t* rows;
+  const int32_t* slot_ids;
+  const int32_t* lengths;
+  int32_t* short_out;
+  int n, len, n_slots, n_pages, page_shift, max_pages;
+};
+
+// Inclusive prefix sum over a workgroup of W waves (every thread calls); `total`: of
+// all.  64 bits: a thousand sequences may lack 2^24 pages each.
+template <int W>
+__device__ __forceinline__ int64_t group_scan(int64_t v, int64_t* red, int64_t& total) {
+  const int lane = tid() & 63, w = tid() >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t u = __shfl_up((long long)v, o);
+    if (lane >= o) v += u;
+  }
+  __syncthreads();
+  if (lane == 63) red[w] = v;
+  __syncthreads();
+  total = 0;
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    if (i < w) v += red[i];
+    total += red[i];
+  }
+  return v;
+}
+
+// The last i in [0, 1 << BITS) with at[i] <= x (at[0] <= x, at does not fall).
+template <int BITS>
+__device__ __forceinline__ int find_last(const int* at, int x) {
+  int i = 0;
+#pragma unroll
+  for (int s = 1 << (BITS - 1); s; s >>= 1)
+    if (at[i + s] <= x) i += s;
+  return i;
+}
+
+__device__ __forceinline__ int clamp_int(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
+
+// Sequence t of a chunk is thread t.  Where all sequences of the chunk before it fit,
+// so do their pages' ranks: page e of the chunk is rank e of those taken.
+__global__ __launch_bounds__(kPoolThreads) void pages_reserve(PoolArgs a) {
+  __shared__ int64_t red[kPoolWaves];
+  __shared__ int first[kPoolThreads], to[kPoolThreads];  // rank of a sequence's first page, its table entry less that rank
+  __shared__ int slots[kPoolThreads];
+  const int t = tid();
+  const int free0 = clamp_int(*a.n_free, 0, a.n_pages);
+  int64_t before = 0;  // pages lacked by the chunks before
+  int taken = 0;
+  for (int b0 = 0; b0 < a.n; b0 += kPoolThreads) {
+    const int b = b0 + t;
+    int slot = b < a.n ? a.slot_ids[b] : -1;
+    if (slot < 0 || slot >= a.n_slots) slot = -1;
+    const int r = slot >= 0 ? a.rows[slot] : -1, h = slot >= 0 ? clamp_int(a.held[slot], 0, a.max_pages) : 0;
+    const int add = b < a.n ? (a.lengths ? a.lengths[b] : a.len) : 0;
+    const int64_t want = ((int64_t)(r < 0 ? 0 : r) + (add < 0 ? 0 : add) + (1 << a.page_shift) - 1) >> a.page_shift;
+    const int64_t lack = slot >= 0 && r >= 0 && want > h ? want - h : 0;
+    const bool fits = want <= a.max_pages;
+    int64_t total, mine = fits ? lack : 0;
+    const int64_t upto = before + group_scan<kPoolWaves>(mine, red, total);
+    const bool served = fits && (lack == 0 || upto <= free0);
+    if (b < a.n && a.short_out) a.short_out[b] = served ? 0 : (int)(lack < 0x7fffffff ? lack : 0x7fffffff);
+    const int take = served ? (int)lack : 0;
+    int64_t chunk;
+    const int rank = (int)group_scan<kPoolWaves>(take, red, chunk) - take;
+    first[t] = rank;
+    to[t] = h - rank;
+    slots[t] = slot;
+    if (take) a.held[slot] = h + take;
+    __syncthreads();
+    for (int e = t; e < (int)chunk; e += kPoolThreads) {
+      const int s = find_last<10>(first, e);
+      a.table[(size_t)slots[s] * a.max_pages + to[s] + e] = a.free_pages[free0 - 1 - taken - e];
+    }
+    taken += (int)chunk;
+    before += total;
+    __syncthreads();
+  }
+  if (t == 0) *a.n_free = free0 - taken;
+}
+
+// Chunks of sequences from the last to the first, each chunk's pages in reverse: the
+// order in which pages_reserve would take them again.
+__global__ __launch_bounds__(kPoolThreads) void pages_release(PoolArgs a) {
+  __shared__ int64_t red[kPoolWaves];
+  __shared__ int first[kPoolThreads], from[kPoolThreads], slots[kPoolThreads];
+  const int t = tid();
+  int64_t end = clamp_int(*a.n_free, 0, a.n_pages);
+  for (int b0 = (a.n - 1) / kPoolThreads * kPoolThreads; b0 >= 0; b0 -= kPoolThreads) {
+    const int b = b0 + t;
+    int slot = b < a.n ? a.slot_ids[b] : -1;
+    if (slot < 0 || slot >= a.n_slots) slot = -1;
+    int keep = 0, give = 0;
+    if (slot >= 0) {
+      const int r = a.rows[slot], h = clamp_int(a.held[slot], 0, a.max_pages);
+      const int64_t k = ((int64_t)(r < 0 ? 0 : r) + (1 << a.page_shift) - 1) >> a.page_shift;
+      keep = k < h ? (int)k : h;
+      give = h - keep;
+      a.held[slot] = keep;
+    }
+    int64_t all, chunk;
+    // more than there are pages would be entries that were handed back twice: left out
+    if (end + group_scan<kPoolWaves>(give, red, all) > a.n_pages) give = 0;
+    const int rank = (int)group_scan<kPoolWaves>(give, red, chunk) - give, m = (int)chunk;
+    first[t] = rank;
+    from[t] = keep - rank;
+    slots[t] = slot;
+    __syncthreads();
+    for (int e = t; e < m; e += kPoolThreads) {
+      const int s = find_last<10>(first, e);
+      int32_t* at = a.table + (size_t)slots[s] * a.max_pages + from[s] + e;
+      a.free_pages[end + m - 1 - e] = *at;
+      *at = -1;
+    }
+    end += m;
+    __syncthreads();
+  }
+  if (t == 0) *a.n_free = (int)end;
+}
+
+constexpr int kMapThreads = 256, kMapTokens = 1024;
+
+struct MapArgs {
+  const int32_t* table;
+  const int32_t* rows;
+  const int32_t* pos;
+  const int32_t* slot_ids;
+  const int32_t* lengths;
+  int32_t* starts;
+  int32_t* seq_of;
+  int32_t* row_of;
+  int32_t* pos_of;
+  int n, tokens, n_slots, n_pages, page_shift, max_pages;
+};
+
+__global__ __launch_bounds__(kMapThreads) void pages_map(MapArgs a) {
+  __shared__ int64_t red[kMapThreads / 64];
+  __shared__ int first[kMapThreads], slots[kMapThreads], rows[kMapThreads], pos[kMapThreads];
+  const int t = tid(), lo = bid_x() * kMapTokens;
+  const int hi = a.tokens - lo < kMapTokens ? a.tokens : lo + kMapTokens;
+  int64_t before = 0;
+  for (int b0 = 0; b0 < a.n; b0 += kMapThreads) {
+    const int b = b0 + t;
+    int len = b < a.n ? a.lengths[b] : 0, slot = b < a.n ? a.slot_ids[b] : -1;
+    len = len < 0 ? 0 : len;
+    if (slot < 0 || slot >= a.n_slots) slot = -1;
+    const int r = slot >= 0 ? a.rows[slot] : -1;
+    int64_t total;
+    const int64_t start = before + group_scan<kMapThreads / 64>(len, red, total) - len;
+    first[t] = start < a.tokens ? (int)start : a.tokens;
+    slots[t] = r < 0 ? -1 : slot;
+    rows[t] = r;
+    pos[t] = r < 0 ? 0 : (a.pos ? a.pos[slot] : r);
+    if (bid_x() == 0 && b < a.n) a.starts[b] = first[t];
+    __syncthreads();
+    const int64_t c1 = before + total;
+    for (int i = (before > lo ? (before < hi ? (int)before : hi) : lo) + t; i < (c1 < hi ? c1 : hi); i += kMapThreads) {
+      const int s = find_last<8>(first, i), at = i - first[s];
+      int64_t row = -1;
+      if (slots[s] >= 0) {
+        const int64_t x = (int64_t)rows[s] + at, p = x >> a.page_shift;
+        const int page = p < a.max_pages ? a.table[(size_t)slots[s] * a.max_pages + p] : -1;
+        if (page >= 0 && page < a.n_pages) row = ((int64_t)page << a.page_shift) + (x & ((1 << a.page_shift) - 1));
+      }
+      a.seq_of[i] = b0 + s;
+      a.row_of[i] = (int)row;
+      a.pos_of[i] = slots[s] >= 0 ? (int)((uint32_t)pos[s] + (uint32_t)at) : 0;
+    }
+    before = c1;
+    __syncthreads();
+    if (bid_x() != 0 && before >= hi) return;  // (the first workgroup has every start to write)
+  }
+  for (int i = (before > lo ? (before < hi ? (int)before : hi) : lo) + t; i < hi; i += kMapThreads) {
+    a.seq_of[i] = -1;
+    a.row_of[i] = -1;
+    a.pos_of[i] = 0;
+  }
+  if (bid_x() == 0 && t == 0) a.starts[a.n] = before < a.tokens ? (int)before : a.tokens;
+}
+
+inline int log2_of(int x) { return 31 - __builtin_clz((unsigned)x); }
+
+PoolArgs pool_args(const snap_page_pool& c, const int32_t* rows, int n, const int32_t* slot_ids) {
+  PoolArgs a = {};
+  a.table = c.page_table;
+  a.held = c.held;
+  a.free_pages = c.free_pages;
+  a.n_free = c.n_free;
+  a.rows = rows;
+  a.slot_ids = slot_ids;
+  a.n = n;
+  a.n_slots = c.n_slots;
+  a.n_pages = c.n_pages;
+  a.page_shift = log2_of(c.page_size);
+  a.max_pages = c.max_pages;
+  return a;
+}
+
+}  // namespace
+
+snap_status launch_pages_reserve(const snap_page_pool& c, const int32_t* rows, int n, const int32_t* slot_ids,
+                                 const int32_t* lengths, int len, int32_t* short_out, hipStream_t stream) {
+  PoolArgs a = pool_args(c, rows, n, slot_ids);
+  a.lengths = lengths;
+  a.len = len;
+  a.short_out = short_out;
+  hipLaunchKernelGGL(pages_reserve, dim3(1), dim3(kPoolThreads), 0, stream, a);
+  return hipGetLastError() == hipSuccess ? SNAP_OK : SNAP_ERR_HIP;
+}
+
+snap_status launch_pages_release(const snap_page_pool& c, const int32_t* rows, int n, const int32_t* slot_ids,
+                                 hipStream_t stream) {
+  const PoolArgs a = pool_args(c, rows, n, slot_ids);
+  hipLaunchKernelGGL(pages_release, dim3(1), dim3(kPoolThreads), 0, stream, a);
+  return hipGetLastError() == hipSuccess ? SNAP_OK : SNAP_ERR_HIP;
+}
+
+snap_status launch_pages_map(const snap_page_pool& c, const int32_t* rows, const int32_t* pos, int n,
+                             const int32_t* slot_ids, const int32_t* lengths, int tokens, int32_t* starts,
+                             int32_t* seq_of, int32_t* row_of, int32_t* pos_of, hipStream_t stream) {
+  MapArgs a = {};
+  a.table = c.page_table;
+  a.rows = rows;
+  a.pos = pos;
+  a.slot_ids = slot_ids;
+  a.lengths = lengths;
+  a.starts = starts;
+  a.seq_of = seq_of;
+  a.row_of = row_of;
+  a.pos_of = pos_of;
+  a.n = n;
+  a.tokens = tokens;
+  a.n_slots = c.n_slots;
+  a.n_pages = c.n_pages;
+  a.page_shift = log2_of(c.page_size);
+  a.max_pages = c.max_pages;
+  const int groups = tokens > 0 ? (int)(((int64_t)tokens + kMapTokens - 1) / kMapTokens) : 1;
+  hipLaunchKernelGGL(pages_map, dim3(groups), dim3(kMapThreads), 0, stream, a);
+  return hipGetLastError() == hipSuccess ? SNAP_OK : SNAP_ERR_HIP;
+}
+
+}  // namespace snap

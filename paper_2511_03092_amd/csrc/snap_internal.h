@@ -151,6 +151,7 @@ enum : uint32_t {
   kDbgPrefill = 1u << 8,     // a prefill block's positions outside the prompt
   kDbgPagedItem = 1u << 9,   // paged rows cut into more items than are launched
   kDbgPagedMove = 1u << 10,  // an evicted slot's move list past its end
+  kDbgBlockList = 1u << 11,  // more blocks selected than a list holds
 };
 #ifdef SNAP_DEBUG_CHECKS
 static __device__ uint32_t g_debug_flags;  // one per translation unit
@@ -181,6 +182,7 @@ uint32_t debug_flags_decode(bool reset);
 uint32_t debug_flags_prefill(bool reset);
 uint32_t debug_flags_paged(bool reset);
 uint32_t debug_flags_evict(bool reset);
+uint32_t debug_flags_blocks(bool reset);
 
 // ---------------------------------------------------------------- launch context
 struct Geometry {
@@ -298,6 +300,39 @@ EvictGeometry evict_geometry(const snap_params& p, int n, int max_rows);
 snap_status launch_paged_evict(const snap_params& p, const snap_paged_cache& c, const int32_t* rows, const int32_t* pos,
                                int32_t* rows_out, int n, const int32_t* slot_ids, int max_rows, int32_t* kept_out,
                                void* ws, hipStream_t stream);
+
+snap_status launch_paged_append_mapped(const snap_params& p, const snap_paged_cache& c, int n, const int32_t* slot_ids,
+                                       int tokens, const int32_t* seq_of, const int32_t* row_of, const int32_t* pos_of,
+                                       const void* k_new, const int64_t* k_stride, const void* v_new,
+                                       const int64_t* v_stride, hipStream_t stream);
+
+snap_status launch_pages_reserve(const snap_page_pool& c, const int32_t* rows, int n, const int32_t* slot_ids,
+                                 const int32_t* lengths, int len, int32_t* short_out, hipStream_t stream);
+snap_status launch_pages_release(const snap_page_pool& c, const int32_t* rows, int n, const int32_t* slot_ids,
+                                 hipStream_t stream);
+snap_status launch_pages_map(const snap_page_pool& c, const int32_t* rows, const int32_t* pos, int n,
+                             const int32_t* slot_ids, const int32_t* lengths, int tokens, int32_t* starts,
+                             int32_t* seq_of, int32_t* row_of, int32_t* pos_of, hipStream_t stream);
+
+// Block decode: work items of a call and its workspace.
+struct BlockGeometry {
+  int blocks;    // whole blocks of a sequence at most
+  int chosen;    // blocks that a selection lists at most
+  int list_ld;   // of which there are at most this many
+  int per_unit;  // work items of a (sequence, KV head), beside the newest token's block
+  size_t off_part, off_ml, off_list, off_count, bytes;
+};
+constexpr int kBlockMost = 32768;  // blocks that one workgroup selects among (their scores in LDS)
+int block_chosen(const snap_params& p, int block);
+BlockGeometry block_geometry(const snap_params& p, int n, int max_rows, int block, bool select);
+snap_status launch_block_append(const snap_params& p, const snap_block_cache& c, const int32_t* rows, int n,
+                                const int32_t* slot_ids, const int32_t* lengths, const int32_t* starts, int tokens,
+                                int max_len, const void* k_new, const int64_t* k_stride, const void* v_new,
+                                const int64_t* v_stride, hipStream_t stream);
+// k_new non-NULL: the token at rows[slot] is stored first, as launch_block_append does
+snap_status launch_block_decode(const snap_params& p, const snap_block_cache& c, const int32_t* rows, int n,
+                                const int32_t* slot_ids, int max_rows, const void* q, const void* k_new, const void* v_new,
+                                void* out, int out_dtype, bool select, int32_t* sel_out, void* ws, hipStream_t stream);
 
 // device address of the current GPU's snap_decode_step_noalloc scratch array
 snap_status noalloc_scratch(void** addr);
