@@ -574,10 +574,11 @@ snap_status snap_pages_map(const snap_page_pool* pool, const int32_t* rows, cons
  *   bound_scale [n_pages][n_kv_heads][page_size / block] fp32: of the whole blocks'
  *          keys, the least (rounded down) and the largest (rounded up) of every dim,
  *          in units of bound_scale; NULL (both) where nothing is selected
- * A whole block's scale is s = amax / 127 (int8, and bounds) or amax / 448 (E4M3),
- * amax the largest magnitude of its finite values, at least 2^-126, 1 where amax is
- * 0; codes are x / s (fp32 quotient) rounded to nearest even, saturating; NaN is the
- * code 0 in int8, E4M3's NaN code there, and no bound.  So codes and scales do not
+ * A whole block's scale is s = amax * fl(1 / 127) (int8, and bounds) or
+ * amax * fl(1 / 448) (E4M3), fl and the product in fp32, amax the largest magnitude
+ * of its finite values; at least 2^-126, and 1 where amax is 0.  Codes are x / s (fp32
+ * quotient) rounded to nearest even, saturating; NaN is the code 0 in int8, E4M3's NaN
+ * code there, and no bound.  So codes and scales do not
  * depend on how the tokens were split into calls.
  * Page ids outside [0, n_pages) are pages that are not there: nothing is stored in
  * their rows (nor kept in the tail for them), and they receive no attention.  Slots
@@ -636,7 +637,7 @@ size_t snap_block_decode_workspace(const snap_params* p, int32_t n, int32_t max_
  *   block),
  * for each KV head.  The score is an upper bound of what a query of the KV head's
  * group may have in a block, formed in whole numbers: with a query's codes a_d =
- * round(q_d / u), u = amax |q_d| / 127 (as a block's scale), and the block's bounds,
+ * round(q_d / u), u its scale (as a block's in int8), and the block's bounds,
  *   score = bound_scale * max_h u_h * sum_d (a_d > 0 ? a_d largest_d : a_d least_d).
  * max_rows (host, at most max_pages * page_size) bounds the rows of every sequence;
  * one that holds more attends those of its whole blocks that lie below max_rows.

@@ -43,7 +43,8 @@ struct BlockArgs {
   void* out;
   const void* k_new;  // a step's token, [n][Hkv][d]; NULL: the launch only attends
   const void* v_new;
-  int n, Hq, Hkv, G, n_slots, n_pages, page_shift, block_shift, max_pages, max_rows, per_unit, chosen, list_ld, out_bf16;
+  int n, Hq, Hkv, G, n_slots, n_pages, page_shift, block_shift, max_pages, max_rows, chosen, list_ld, out_bf16;
+  int waves, target, max_items;  // the cut (paged_cut.h)
   int sink, recent, best;  // selection: rows, rows, blocks
   float scale2, scale2_lo;
 };
@@ -77,10 +78,83 @@ __device__ __forceinline__ int block_at(const BlockArgs& a, int slot, int g, int
   return (int)((((int64_t)page * a.Hkv + g) << per) + (block & ((1 << per) - 1)));
 }
 
+// Where the blocks of a call's units are cut.  Work item u < units is unit u's newest
+// block; the others are shares of the blocks before it: unit (b, g) has `items` of them
+// from item0 + g items on.
+struct BlockCut {
+  BlockSeq s;
+  int b, items, item0, blocks;  // blocks to read of a unit: all, or of the longest selection
+};
+
+// The whole blocks of sequence b.
+__device__ __forceinline__ int blocks_of(const BlockArgs& a, int b) {
+  const int slot = a.slot_ids[b];
+  const bool ok = slot >= 0 && slot < a.n_slots;
+  const int r = a.rows[ok ? slot : 0];  // no branch: the loads of several sequences go out together
+  return !ok || r < 0 ? 0 : (r < a.max_rows ? r : a.max_rows) >> a.block_shift;
+}
+
+// Called by a whole wave.  by_item: the sequence that holds item `key`; otherwise
+// sequence `key`.  false: there is none.
+__device__ __forceinline__ bool block_cut(const BlockArgs& a, int key, bool by_item, BlockCut& c) {
+  const int lane = tid() & 63;
+  const int units = a.n * a.Hkv;
+  if (a.list) {  // selections are about as long as one another: the same items each
+    const int each = a.max_items / units;
+    c.b = by_item ? (key - units) / (each * a.Hkv) : key;
+    c.items = each;
+    c.item0 = units + c.b * a.Hkv * each;
+    return c.b < a.n;
+  }
+  int64_t mine = 0;
+  int nb0 = 0;
+#pragma unroll 4
+  for (int b0 = 0; b0 < a.n; b0 += 64) {
+    const int b = b0 + lane, nb = b < a.n ? blocks_of(a, min(b, a.n - 1)) : 0;
+    if (b0 == 0) nb0 = nb;
+    mine += nb;
+  }
+  const int64_t total = wave_total((int)(mine & 0xfffff)) + ((int64_t)wave_total((int)(mine >> 20)) << 20);
+  const int C = paged_chunk(a.waves, a.target, a.n, a.Hkv, total,
+                            [&](int x) { return wave_total(x > 0 ? (nb0 + x - 1) / x : 0); });
+  int before = units;
+  for (int b0 = 0; b0 < a.n; b0 += 64) {
+    const int b = b0 + lane, nb = b < a.n ? blocks_of(a, min(b, a.n - 1)) : 0, ni = (nb + C - 1) / C;
+    const int si = wave_scan(ni), first = before + a.Hkv * (si - ni);
+    const bool here = b < a.n && (by_item ? key >= first && key < first + a.Hkv * ni : key == b);
+    const uint64_t m = __builtin_amdgcn_ballot_w64(here);
+    if (m) {
+      const int at = __builtin_ctzll(m);
+      c.b = b0 + at;
+      c.items = __builtin_amdgcn_readlane(ni, at);
+      c.item0 = __builtin_amdgcn_readlane(first, at);
+      return debug_check(c.item0 + a.Hkv * c.items <= units + a.max_items, kDbgPagedItem);
+    }
+    before += a.Hkv * __builtin_amdgcn_readlane(si, 63);
+  }
+  return false;
+}
+
+// A loaded value is waited for here.  Before a loop, and behind a branch in one: where
+// the compiler sees a load that may be in flight as the loop comes round, it waits at the
+// value's use, every time, for all loads in flight.
+template <typename T>
+__device__ __forceinline__ void settle(T& v) {
+  asm volatile("" : "+v"(v));
+}
+
+template <bool NT, typename T>
+__device__ __forceinline__ T load_as(const void* p) {
+  if constexpr (NT)
+    return __builtin_nontemporal_load((const T*)p);
+  else
+    return *(const T*)p;
+}
+
 // ---------------------------------------------------------------- codes
 constexpr float kLeastScale = 0x1p-126f;
 __device__ __forceinline__ float block_scale(uint32_t amax_bf16, float top) {
-  const float s = bf16_bits_to_f32(amax_bf16) / top;
+  const float s = bf16_bits_to_f32(amax_bf16) * (1.f / top);
   return amax_bf16 == 0 ? 1.f : fmaxf(s, kLeastScale);
 }
 
@@ -497,9 +571,8 @@ struct Soft {
 #pragma unroll
     for (int c = 0; c < VE; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  // products x of eight rows at xs a unit (xlo: its low part), values vw (two bf16 a
-  // word) at vs
-  __device__ __forceinline__ void add(const float (&x)[8], float xs, float xlo, const uint32_t (&vw)[8][VE / 2], float vs) {
+  // products x of eight rows at xs a unit (xlo: its low part) -> probabilities times vs
+  __device__ __forceinline__ void softmax(const float (&x)[8], float xs, float xlo, float vs, float (&pe)[8]) {
     float bm = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
     bm = fmaxf(bm, __shfl_xor(bm, 16));
     bm = fmaxf(bm, __shfl_xor(bm, 32));
@@ -513,12 +586,14 @@ struct Soft {
       m = mnew;
       mref = m == -INFINITY ? 0.f : m;
     }
-    float pe[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) pe[i] = fast_exp2(fmaf(x[i], xs, fmaf(x[i], xlo, -mref)));
     lsum += ((pe[0] + pe[1]) + (pe[2] + pe[3])) + ((pe[4] + pe[5]) + (pe[6] + pe[7]));
 #pragma unroll
     for (int i = 0; i < 8; ++i) pe[i] *= vs;
+  }
+  // their sum over the rows' values (two bf16 a word)
+  __device__ __forceinline__ void values(float (&pe)[8], const uint32_t (&vw)[8][VE / 2]) {
     bf16x8 p[3];
     three_terms(pe, p);
 #pragma unroll
@@ -534,22 +609,20 @@ struct Soft {
   }
 };
 
-template <int D, int KIND>
+template <int D, int KIND, bool NT>
 __global__ __launch_bounds__(64) void block_attn(BlockArgs a) {
   constexpr int E = KIND == kRowsBf16 ? 2 : 1, VE = D / 16;
   constexpr int NK = D * E / 64;
   typedef uint32_t VRaw __attribute__((ext_vector_type(VE * E / 4)));
   typedef uint32_t VTail __attribute__((ext_vector_type(VE * 2 / 4)));
   const int lane = tid() & 63, l16 = lane & 15, lg = lane >> 4, item = bid_x(), units = a.n * a.Hkv, B = 1 << a.block_shift;
-  const bool own_block = item < units;
-  const int unit = own_block ? item : (item - units) / a.per_unit, chunk = own_block ? 0 : (item - units) % a.per_unit;
-  const int b = unit / a.Hkv, g = unit % a.Hkv;
-  const BlockSeq s = block_seq(a, b);
-  const bool hval = l16 < a.G;
-  const unsigned char* qp = (const unsigned char*)a.q + ((size_t)b * a.Hq + g * a.G + (hval ? l16 : 0)) * D * 2;
+  const bool own_block = item < units, hval = l16 < a.G;
   Soft<D> o;
   o.init();
   if (own_block) {
+    const int unit = item, b = unit / a.Hkv, g = unit % a.Hkv;
+    const BlockSeq s = block_seq(a, b);
+    const unsigned char* qp = (const unsigned char*)a.q + ((size_t)b * a.Hq + g * a.G + (hval ? l16 : 0)) * D * 2;
     const int T = s.row >> a.block_shift, at = s.row < 0 ? -1 : uniform(block_at(a, s.slot, g, T));
     if (at >= 0) {
       const int newest = s.row & (B - 1);
@@ -566,13 +639,23 @@ __global__ __launch_bounds__(64) void block_attn(BlockArgs a) {
           const int ra = r0 + l16, rb = ra + 16;
           const unsigned char* pa = ra >= newest ? kn : kb + ra * (D * 2);  // (rows past the newest are masked)
           const unsigned char* pb = rb >= newest ? kn : kb + rb * (D * 2);
+          u32x4 k0[D / 32], k1[D / 32];
+#pragma unroll
+          for (int j = 0; j < D / 32; ++j) {
+            k0[j] = *(const u32x4*)(pa + 64 * j + 16 * lg);
+            k1[j] = *(const u32x4*)(pb + 64 * j + 16 * lg);
+          }
+          VTail v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int r = r0 + (i < 4 ? 0 : 16) + 4 * lg + (i & 3);
+            v[i] = *(const VTail*)((r >= newest ? vn : vb + r * (D * 2)) + l16 * (VE * 2));
+          }
           f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int j = 0; j < D / 32; ++j) {
-            s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, *(const u32x4*)(pa + 64 * j + 16 * lg)),
-                                                         __builtin_bit_cast(bf16x8, q[j]), s0, 0, 0, 0);
-            s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, *(const u32x4*)(pb + 64 * j + 16 * lg)),
-                                                         __builtin_bit_cast(bf16x8, q[j]), s1, 0, 0, 0);
+            s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k0[j]), __builtin_bit_cast(bf16x8, q[j]), s0, 0, 0, 0);
+            s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k1[j]), __builtin_bit_cast(bf16x8, q[j]), s1, 0, 0, 0);
           }
           float x[8];
           uint32_t vw[8][VE / 2];
@@ -580,12 +663,13 @@ __global__ __launch_bounds__(64) void block_attn(BlockArgs a) {
           for (int i = 0; i < 8; ++i) {
             const int r = r0 + (i < 4 ? 0 : 16) + 4 * lg + (i & 3);
             x[i] = r <= newest ? (i < 4 ? s0[i & 3] : s1[i & 3]) : -INFINITY;
-            VTail v = *(const VTail*)((r >= newest ? vn : vb + r * (D * 2)) + l16 * (VE * 2));
-            if (r > newest) v = VTail{};
+            if (r > newest) v[i] = VTail{};
 #pragma unroll
-            for (int u = 0; u < VE / 2; ++u) vw[i][u] = v[u];
+            for (int u = 0; u < VE / 2; ++u) vw[i][u] = v[i][u];
           }
-          o.add(x, a.scale2, a.scale2_lo, vw, 1.f);
+          float pe[8];
+          o.softmax(x, a.scale2, a.scale2_lo, 1.f, pe);
+          o.values(pe, vw);
         }
       }
       if (a.k_new && s.row < a.max_pages << a.page_shift) {
@@ -599,60 +683,141 @@ __global__ __launch_bounds__(64) void block_attn(BlockArgs a) {
       }
     }
   } else {
+    BlockCut c;
+    if (!block_cut(a, item, true, c)) return;
+    const int local = item - c.item0, g = local / c.items, chunk = local % c.items, b = c.b, unit = b * a.Hkv + g;
+    const int slot = uniform(a.slot_ids[b]);
     const int32_t* list = a.list ? a.list + (size_t)unit * a.list_ld : nullptr;
-    const int nb = a.list ? uniform(a.count[unit]) : s.blocks;
-    const int e0 = (int)((int64_t)chunk * nb / a.per_unit), e1 = (int)((int64_t)(chunk + 1) * nb / a.per_unit);
+    const int nb = a.list ? uniform(a.count[unit]) : uniform(blocks_of(a, b));
+    const int e0 = (int)((int64_t)chunk * nb / c.items), e1 = (int)((int64_t)(chunk + 1) * nb / c.items);
+    const unsigned char* qp = (const unsigned char*)a.q + ((size_t)b * a.Hq + g * a.G + (hval ? l16 : 0)) * D * 2;
     u32x4 q[D / 32];
 #pragma unroll
     for (int j = 0; j < D / 32; ++j) {
       const int off = KIND == kRowsBf16 ? 64 * j + 16 * lg : (64 * (j / 2) + 16 * lg + 8 * (j & 1)) * 2;
       q[j] = hval ? *(const u32x4*)(qp + off) : u32x4{0u, 0u, 0u, 0u};
     }
-    for (int e = e0; e < e1; ++e) {
-      const int at = uniform(block_at(a, s.slot, g, list ? list[e] : e));
-      if (at < 0) continue;
-      const float ksc = KIND == kRowsBf16 ? 1.f : a.ks[at], vsc = KIND == kRowsBf16 ? 1.f : a.vs[at];
-      const float xs = a.scale2 * ksc, xlo = a.scale2_lo * ksc;
-      for (int r0 = 0; r0 < B; r0 += 32) {
-        const size_t p0 = (((size_t)at << a.block_shift) + r0) * (D * E);
-        const unsigned char* kp = a.ck + p0 + l16 * (D * E) + 16 * lg;
-        const unsigned char* vp = a.cv + p0 + 4 * lg * (D * E) + l16 * (VE * E);
-        f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+    // The next 64 blocks of the item, one a lane: place and scales.  Those whose pages are
+    // not there have no bit in `left`.
+    int at, e = e0, sub = 0;
+    float ksc = 1.f, vsc = 1.f;
+    uint64_t left = 0;
+    auto look = [&]() {
+      const int i = e + lane;
+      at = i < e1 ? block_at(a, slot, g, list ? list[i] : i) : -1;
+      if constexpr (KIND != kRowsBf16) {
+        ksc = a.ks[max(at, 0)];
+        vsc = a.vs[max(at, 0)];
+      }
+      left = __builtin_amdgcn_ballot_w64(at >= 0);
+    };
+    // to the next 32 rows; false: there are none
+    auto next = [&]() {
+      if (left && sub + 32 < B) {
+        sub += 32;
+        return true;
+      }
+      sub = 0;
+      left &= left - 1;
+      while (!left && (e += 64) < e1) {
+        look();
+        settle(at);
+        settle(ksc);
+        settle(vsc);
+      }
+      return left != 0;
+    };
+    auto load_k = [&](const unsigned char* kp, u32x4 (&k0)[NK], u32x4 (&k1)[NK]) {
 #pragma unroll
-        for (int j = 0; j < NK; ++j) {
-          const u32x4 k0 = *(const u32x4*)(kp + 64 * j), k1 = *(const u32x4*)(kp + 16 * (D * E) + 64 * j);
-          if constexpr (KIND == kRowsBf16) {
-            s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k0), __builtin_bit_cast(bf16x8, q[j]), s0, 0, 0, 0);
-            s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k1), __builtin_bit_cast(bf16x8, q[j]), s1, 0, 0, 0);
-          } else {
+      for (int j = 0; j < NK; ++j) {
+        k0[j] = load_as<NT, u32x4>(kp + 64 * j);
+        k1[j] = load_as<NT, u32x4>(kp + 16 * (D * E) + 64 * j);
+      }
+    };
+    const int koff = l16 * (D * E) + 16 * lg, voff = 4 * lg * (D * E) + l16 * (VE * E);
+    // the row of the 32 that are next, and their scales
+    auto row = [&]() {
+      return ((size_t)(uint32_t)__builtin_amdgcn_readlane(at, __builtin_ctzll(left)) << a.block_shift) + sub;
+    };
+    auto of = [&](float v) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), __builtin_ctzll(left))); };
+    bool more = false;
+    if (e0 < e1) {
+      look();
+      more = left != 0;
+      if (!more) {
+        left = 0;
+        more = next();
+      }
+    }
+    u32x4 k0[NK], k1[NK];
+    size_t r = 0;
+    float xk = 1.f, xv = 1.f;
+    if (more) {
+      r = row();
+      load_k(a.ck + r * (D * E) + koff, k0, k1);
+      xk = of(ksc);
+      xv = of(vsc);
+    }
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const bf16x8 qq = __builtin_bit_cast(bf16x8, q[2 * j + u]);
-              const u32x2 a0 = bf16x4<KIND>(k0[2 * u]), a1 = bf16x4<KIND>(k0[2 * u + 1]);
-              const u32x2 b0 = bf16x4<KIND>(k1[2 * u]), b1 = bf16x4<KIND>(k1[2 * u + 1]);
-              s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{a0[0], a0[1], a1[0], a1[1]}), qq, s0, 0, 0, 0);
-              s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{b0[0], b0[1], b1[0], b1[1]}), qq, s1, 0, 0, 0);
-            }
+    for (int j = 0; j < D / 32; ++j) settle(q[j]);
+    settle(ksc);
+    settle(vsc);
+    while (more) {
+      // values of these rows, then keys of the next: the second product waits for the
+      // values only
+      VRaw v[8];
+      const unsigned char* vp = a.cv + r * (D * E) + voff;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = load_as<NT, VRaw>(vp + ((i < 4 ? 0 : 16) + (i & 3)) * (D * E));
+      const float xs = a.scale2 * xk, xlo = a.scale2_lo * xk, vs = xv;
+      u32x4 n0[NK], n1[NK];
+      more = next();
+      if (more) {
+        r = row();
+        load_k(a.ck + r * (D * E) + koff, n0, n1);
+        xk = of(ksc);
+        xv = of(vsc);
+      }
+      f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < NK; ++j) {
+        if constexpr (KIND == kRowsBf16) {
+          s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k0[j]), __builtin_bit_cast(bf16x8, q[j]), s0, 0, 0, 0);
+          s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k1[j]), __builtin_bit_cast(bf16x8, q[j]), s1, 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const bf16x8 qq = __builtin_bit_cast(bf16x8, q[2 * j + u]);
+            const u32x2 a0 = bf16x4<KIND>(k0[j][2 * u]), a1 = bf16x4<KIND>(k0[j][2 * u + 1]);
+            const u32x2 b0 = bf16x4<KIND>(k1[j][2 * u]), b1 = bf16x4<KIND>(k1[j][2 * u + 1]);
+            s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{a0[0], a0[1], a1[0], a1[1]}), qq, s0, 0, 0, 0);
+            s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{b0[0], b0[1], b1[0], b1[1]}), qq, s1, 0, 0, 0);
           }
         }
-        const float x[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
-        uint32_t vw[8][VE / 2];
+      }
+      const float x[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
+      float pe[8];
+      o.softmax(x, xs, xlo, vs, pe);
+      uint32_t vw[8][VE / 2];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const VRaw v = *(const VRaw*)(vp + ((i < 4 ? 0 : 16) + (i & 3)) * (D * E));
-          if constexpr (KIND == kRowsBf16) {
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (KIND == kRowsBf16) {
 #pragma unroll
-            for (int u = 0; u < VE / 2; ++u) vw[i][u] = v[u];
-          } else {
+          for (int u = 0; u < VE / 2; ++u) vw[i][u] = v[i][u];
+        } else {
 #pragma unroll
-            for (int u = 0; u < VE / 4; ++u) {
-              const u32x2 c = bf16x4<KIND>(v[u]);
-              vw[i][2 * u] = c[0];
-              vw[i][2 * u + 1] = c[1];
-            }
+          for (int u = 0; u < VE / 4; ++u) {
+            const u32x2 w = bf16x4<KIND>(v[i][u]);
+            vw[i][2 * u] = w[0];
+            vw[i][2 * u + 1] = w[1];
           }
         }
-        o.add(x, xs, xlo, vw, vsc);
+      }
+      o.values(pe, vw);
+#pragma unroll
+      for (int j = 0; j < NK; ++j) {
+        k0[j] = n0[j];
+        k1[j] = n1[j];
       }
     }
   }
@@ -670,25 +835,62 @@ __global__ __launch_bounds__(64) void block_attn(BlockArgs a) {
 }
 
 // ---------------------------------------------------------------- join
+// A workgroup for each (sequence, query head): thread t takes dims 4 (t % DG) .. + 3 of
+// items t / DG, t / DG + CL, ...  Item 0 is the newest block's.
+constexpr int kJoinThreads = 256;
 template <int D>
-__global__ __launch_bounds__(D) void block_join(BlockArgs a) {
-  const int bh = bid_x(), b = bh / a.Hq, qh = bh % a.Hq, g = qh / a.G, h = qh % a.G, units = a.n * a.Hkv, unit = b * a.Hkv + g;
-  const int t = tid();
-  auto item = [&](int i) { return (size_t)(i == 0 ? unit : units + unit * a.per_unit + i - 1) * a.G + h; };
-  float M = -INFINITY, L = 0.f, o = 0.f;
-  for (int i = 0; i <= a.per_unit; ++i) M = fmaxf(M, a.ml[item(i)].x);
-  for (int i = 0; i <= a.per_unit; ++i) {
-    const float2 v = a.ml[item(i)];
-    if (v.x == -INFINITY) continue;
-    const float f = fast_exp2(v.x - M);
-    L = fmaf(f, v.y, L);
-    o = fmaf(f, a.part[item(i) * D + t], o);
+__global__ __launch_bounds__(kJoinThreads) void block_join(BlockArgs a) {
+  constexpr int DG = D / 4, CL = kJoinThreads / DG, kHeld = 4;
+  __shared__ f32x4 sacc[kJoinThreads];
+  const int bh = bid_x(), b = bh / a.Hq, qh = bh % a.Hq, g = qh / a.G, h = qh % a.G, unit = b * a.Hkv + g;
+  const int t = tid(), lane = t & 63, dg = t % DG, cl = t / DG;
+  BlockCut c;
+  if (!block_cut(a, b, false, c)) return;
+  const int items = c.items + 1;
+  auto place = [&](int i) { return (size_t)(i == 0 ? unit : c.item0 + g * c.items + i - 1) * a.G + h; };
+  // the first partials of the thread are in flight with the references
+  f32x4 held[kHeld];
+  float mheld[kHeld];
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    const size_t pi = place(min(cl + j * CL, items - 1));
+    held[j] = *(const f32x4*)(a.part + pi * D + 4 * dg);
+    mheld[j] = a.ml[pi].x;
   }
-  o = L > 0.f ? o / L : 0.f;
+  float m = -INFINITY, l = 0.f;
+  for (int i = lane; i < items; i += 64) {
+    const float2 v = a.ml[place(i)];
+    const float mn = fmaxf(m, v.x);
+    if (mn != -INFINITY) l = l * fast_exp2(m - mn) + v.y * fast_exp2(v.x - mn);
+    m = mn;
+  }
+  float M = m;
+#pragma unroll
+  for (int x = 32; x >= 1; x >>= 1) M = fmaxf(M, __shfl_xor(M, x));
+  const float L = warp_sum(m == -INFINITY ? 0.f : l * fast_exp2(m - M));
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  // (an item without a row holds zeros)
+  auto add = [&](f32x4 v, float mi) { o += v * (mi == -INFINITY ? 0.f : fast_exp2(mi - M)); };
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j)
+    if (cl + j * CL < items) add(held[j], mheld[j]);
+#pragma unroll 4
+  for (int i = cl + kHeld * CL; i < items; i += CL) {
+    const size_t pi = place(i);
+    add(*(const f32x4*)(a.part + pi * D + 4 * dg), a.ml[pi].x);
+  }
+  sacc[t] = o;
+  __syncthreads();
+  if (cl) return;
+#pragma unroll
+  for (int i = 1; i < CL; ++i) o += sacc[dg + DG * i];
+  o *= L > 0.f ? 1.f / L : 0.f;
+  const size_t oi = (size_t)bh * D + 4 * dg;
   if (a.out_bf16)
-    ((uint16_t*)a.out)[(size_t)bh * D + t] = (uint16_t)f32_to_bf16_bits(o);
+    *(u32x2*)((uint16_t*)a.out + oi) = u32x2{f32_to_bf16_bits(o[0]) | (f32_to_bf16_bits(o[1]) << 16),
+                                             f32_to_bf16_bits(o[2]) | (f32_to_bf16_bits(o[3]) << 16)};
   else
-    ((float*)a.out)[(size_t)bh * D + t] = o;
+    *(f32x4*)((float*)a.out + oi) = o;
 }
 
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -732,21 +934,25 @@ int block_chosen(const snap_params& p, int block) {
   return (p.sink + block - 1) / block + (p.recent - 1 + block - 1) / block + (p.topk + block - 1) / block;
 }
 
+// Work items that the card holds at once, by the registers of a wave (two a SIMD).
 constexpr int kResident = 2048;
 BlockGeometry block_geometry(const snap_params& p, int n, int max_rows, int block, bool select) {
   BlockGeometry g{};
   const int units = (n > 0 ? n : 1) * p.n_kv_heads, G = p.n_q_heads / p.n_kv_heads;
   g.blocks = max_rows / block;
   g.chosen = block_chosen(p, block);
-  const int most = g.blocks < 1 ? 1 : g.blocks, read = select && g.chosen < most ? (g.chosen < 1 ? 1 : g.chosen) : most;
-  g.list_ld = g.chosen < most ? g.chosen : most;
-  g.per_unit = kResident / units;
-  if (g.per_unit < 1) g.per_unit = 1;
-  if (g.per_unit > read) g.per_unit = read;
-  // a bound that does not fall as sequences or rows grow
-  const int64_t codes = (int64_t)units * most < (units > kResident ? units : kResident) ? (int64_t)units * most
-                                                                                        : (units > kResident ? units : kResident);
-  const size_t items = (size_t)units + (size_t)codes;
+  const int most = g.blocks < 1 ? 1 : g.blocks;
+  g.list_ld = g.chosen < most ? (g.chosen < 1 ? 1 : g.chosen) : most;
+  (PagedCut&)g = paged_cut(units, kResident, (int64_t)units * most);
+  size_t items = (size_t)units + g.max_items;
+  if (select) {  // the same items for every unit
+    int each = kResident / units;
+    each = each < 1 ? 1 : (each > g.list_ld ? g.list_ld : each);
+    g.max_items = units * each;
+    // (a bound that does not fall as sequences or rows grow, and serves calls without)
+    const int64_t bound = units > kResident ? units : kResident;
+    items += (size_t)((int64_t)units * most < bound ? (int64_t)units * most : bound);
+  }
   size_t off = 0;
   g.off_part = off;
   off = align256(off + items * G * p.d_v * sizeof(float));
@@ -794,7 +1000,9 @@ snap_status launch_block_decode(const snap_params& p, const snap_block_cache& c,
   a.ml = (float2*)((unsigned char*)ws + geo.off_ml);
   a.out = out;
   a.max_rows = max_rows;
-  a.per_unit = geo.per_unit;
+  a.waves = geo.waves;
+  a.target = geo.target;
+  a.max_items = geo.max_items;
   a.chosen = geo.chosen;
   a.list_ld = geo.list_ld;
   a.out_bf16 = out_dtype == SNAP_BF16;
@@ -811,12 +1019,18 @@ snap_status launch_block_decode(const snap_params& p, const snap_block_cache& c,
     hipLaunchKernelGGL((p.d_qk == 128 ? block_select<128> : block_select<64>), dim3(units), dim3(kSelThreadsB), lds, stream, a);
     if (hipGetLastError() != hipSuccess) return SNAP_ERR_HIP;
   }
-  static constexpr void (*kernels[2][3])(BlockArgs) = {
-      {block_attn<64, kRowsBf16>, block_attn<64, kRowsFp8>, block_attn<64, kRowsInt8>},
-      {block_attn<128, kRowsBf16>, block_attn<128, kRowsFp8>, block_attn<128, kRowsInt8>}};
-  hipLaunchKernelGGL(kernels[p.d_qk == 128][kind_of(p.kv_dtype)], dim3(units + units * geo.per_unit), dim3(64), 0, stream, a);
+  // streaming loads where the blocks read are more than half the last-level cache
+  const size_t row_bytes = (size_t)2 * p.d_qk * (p.kv_dtype == SNAP_BF16 ? 2 : 1);
+  const size_t call_bytes = (size_t)units * (select ? geo.list_ld : geo.blocks) * c.block * row_bytes;
+  const bool nt = p.kv_reuse == SNAP_KV_STREAM || (p.kv_reuse == SNAP_KV_AUTO && call_bytes >= (size_t)128 << 20);
+#define SNAP_BLOCK_ATTN(D) \
+  {{block_attn<D, kRowsBf16, false>, block_attn<D, kRowsFp8, false>, block_attn<D, kRowsInt8, false>}, \
+   {block_attn<D, kRowsBf16, true>, block_attn<D, kRowsFp8, true>, block_attn<D, kRowsInt8, true>}}
+  static constexpr void (*kernels[2][2][3])(BlockArgs) = {SNAP_BLOCK_ATTN(64), SNAP_BLOCK_ATTN(128)};  // [width][NT][rows]
+#undef SNAP_BLOCK_ATTN
+  hipLaunchKernelGGL(kernels[p.d_qk == 128][nt][kind_of(p.kv_dtype)], dim3(units + geo.max_items), dim3(64), 0, stream, a);
   if (hipGetLastError() != hipSuccess) return SNAP_ERR_HIP;
-  hipLaunchKernelGGL((p.d_qk == 128 ? block_join<128> : block_join<64>), dim3(n * p.n_q_heads), dim3(p.d_qk), 0, stream, a);
+  hipLaunchKernelGGL((p.d_qk == 128 ? block_join<128> : block_join<64>), dim3(n * p.n_q_heads), dim3(kJoinThreads), 0, stream, a);
   return hipGetLastError() == hipSuccess ? SNAP_OK : SNAP_ERR_HIP;
 }
 

@@ -315,11 +315,10 @@ snap_status launch_pages_map(const snap_page_pool& c, const int32_t* rows, const
                              int32_t* seq_of, int32_t* row_of, int32_t* pos_of, hipStream_t stream);
 
 // Block decode: work items of a call and its workspace.
-struct BlockGeometry {
-  int blocks;    // whole blocks of a sequence at most
-  int chosen;    // blocks that a selection lists at most
-  int list_ld;   // of which there are at most this many
-  int per_unit;  // work items of a (sequence, KV head), beside the newest token's block
+struct BlockGeometry : PagedCut {
+  int blocks;   // whole blocks of a sequence at most
+  int chosen;   // blocks that a selection lists at most
+  int list_ld;  // of which there are at most this many
   size_t off_part, off_ml, off_list, off_count, bytes;
 };
 constexpr int kBlockMost = 32768;  // blocks that one workgroup selects among (their scores in LDS)

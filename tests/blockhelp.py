@@ -35,7 +35,7 @@ def amax(x):
 
 def scale_of(x, top):
     m = amax(x)
-    s = (m / torch.tensor(top, dtype=torch.float32)).clamp(min=2.0 ** -126)
+    s = (m * (1.0 / torch.tensor(top, dtype=torch.float32))).clamp(min=2.0 ** -126)
     return torch.where(m == 0, torch.ones_like(s), s)
 
 
