@@ -37,8 +37,7 @@ struct BlockArgs {
   const int32_t* table;
   float* part;     // [items][G][d]
   float2* ml;      // [items][G]  (max in log2 units, sum)
-  int32_t* list;   // [units][list_ld] selected blocks, ascending; NULL: all
-  int32_t* count;  // [units]
+  int32_t* list;   // [units][list_ld] places of the selected blocks, ascending by block, then -1; NULL: all
   int32_t* sel_out;
   void* out;
   const void* k_new;  // a step's token, [n][Hkv][d]; NULL: the launch only attends
@@ -78,12 +77,10 @@ __device__ __forceinline__ int block_at(const BlockArgs& a, int slot, int g, int
   return (int)((((int64_t)page * a.Hkv + g) << per) + (block & ((1 << per) - 1)));
 }
 
-// Where the blocks of a call's units are cut.  Work item u < units is unit u's newest
-// block; the others are shares of the blocks before it: unit (b, g) has `items` of them
-// from item0 + g items on.
+// Where the blocks of a call's units are cut: unit (b, g) has `items` work items from
+// item0 + g items on.
 struct BlockCut {
-  BlockSeq s;
-  int b, items, item0, blocks;  // blocks to read of a unit: all, or of the longest selection
+  int b, items, item0;
 };
 
 // The whole blocks of sequence b.
@@ -98,12 +95,10 @@ __device__ __forceinline__ int blocks_of(const BlockArgs& a, int b) {
 // sequence `key`.  false: there is none.
 __device__ __forceinline__ bool block_cut(const BlockArgs& a, int key, bool by_item, BlockCut& c) {
   const int lane = tid() & 63;
-  const int units = a.n * a.Hkv;
   if (a.list) {  // selections are about as long as one another: the same items each
-    const int each = a.max_items / units;
-    c.b = by_item ? (key - units) / (each * a.Hkv) : key;
-    c.items = each;
-    c.item0 = units + c.b * a.Hkv * each;
+    c.items = a.max_items / (a.n * a.Hkv);
+    c.b = by_item ? key / (c.items * a.Hkv) : key;
+    c.item0 = c.b * a.Hkv * c.items;
     return c.b < a.n;
   }
   int64_t mine = 0;
@@ -117,7 +112,7 @@ __device__ __forceinline__ bool block_cut(const BlockArgs& a, int key, bool by_i
   const int64_t total = wave_total((int)(mine & 0xfffff)) + ((int64_t)wave_total((int)(mine >> 20)) << 20);
   const int C = paged_chunk(a.waves, a.target, a.n, a.Hkv, total,
                             [&](int x) { return wave_total(x > 0 ? (nb0 + x - 1) / x : 0); });
-  int before = units;
+  int before = 0;
   for (int b0 = 0; b0 < a.n; b0 += 64) {
     const int b = b0 + lane, nb = b < a.n ? blocks_of(a, min(b, a.n - 1)) : 0, ni = (nb + C - 1) / C;
     const int si = wave_scan(ni), first = before + a.Hkv * (si - ni);
@@ -128,7 +123,7 @@ __device__ __forceinline__ bool block_cut(const BlockArgs& a, int key, bool by_i
       c.b = b0 + at;
       c.items = __builtin_amdgcn_readlane(ni, at);
       c.item0 = __builtin_amdgcn_readlane(first, at);
-      return debug_check(c.item0 + a.Hkv * c.items <= units + a.max_items, kDbgPagedItem);
+      return debug_check(c.item0 + a.Hkv * c.items <= a.max_items, kDbgPagedItem);
     }
     before += a.Hkv * __builtin_amdgcn_readlane(si, 63);
   }
@@ -284,6 +279,22 @@ __device__ __forceinline__ void put_block(const BlockArgs& a, int at, bool keys,
     }
     if (lane == 0) a.bscale[at] = s;
   }
+}
+
+// A step's token of a unit stored, keys or values: its row in the tail (bf16: the page),
+// and the block's codes and bounds when it is the last of one.
+template <int D, int KIND>
+__device__ __forceinline__ void put_token(const BlockArgs& a, int unit, bool keys) {
+  const int b = unit / a.Hkv, g = unit % a.Hkv, B = 1 << a.block_shift, lane = tid() & 63;
+  const BlockSeq s = block_seq(a, b);
+  if (s.row < 0) return;
+  const int at = uniform(block_at(a, s.slot, g, s.row >> a.block_shift)), newest = s.row & (B - 1);
+  if (at < 0) return;
+  unsigned char* rows = KIND == kRowsBf16 ? (keys ? a.ck : a.cv) + ((size_t)at << a.block_shift) * D * 2
+                                          : (keys ? a.kt : a.vt) + (((size_t)s.slot * a.Hkv + g) << a.block_shift) * D * 2;
+  const unsigned char* in = (const unsigned char*)(keys ? a.k_new : a.v_new) + (size_t)unit * D * 2;
+  if (lane < D / 8) *((u32x4*)(rows + newest * (D * 2)) + lane) = *((const u32x4*)in + lane);
+  if (newest == B - 1) put_block<D, KIND>(a, at, keys, [&](int r) { return r == newest ? in : rows + r * (D * 2); });
 }
 
 // ---------------------------------------------------------------- append
@@ -517,13 +528,13 @@ __global__ __launch_bounds__(kSelThreadsB) void block_select(BlockArgs a) {
     const uint64_t tm = __builtin_amdgcn_ballot_w64(take);
     const int i = at + __builtin_popcountll(tm & below);
     if (take && debug_check(i < a.list_ld, kDbgBlockList)) {
-      list[i] = j;
+      list[i] = block_at(a, s.slot, g, j);
       if (sel) sel[i] = j;
     }
     at += __builtin_popcountll(tm);
     e0 += __builtin_popcountll(me);
   }
-  if (t == 0) a.count[unit] = min(total, a.list_ld);
+  for (int i = total + t; i < a.list_ld; i += kSelThreadsB) list[i] = -1;
   if (sel)
     for (int i = total + t; i < a.chosen; i += kSelThreadsB) sel[i] = -1;
 }
@@ -615,80 +626,74 @@ __global__ __launch_bounds__(64) void block_attn(BlockArgs a) {
   constexpr int NK = D * E / 64;
   typedef uint32_t VRaw __attribute__((ext_vector_type(VE * E / 4)));
   typedef uint32_t VTail __attribute__((ext_vector_type(VE * 2 / 4)));
-  const int lane = tid() & 63, l16 = lane & 15, lg = lane >> 4, item = bid_x(), units = a.n * a.Hkv, B = 1 << a.block_shift;
-  const bool own_block = item < units, hval = l16 < a.G;
+  const int lane = tid() & 63, l16 = lane & 15, lg = lane >> 4, units = a.n * a.Hkv, B = 1 << a.block_shift;
+  const bool hval = l16 < a.G;
+  // Workgroups [0, 2 units) store a step's token, those up to (2 + B / 32) units attend
+  // 32 rows each of the newest token's block, the others a work item each.
+  const int stores = a.k_new ? 2 * units : 0, parts = B >> 5;
+  const int w = bid_x() - stores, item = w - parts * units;
+  if (w < 0) {
+    put_token<D, KIND>(a, bid_x() >> 1, !(bid_x() & 1));
+    return;
+  }
+  size_t place;  // among the partials: a unit's 32-row parts, then the items
   Soft<D> o;
   o.init();
-  if (own_block) {
-    const int unit = item, b = unit / a.Hkv, g = unit % a.Hkv;
+  if (item < 0) {
+    const int unit = w / parts, r0 = w % parts * 32, b = unit / a.Hkv, g = unit % a.Hkv;
     const BlockSeq s = block_seq(a, b);
-    const unsigned char* qp = (const unsigned char*)a.q + ((size_t)b * a.Hq + g * a.G + (hval ? l16 : 0)) * D * 2;
-    const int T = s.row >> a.block_shift, at = s.row < 0 ? -1 : uniform(block_at(a, s.slot, g, T));
+    const int newest = s.row & (B - 1), at = s.tail && r0 <= newest ? uniform(block_at(a, s.slot, g, s.row >> a.block_shift)) : -1;
+    place = w;
     if (at >= 0) {
-      const int newest = s.row & (B - 1);
+      const unsigned char* qp = (const unsigned char*)a.q + ((size_t)b * a.Hq + g * a.G + (hval ? l16 : 0)) * D * 2;
       const size_t t0 = (((size_t)s.slot * a.Hkv + g) << a.block_shift) * D * 2, p0 = ((size_t)at << a.block_shift) * D * 2;
-      unsigned char* kb = KIND == kRowsBf16 ? a.ck + p0 : a.kt + t0;
-      unsigned char* vb = KIND == kRowsBf16 ? a.cv + p0 : a.vt + t0;
+      const unsigned char* kb = KIND == kRowsBf16 ? a.ck + p0 : a.kt + t0;
+      const unsigned char* vb = KIND == kRowsBf16 ? a.cv + p0 : a.vt + t0;
       const unsigned char* kn = a.k_new ? (const unsigned char*)a.k_new + (size_t)unit * D * 2 : kb + newest * (D * 2);
       const unsigned char* vn = a.k_new ? (const unsigned char*)a.v_new + (size_t)unit * D * 2 : vb + newest * (D * 2);
-      if (s.tail) {
-        u32x4 q[D / 32];
+      const int ra = r0 + l16, rb = ra + 16;
+      const unsigned char* pa = ra >= newest ? kn : kb + ra * (D * 2);  // (rows past the newest are masked)
+      const unsigned char* pb = rb >= newest ? kn : kb + rb * (D * 2);
+      u32x4 q[D / 32], k0[D / 32], k1[D / 32];
 #pragma unroll
-        for (int j = 0; j < D / 32; ++j) q[j] = hval ? *(const u32x4*)(qp + 64 * j + 16 * lg) : u32x4{0u, 0u, 0u, 0u};
-        for (int r0 = 0; r0 <= newest; r0 += 32) {
-          const int ra = r0 + l16, rb = ra + 16;
-          const unsigned char* pa = ra >= newest ? kn : kb + ra * (D * 2);  // (rows past the newest are masked)
-          const unsigned char* pb = rb >= newest ? kn : kb + rb * (D * 2);
-          u32x4 k0[D / 32], k1[D / 32];
-#pragma unroll
-          for (int j = 0; j < D / 32; ++j) {
-            k0[j] = *(const u32x4*)(pa + 64 * j + 16 * lg);
-            k1[j] = *(const u32x4*)(pb + 64 * j + 16 * lg);
-          }
-          VTail v[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int r = r0 + (i < 4 ? 0 : 16) + 4 * lg + (i & 3);
-            v[i] = *(const VTail*)((r >= newest ? vn : vb + r * (D * 2)) + l16 * (VE * 2));
-          }
-          f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int j = 0; j < D / 32; ++j) {
-            s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k0[j]), __builtin_bit_cast(bf16x8, q[j]), s0, 0, 0, 0);
-            s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k1[j]), __builtin_bit_cast(bf16x8, q[j]), s1, 0, 0, 0);
-          }
-          float x[8];
-          uint32_t vw[8][VE / 2];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int r = r0 + (i < 4 ? 0 : 16) + 4 * lg + (i & 3);
-            x[i] = r <= newest ? (i < 4 ? s0[i & 3] : s1[i & 3]) : -INFINITY;
-            if (r > newest) v[i] = VTail{};
-#pragma unroll
-            for (int u = 0; u < VE / 2; ++u) vw[i][u] = v[i][u];
-          }
-          float pe[8];
-          o.softmax(x, a.scale2, a.scale2_lo, 1.f, pe);
-          o.values(pe, vw);
-        }
+      for (int j = 0; j < D / 32; ++j) {
+        q[j] = hval ? *(const u32x4*)(qp + 64 * j + 16 * lg) : u32x4{0u, 0u, 0u, 0u};
+        k0[j] = *(const u32x4*)(pa + 64 * j + 16 * lg);
+        k1[j] = *(const u32x4*)(pb + 64 * j + 16 * lg);
       }
-      if (a.k_new && s.row < a.max_pages << a.page_shift) {
-        // the token's row, and the block's codes and bounds when it is the last of one
-        if (lane < D / 8) *((u32x4*)(kb + newest * (D * 2)) + lane) = *((const u32x4*)kn + lane);
-        else if (lane < D / 4) *((u32x4*)(vb + newest * (D * 2)) + lane - D / 8) = *((const u32x4*)vn + lane - D / 8);
-        if (newest == B - 1) {
-          put_block<D, KIND>(a, at, true, [&](int r) { return r == newest ? kn : kb + r * (D * 2); });
-          put_block<D, KIND>(a, at, false, [&](int r) { return r == newest ? vn : vb + r * (D * 2); });
-        }
+      VTail v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = r0 + (i < 4 ? 0 : 16) + 4 * lg + (i & 3);
+        v[i] = *(const VTail*)((r >= newest ? vn : vb + r * (D * 2)) + l16 * (VE * 2));
       }
+      f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) {
+        s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k0[j]), __builtin_bit_cast(bf16x8, q[j]), s0, 0, 0, 0);
+        s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k1[j]), __builtin_bit_cast(bf16x8, q[j]), s1, 0, 0, 0);
+      }
+      float x[8], pe[8];
+      uint32_t vw[8][VE / 2];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = r0 + (i < 4 ? 0 : 16) + 4 * lg + (i & 3);
+        x[i] = r <= newest ? (i < 4 ? s0[i & 3] : s1[i & 3]) : -INFINITY;
+        if (r > newest) v[i] = VTail{};
+#pragma unroll
+        for (int u = 0; u < VE / 2; ++u) vw[i][u] = v[i][u];
+      }
+      o.softmax(x, a.scale2, a.scale2_lo, 1.f, pe);
+      o.values(pe, vw);
     }
   } else {
     BlockCut c;
     if (!block_cut(a, item, true, c)) return;
-    const int local = item - c.item0, g = local / c.items, chunk = local % c.items, b = c.b, unit = b * a.Hkv + g;
+    place = (size_t)parts * units + item;
+    const int local = item - c.item0, g = local / c.items, chunk = local % c.items, b = c.b;
     const int slot = uniform(a.slot_ids[b]);
-    const int32_t* list = a.list ? a.list + (size_t)unit * a.list_ld : nullptr;
-    const int nb = a.list ? uniform(a.count[unit]) : uniform(blocks_of(a, b));
+    const int32_t* list = a.list ? a.list + (size_t)(b * a.Hkv + g) * a.list_ld : nullptr;
+    const int nb = a.list ? a.list_ld : uniform(blocks_of(a, b));
     const int e0 = (int)((int64_t)chunk * nb / c.items), e1 = (int)((int64_t)(chunk + 1) * nb / c.items);
     const unsigned char* qp = (const unsigned char*)a.q + ((size_t)b * a.Hq + g * a.G + (hval ? l16 : 0)) * D * 2;
     u32x4 q[D / 32];
@@ -704,7 +709,7 @@ __global__ __launch_bounds__(64) void block_attn(BlockArgs a) {
     uint64_t left = 0;
     auto look = [&]() {
       const int i = e + lane;
-      at = i < e1 ? block_at(a, slot, g, list ? list[i] : i) : -1;
+      at = i >= e1 ? -1 : (list ? list[i] : block_at(a, slot, g, i));
       if constexpr (KIND != kRowsBf16) {
         ksc = a.ks[max(at, 0)];
         vsc = a.vs[max(at, 0)];
@@ -824,7 +829,7 @@ __global__ __launch_bounds__(64) void block_attn(BlockArgs a) {
   o.lsum += __shfl_xor(o.lsum, 16);
   o.lsum += __shfl_xor(o.lsum, 32);
   if (!hval) return;
-  const size_t pi = (size_t)item * a.G + l16;
+  const size_t pi = place * a.G + l16;
   if (lg == 0) a.ml[pi] = make_float2(o.m, o.lsum);
   float* dst = a.part + pi * D + 4 * lg * VE;
 #pragma unroll
@@ -836,7 +841,7 @@ __global__ __launch_bounds__(64) void block_attn(BlockArgs a) {
 
 // ---------------------------------------------------------------- join
 // A workgroup for each (sequence, query head): thread t takes dims 4 (t % DG) .. + 3 of
-// items t / DG, t / DG + CL, ...  Item 0 is the newest block's.
+// items t / DG, t / DG + CL, ..., after the parts of the newest token's block.
 constexpr int kJoinThreads = 256;
 template <int D>
 __global__ __launch_bounds__(kJoinThreads) void block_join(BlockArgs a) {
@@ -846,8 +851,8 @@ __global__ __launch_bounds__(kJoinThreads) void block_join(BlockArgs a) {
   const int t = tid(), lane = t & 63, dg = t % DG, cl = t / DG;
   BlockCut c;
   if (!block_cut(a, b, false, c)) return;
-  const int items = c.items + 1;
-  auto place = [&](int i) { return (size_t)(i == 0 ? unit : c.item0 + g * c.items + i - 1) * a.G + h; };
+  const int parts = (1 << a.block_shift) >> 5, items = c.items + parts, first = parts * a.n * a.Hkv + c.item0 + g * c.items - parts;
+  auto place = [&](int i) { return (size_t)(i < parts ? parts * unit + i : first + i) * a.G + h; };
   // the first partials of the thread are in flight with the references
   f32x4 held[kHeld];
   float mheld[kHeld];
@@ -944,7 +949,7 @@ BlockGeometry block_geometry(const snap_params& p, int n, int max_rows, int bloc
   const int most = g.blocks < 1 ? 1 : g.blocks;
   g.list_ld = g.chosen < most ? (g.chosen < 1 ? 1 : g.chosen) : most;
   (PagedCut&)g = paged_cut(units, kResident, (int64_t)units * most);
-  size_t items = (size_t)units + g.max_items;
+  size_t items = (size_t)units * (block / 32) + g.max_items;
   if (select) {  // the same items for every unit
     int each = kResident / units;
     each = each < 1 ? 1 : (each > g.list_ld ? g.list_ld : each);
@@ -960,8 +965,6 @@ BlockGeometry block_geometry(const snap_params& p, int n, int max_rows, int bloc
   off = align256(off + items * G * sizeof(float2));
   g.off_list = off;
   if (select) off = align256(off + (size_t)units * g.list_ld * sizeof(int32_t));
-  g.off_count = off;
-  if (select) off = align256(off + (size_t)units * sizeof(int32_t));
   g.bytes = off;
   return g;
 }
@@ -1010,7 +1013,6 @@ snap_status launch_block_decode(const snap_params& p, const snap_block_cache& c,
   const int units = n * p.n_kv_heads;
   if (select) {
     a.list = (int32_t*)((unsigned char*)ws + geo.off_list);
-    a.count = (int32_t*)((unsigned char*)ws + geo.off_count);
     a.sel_out = sel_out;
     a.sink = p.sink;
     a.recent = p.recent;
@@ -1028,7 +1030,8 @@ snap_status launch_block_decode(const snap_params& p, const snap_block_cache& c,
    {block_attn<D, kRowsBf16, true>, block_attn<D, kRowsFp8, true>, block_attn<D, kRowsInt8, true>}}
   static constexpr void (*kernels[2][2][3])(BlockArgs) = {SNAP_BLOCK_ATTN(64), SNAP_BLOCK_ATTN(128)};  // [width][NT][rows]
 #undef SNAP_BLOCK_ATTN
-  hipLaunchKernelGGL(kernels[p.d_qk == 128][nt][kind_of(p.kv_dtype)], dim3(units + geo.max_items), dim3(64), 0, stream, a);
+  hipLaunchKernelGGL(kernels[p.d_qk == 128][nt][kind_of(p.kv_dtype)], dim3(units * ((k_new ? 2 : 0) + c.block / 32) + geo.max_items),
+                     dim3(64), 0, stream, a);
   if (hipGetLastError() != hipSuccess) return SNAP_ERR_HIP;
   hipLaunchKernelGGL((p.d_qk == 128 ? block_join<128> : block_join<64>), dim3(n * p.n_q_heads), dim3(kJoinThreads), 0, stream, a);
   return hipGetLastError() == hipSuccess ? SNAP_OK : SNAP_ERR_HIP;
