@@ -255,16 +255,28 @@ __device__ __forceinline__ void put_block(const BlockArgs& a, int at, bool keys,
   uint32_t m = 0;
   Bounds8 bd;
   bd.init();
-  for (int r = r0; r < B; r += R) {
-    const u32x4 x = *((const u32x4*)row(r) + col);
-    m = amax8(x, m);
-    if (bounds) bd.add(x);
+  constexpr int N = 4;  // pieces in flight (B is a multiple of N R)
+  for (int r = r0; r < B; r += N * R) {
+    u32x4 x[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = *((const u32x4*)row(r + i * R) + col);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      m = amax8(x[i], m);
+      if (bounds) bd.add(x[i]);
+    }
   }
   m = wave_max(m);
   if constexpr (KIND != kRowsBf16) {
     const float s = block_scale(m, KIND == kRowsInt8 ? 127.f : 448.f);
     unsigned char* to = (keys ? a.ck : a.cv) + ((size_t)at << a.block_shift) * D + 8 * col;
-    for (int r = r0; r < B; r += R) *(u32x2*)(to + (size_t)r * D) = codes8<KIND>(*((const u32x4*)row(r) + col), s);
+    for (int r = r0; r < B; r += N * R) {
+      u32x4 x[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = *((const u32x4*)row(r + i * R) + col);
+#pragma unroll
+      for (int i = 0; i < N; ++i) *(u32x2*)(to + (size_t)(r + i * R) * D) = codes8<KIND>(x[i], s);
+    }
     if (lane == 0) (keys ? a.ks : a.vs)[at] = s;
   }
   if (bounds) {
@@ -277,6 +289,128 @@ __device__ __forceinline__ void put_block(const BlockArgs& a, int at, bool keys,
       *(u32x2*)(a.bound + (size_t)at * 2 * D + 8 * col) = least;
       *(u32x2*)(a.bound + (size_t)at * 2 * D + D + 8 * col) = largest;
     }
+    if (lane == 0) a.bscale[at] = s;
+  }
+}
+
+// The same from registers, where every value is finite and of a middling size (else
+// put_block does it): all rows are in flight at once and read once.
+// Two bf16 a word: least and largest in whole numbers whose order is theirs, which give
+// the largest magnitude too (a negative one of magnitude m is the number -1 - m).
+// The quotient x / s of each code is off by 1.5 steps at most when it is x * fl(1 / s):
+// an int8 code is rounded from that (by adding 1.5 * 2^23, whose last byte is then the
+// code) unless it lies next to a tie, where the division is made; an E4M3 code from the
+// quotient itself, which two corrections by the remainder give (a correctly rounded
+// reciprocal and a quotient off by less than a step give it in one).
+constexpr float kRoundMagic = 12582912.f;  // 1.5 * 2^23
+template <int KIND>
+__device__ __forceinline__ u32x2 quick_codes8(u32x4 raw, float scale, float inv) {
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = __uint_as_float(raw[i] << 16);
+    f[2 * i + 1] = __uint_as_float(raw[i] & 0xffff0000u);
+  }
+  if constexpr (KIND == kRowsInt8) {
+    uint32_t c[8];
+    float off = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float r = fmaf(f[i], inv, kRoundMagic);
+      c[i] = __float_as_uint(r);
+      off = fmaxf(off, fabsf(fmaf(f[i], inv, kRoundMagic - r)));
+    }
+    u32x2 w;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      w[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(c[4 * i + 3], c[4 * i + 2], 0x0c0c0400u),
+                                   __builtin_amdgcn_perm(c[4 * i + 1], c[4 * i], 0x0c0c0400u), 0x05040100u);
+    if (wave_any(off > 0.5f - 0x1p-15f)) {
+      const u32x2 e = codes8<KIND>(raw, scale);
+      if (off > 0.5f - 0x1p-15f) w = e;
+    }
+    return w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float y = f[i] * inv;
+      y = fmaf(fmaf(-scale, y, f[i]), inv, y);
+      f[i] = fmaf(fmaf(-scale, y, f[i]), inv, y);
+    }
+    u32x2 w;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      e4m3_v2i16 r = {0, 0};
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, f[4 * i], f[4 * i + 1], 1.0f, false);
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, f[4 * i + 2], f[4 * i + 3], 1.0f, true);
+      w[i] = __builtin_bit_cast(uint32_t, r);
+    }
+    return w;
+  }
+}
+
+template <int D, int KIND, int B, typename Row>
+__device__ __forceinline__ void put_block_at_once(const BlockArgs& a, int at, bool keys, Row row) {
+  constexpr int P = D / 8, R = 64 / P, NP = B / R;
+  const int lane = tid() & 63, col = lane % P, r0 = lane / P;
+  const bool bounds = keys && a.bound;
+  if (KIND == kRowsBf16 && !bounds) return;
+  u32x4 x[NP];
+#pragma unroll
+  for (int p = 0; p < NP; ++p) x[p] = *((const u32x4*)row(p * R + r0) + col);
+  i16x2 lo[4], hi[4], m = {0, 0};
+  if (bounds) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t raw = x[p][i];  // (a vector's element as such would be cast as its first)
+        const i16x2 h = __builtin_bit_cast(i16x2, raw), k = h ^ ((h >> 15) & (short)0x7fff);
+        lo[i] = p ? __builtin_elementwise_min(lo[i], k) : k;
+        hi[i] = p ? __builtin_elementwise_max(hi[i], k) : k;
+      }
+#pragma unroll
+    for (int o = P; o < 64; o <<= 1)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        lo[i] = __builtin_elementwise_min(lo[i], __builtin_bit_cast(i16x2, __shfl_xor(__builtin_bit_cast(int, lo[i]), o)));
+        hi[i] = __builtin_elementwise_max(hi[i], __builtin_bit_cast(i16x2, __shfl_xor(__builtin_bit_cast(int, hi[i]), o)));
+      }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_elementwise_max(hi[i], ~lo[i]));
+  } else {
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(i16x2, x[p][i] & 0x7fff7fffu));
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) m = __builtin_elementwise_max(m, __builtin_bit_cast(i16x2, __shfl_xor(__builtin_bit_cast(int, m), o)));
+  const int amax = uniform(max((int)m[0], (int)m[1]));
+  // magnitudes of 2^-60 to 2^60
+  if (amax < (127 - 60) << 7 || amax >= (127 + 60) << 7) {
+    put_block<D, KIND>(a, at, keys, row);
+    return;
+  }
+  if constexpr (KIND != kRowsBf16) {
+    const float s = block_scale(amax, KIND == kRowsInt8 ? 127.f : 448.f), inv = 1.f / s;
+    unsigned char* to = (keys ? a.ck : a.cv) + ((size_t)at * B + r0) * D + 8 * col;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) *(u32x2*)(to + p * R * D) = quick_codes8<KIND>(x[p], s, inv);
+    if (lane == 0) (keys ? a.ks : a.vs)[at] = s;
+  }
+  if (bounds && lane < P) {
+    const float s = block_scale(amax, 127.f);
+    Bounds8 bd;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      bd.lo[i] = lo[i >> 1][i & 1];
+      bd.hi[i] = hi[i >> 1][i & 1];
+    }
+    u32x2 least, largest;
+    bd.codes(s, least, largest);
+    *(u32x2*)(a.bound + (size_t)at * 2 * D + 8 * col) = least;
+    *(u32x2*)(a.bound + (size_t)at * 2 * D + D + 8 * col) = largest;
     if (lane == 0) a.bscale[at] = s;
   }
 }
@@ -294,7 +428,16 @@ __device__ __forceinline__ void put_token(const BlockArgs& a, int unit, bool key
                                           : (keys ? a.kt : a.vt) + (((size_t)s.slot * a.Hkv + g) << a.block_shift) * D * 2;
   const unsigned char* in = (const unsigned char*)(keys ? a.k_new : a.v_new) + (size_t)unit * D * 2;
   if (lane < D / 8) *((u32x4*)(rows + newest * (D * 2)) + lane) = *((const u32x4*)in + lane);
-  if (newest == B - 1) put_block<D, KIND>(a, at, keys, [&](int r) { return r == newest ? in : rows + r * (D * 2); });
+  if (newest != B - 1) return;
+  auto row = [&](int r) { return r == newest ? in : rows + r * (D * 2); };
+  if (B == 32)
+    put_block_at_once<D, KIND, 32>(a, at, keys, row);
+  else if (B == 64)
+    put_block_at_once<D, KIND, 64>(a, at, keys, row);
+  else if (D == 64)
+    put_block_at_once<64, KIND, 128>(a, at, keys, row);
+  else  // (128 registers of rows would cost the attention a wave a SIMD)
+    put_block<D, KIND>(a, at, keys, row);
 }
 
 // ---------------------------------------------------------------- append
@@ -309,12 +452,12 @@ struct BlockAppend {
 // Wave w of workgroup x takes block 2 x + w / 2 of the sequence's new ones, keys (w even)
 // or values.  The wave of the first block, which may read the tail's old rows, writes the
 // last one's afterwards, so that no other wave's writes meet those reads.
-template <int D, int KIND>
+template <int D, int KIND, int B>
 __global__ __launch_bounds__(256) void block_append(BlockAppend p) {
   const BlockArgs& a = p.c;
   constexpr int P = D / 8, R = 64 / P;
   const int w = uniform(tid() >> 6), lane = tid() & 63, col = lane % P, r0 = lane / P;
-  const int g = bid_y(), b = __builtin_amdgcn_workgroup_id_z(), j = 2 * bid_x() + (w >> 1), B = 1 << a.block_shift;
+  const int g = bid_y(), b = __builtin_amdgcn_workgroup_id_z(), j = 2 * bid_x() + (w >> 1);
   const bool keys = !(w & 1);
   const int slot = uniform(a.slot_ids[b]);
   if (slot < 0 || slot >= a.n_slots) return;
@@ -345,7 +488,7 @@ __global__ __launch_bounds__(256) void block_append(BlockAppend p) {
     auto row = [&](int r) -> const unsigned char* {
       return r < from ? old + (size_t)r * D * 2 : in + (t0 + (int64_t)i * B + r - skip) * st[2];
     };
-    if (upto == B && i == j) put_block<D, KIND>(a, at, keys, row);
+    if (upto == B && i == j) put_block_at_once<D, KIND, B>(a, at, keys, row);
     if (KIND == kRowsBf16 || i == last)
       for (int r = r0; r < upto; r += R)
         if (r >= from) *((u32x4*)(old + (size_t)r * D * 2) + col) = *((const u32x4*)row(r) + col);
@@ -356,7 +499,7 @@ __global__ __launch_bounds__(256) void block_append(BlockAppend p) {
     if (j != last || j == 0) block(j);
     else if (skip + len == (last + 1) * B) {  // a whole last block: its codes here, its tail rows by the first block's wave
       const int at = uniform(block_at(a, slot, g, first + j));
-      if (at >= 0) put_block<D, KIND>(a, at, keys, [&](int r) { return in + (t0 + (int64_t)j * B + r - skip) * st[2]; });
+      if (at >= 0) put_block_at_once<D, KIND, B>(a, at, keys, [&](int r) { return in + (t0 + (int64_t)j * B + r - skip) * st[2]; });
     }
     if (j == 0 && last > 0) block(last);
   }
@@ -372,15 +515,52 @@ __device__ __forceinline__ uint32_t score_key(float s) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// Largest bin of a falling search: the bin of hist[0 .. 1023] that holds the rem-th
+// largest, how many are in the bins above it and in it; {-1, ..} when there are fewer.
+// Called by one wave.
+__device__ __forceinline__ void find_bin(const int* hist, int rem, int* out) {
+  const int lane = tid() & 63;
+  int c[16], sum = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const i32x4 v = *(const i32x4*)(hist + 1008 - 16 * lane + 4 * i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum += c[4 * i + e] = v[e];
+  }
+  const int upto = wave_scan(sum);
+  int before = upto - sum;
+  if (lane == 63 && upto < rem) out[0] = -1;
+  if (before < rem && rem <= upto) {
+    int bin = 0, above = before, in = 0;
+#pragma unroll
+    for (int i = 15; i >= 0; --i) {
+      if (before < rem && rem <= before + c[i]) {
+        bin = 1008 - 16 * lane + i;
+        above = before;
+        in = c[i];
+      }
+      before += c[i];
+    }
+    out[0] = bin;
+    out[1] = above;
+    out[2] = in;
+  }
+}
+
 // The scores are products of 8-bit whole numbers on the matrix units, exact in 32 bits,
-// so that the choice does not depend on the order of sums.
+// so that the choice does not depend on the order of sums.  Wave w scores 16 blocks at a
+// time, kGroups of them in flight; the keys stay in LDS.  The last score taken is found by
+// a histogram over the range that the scores span, then over the bin that holds it, and so
+// on until a bin is taken whole or is one score: two rounds, mostly.
 template <int D>
 __global__ __launch_bounds__(kSelThreadsB) void block_select(BlockArgs a) {
-  constexpr int NK = 2 * D / 64;
+  constexpr int NK = 2 * D / 64, kGroups = D == 128 ? 2 : 4;
   extern __shared__ __align__(16) uint32_t key[];  // one a block
   __shared__ __align__(16) int8_t qa[16][2 * D];
+  __shared__ __align__(16) int hist[2][1024];
   __shared__ float qu[16];
-  __shared__ int hist[256], cnt[kSelWaves], out[2];
+  __shared__ uint32_t range[kSelWaves][2];
+  __shared__ int cnt[kSelWaves][2], out[3];
   const int t = tid(), lane = t & 63, w = uniform(t >> 6), l16 = lane & 15, lg = lane >> 4, unit = bid_x();
   const int b = unit / a.Hkv, g = unit % a.Hkv, B = 1 << a.block_shift;
   const BlockSeq s = block_seq(a, b);
@@ -391,7 +571,10 @@ __global__ __launch_bounds__(kSelThreadsB) void block_select(BlockArgs a) {
   int f1 = s.row + 1 - a.recent;
   f1 = max(f0, min(nb, f1 <= 0 ? 0 : f1 >> a.block_shift));
   const bool scored = f1 - f0 > a.best && a.best > 0;
+  uint32_t T = 0;  // taken: above T, and the first `rem` of T
+  int rem = a.best;
   if (scored) {
+    hist[0][t] = 0;
     {
       const int h = w;
       const bool ok = h < a.G;
@@ -419,26 +602,56 @@ __global__ __launch_bounds__(kSelThreadsB) void block_select(BlockArgs a) {
 #pragma unroll
     for (int i = 0; i < NK; ++i) q[i] = *(const i32x4*)(&qa[l16][64 * i + 16 * lg]);
     const float u = qu[l16];
-    for (int j0 = f0 + 16 * w; j0 < f1; j0 += 16 * kSelWaves) {
-      const int j = min(j0 + l16, f1 - 1), at = block_at(a, s.slot, g, j);
-      const float bs = at < 0 ? 0.f : a.bscale[at];
-      const int8_t* from = a.bound + (size_t)max(at, 0) * 2 * D + 16 * lg;
-      i32x4 c = {0, 0, 0, 0};
+    uint32_t least = kForced, most = 0;
+    for (int j0 = f0 + 16 * w; j0 < f1; j0 += 16 * kSelWaves * kGroups) {
+      int at[kGroups];
 #pragma unroll
-      for (int i = 0; i < NK; ++i) c = __builtin_amdgcn_mfma_i32_16x16x64_i8(*(const i32x4*)(from + 64 * i), q[i], c, 0, 0, 0);
-      float best[4];
+      for (int i = 0; i < kGroups; ++i) at[i] = block_at(a, s.slot, g, min(j0 + 16 * kSelWaves * i + l16, f1 - 1));
+      float bs[kGroups];
+      i32x4 x[kGroups][NK];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        best[e] = l16 < a.G ? (float)c[e] * u : -INFINITY;
+      for (int i = 0; i < kGroups; ++i) {
+        bs[i] = a.bscale[max(at[i], 0)];
+        const int8_t* from = a.bound + (size_t)max(at[i], 0) * 2 * D + 16 * lg;
 #pragma unroll
-        for (int o = 8; o >= 1; o >>= 1) best[e] = fmaxf(best[e], __shfl_xor(best[e], o));
+        for (int k = 0; k < NK; ++k) x[i][k] = *(const i32x4*)(from + 64 * k);
       }
-      // lane (l16 < 4, lg) keeps block 4 lg + l16's; its scale and place are lane 4 lg + l16's
-      const int from_lane = 4 * lg + (l16 & 3);
-      const float mine = l16 == 0 ? best[0] : (l16 == 1 ? best[1] : (l16 == 2 ? best[2] : best[3]));
-      const float scale = __shfl(bs, from_lane);
-      const int place = __shfl(at, from_lane);
-      if (l16 < 4 && j0 + from_lane < f1) key[j0 + from_lane] = place < 0 ? 0u : score_key(mine * scale);
+#pragma unroll
+      for (int i = 0; i < kGroups; ++i) {
+        const int j1 = j0 + 16 * kSelWaves * i;
+        i32x4 c = {0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < NK; ++k) c = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[i][k], q[k], c, 0, 0, 0);
+        float best[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          best[e] = l16 < a.G ? (float)c[e] * u : -INFINITY;
+#pragma unroll
+          for (int o = 8; o >= 1; o >>= 1) best[e] = fmaxf(best[e], __shfl_xor(best[e], o));
+        }
+        // lane (l16 < 4, lg) keeps block 4 lg + l16's; its scale and place are lane 4 lg + l16's
+        const int from_lane = 4 * lg + (l16 & 3);
+        const float mine = l16 == 0 ? best[0] : (l16 == 1 ? best[1] : (l16 == 2 ? best[2] : best[3]));
+        const float scale = __shfl(bs[i], from_lane);
+        const int place = __shfl(at[i], from_lane);
+        if (l16 < 4 && j1 + from_lane < f1) {
+          const uint32_t k = place < 0 ? 0u : score_key(mine * scale);
+          key[j1 + from_lane] = k;
+          if (k) {
+            least = min(least, k);
+            most = max(most, k);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+      least = min(least, (uint32_t)__shfl_xor((int)least, o));
+      most = max(most, (uint32_t)__shfl_xor((int)most, o));
+    }
+    if (lane == 0) {
+      range[w][0] = least;
+      range[w][1] = most;
     }
   } else {
     for (int j = f0 + t; j < f1; j += kSelThreadsB) key[j] = a.best > 0 && block_at(a, s.slot, g, j) >= 0 ? kForced : 0u;
@@ -447,92 +660,80 @@ __global__ __launch_bounds__(kSelThreadsB) void block_select(BlockArgs a) {
     const int j = i < f0 ? i : f1 + i - f0;
     key[j] = block_at(a, s.slot, g, j) >= 0 ? kForced : 0u;
   }
-  // the score of the last one taken, T, and how many of that score are
-  uint32_t T = 0;
-  int rem = a.best;
+  __syncthreads();
   if (scored) {
-    for (int sh = 24; sh >= 0; sh -= 8) {
-      __syncthreads();
-      if (t < 256) hist[t] = 0;
-      __syncthreads();
+    uint32_t lo = kForced, hi = 0;
+#pragma unroll
+    for (int i = 0; i < kSelWaves; ++i) {
+      lo = min(lo, range[i][0]);
+      hi = max(hi, range[i][1]);
+    }
+    for (int round = 0;; ++round) {
+      if (lo > hi) break;  // no block is there: nothing is above T that is not forced
+      const int span = 32 - __builtin_clz((hi - lo) | 1u), sh = span > 10 ? span - 10 : 0;
+      int* h = hist[round & 1];
       for (int j = f0 + t; j < f1; j += kSelThreadsB) {
         const uint32_t k = key[j];
-        if (k != 0 && (sh == 24 || (k >> (sh + 8)) == (T >> (sh + 8)))) atomicAdd(&hist[(k >> sh) & 255], 1);
+        if (k >= lo && k <= hi) atomicAdd(&h[(k - lo) >> sh], 1);
       }
+      hist[~round & 1][t] = 0;
       __syncthreads();
-      if (w == 0) {  // lane's four bins, the largest first
-        int c[4], sum = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          c[i] = hist[255 - 4 * lane - i];
-          sum += c[i];
-        }
-        int before = wave_scan(sum) - sum;
-        const int total = wave_total(sum);
-        if (total < rem && lane == 0) {  // fewer than wanted are there at all: everything is taken
-          out[0] = -1;
-          out[1] = 0;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (before < rem && before + c[i] >= rem) {
-            out[0] = 255 - 4 * lane - i;
-            out[1] = before;
-          }
-          before += c[i];
-        }
-      }
+      if (w == 0) find_bin(h, rem, out);
       __syncthreads();
-      if (out[0] < 0) {
-        T = 1;  // keys are 1 at least; only equal ones would be counted
-        rem = 0x7fffffff;
+      const int bin = out[0];
+      if (bin < 0) break;  // fewer than wanted are there at all: all of them are taken (T = 0)
+      rem -= out[1];
+      lo += (uint32_t)bin << sh;
+      if (rem == out[2]) {  // all of the bin
+        T = lo - 1;
+        rem = 0;
         break;
       }
-      T |= (uint32_t)out[0] << sh;
-      rem -= out[1];
+      if (sh == 0) {
+        T = lo;
+        break;
+      }
+      const uint32_t top = lo + ((1u << sh) - 1u);
+      hi = top < hi ? top : hi;
+      __syncthreads();  // (out is read before it is written again)
     }
-  } else {
-    T = 1;
   }
-  __syncthreads();
-  // taken in order: above T, and the first `rem` of T; wave w ranks its share of the blocks
+  // in order; wave w writes its share of the blocks
   const int share = ((nb + kSelWaves - 1) / kSelWaves + 63) & ~63, a0 = min(nb, w * share), a1 = min(nb, a0 + share);
-  int eq = 0;
-  for (int j = a0 + lane; j - lane < a1; j += 64) eq += __builtin_popcountll(__builtin_amdgcn_ballot_w64(j < a1 && key[j] == T));
-  if (lane == 0) cnt[w] = eq;
-  __syncthreads();
-  int eq_before = 0;
-  for (int i = 0; i < w; ++i) eq_before += cnt[i];
-  __syncthreads();
-  const uint64_t below = ((uint64_t)1 << lane) - 1;
-  int taken = 0, e0 = eq_before;
+  int above = 0, equal = 0;
   for (int j = a0 + lane; j - lane < a1; j += 64) {
     const uint32_t k = j < a1 ? key[j] : 0u;
-    const uint64_t me = __builtin_amdgcn_ballot_w64(j < a1 && k == T);
-    const bool take = k != 0 && (k > T || (k == T && e0 + __builtin_popcountll(me & below) < rem));
-    taken += __builtin_popcountll(__builtin_amdgcn_ballot_w64(take));
-    e0 += __builtin_popcountll(me);
+    above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k > T));
+    equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k != 0 && k == T));
   }
-  if (lane == 0) cnt[w] = taken;
+  if (lane == 0) {
+    cnt[w][0] = above;
+    cnt[w][1] = equal;
+  }
   __syncthreads();
-  int at = 0, total = 0;
+  int above0 = 0, equal0 = 0, aboves = 0, equals = 0;
+#pragma unroll
   for (int i = 0; i < kSelWaves; ++i) {
-    if (i < w) at += cnt[i];
-    total += cnt[i];
+    if (i < w) {
+      above0 += cnt[i][0];
+      equal0 += cnt[i][1];
+    }
+    aboves += cnt[i][0];
+    equals += cnt[i][1];
   }
-  e0 = eq_before;
+  const int total = aboves + min(equals, rem);
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
   for (int j = a0 + lane; j - lane < a1; j += 64) {
     const uint32_t k = j < a1 ? key[j] : 0u;
-    const uint64_t me = __builtin_amdgcn_ballot_w64(j < a1 && k == T);
-    const bool take = k != 0 && (k > T || (k == T && e0 + __builtin_popcountll(me & below) < rem));
-    const uint64_t tm = __builtin_amdgcn_ballot_w64(take);
-    const int i = at + __builtin_popcountll(tm & below);
+    const uint64_t am = __builtin_amdgcn_ballot_w64(k > T), em = __builtin_amdgcn_ballot_w64(k != 0 && k == T);
+    const int e = equal0 + __builtin_popcountll(em & below), i = above0 + __builtin_popcountll(am & below) + min(e, rem);
+    const bool take = k > T || (k != 0 && k == T && e < rem);
     if (take && debug_check(i < a.list_ld, kDbgBlockList)) {
       list[i] = block_at(a, s.slot, g, j);
       if (sel) sel[i] = j;
     }
-    at += __builtin_popcountll(tm);
-    e0 += __builtin_popcountll(me);
+    above0 += __builtin_popcountll(am);
+    equal0 += __builtin_popcountll(em);
   }
   for (int i = total + t; i < a.list_ld; i += kSelThreadsB) list[i] = -1;
   if (sel)
@@ -986,10 +1187,13 @@ snap_status launch_block_append(const snap_params& p, const snap_block_cache& c,
     a.vs[i] = 2 * (v_stride ? v_stride[i] : kd[i]);
   }
   const int blocks = (int)(((int64_t)max_len + 2 * c.block - 2) / c.block);
-  static constexpr void (*kernels[2][3])(BlockAppend) = {
-      {block_append<64, kRowsBf16>, block_append<64, kRowsFp8>, block_append<64, kRowsInt8>},
-      {block_append<128, kRowsBf16>, block_append<128, kRowsFp8>, block_append<128, kRowsInt8>}};
-  hipLaunchKernelGGL(kernels[p.d_qk == 128][kind_of(p.kv_dtype)], dim3((blocks + 1) / 2, p.n_kv_heads, n), dim3(256), 0, stream, a);
+#define SNAP_BLOCK_APPEND(D, KIND) {block_append<D, KIND, 32>, block_append<D, KIND, 64>, block_append<D, KIND, 128>}
+  static constexpr void (*kernels[2][3][3])(BlockAppend) = {  // [width][rows][block]
+      {SNAP_BLOCK_APPEND(64, kRowsBf16), SNAP_BLOCK_APPEND(64, kRowsFp8), SNAP_BLOCK_APPEND(64, kRowsInt8)},
+      {SNAP_BLOCK_APPEND(128, kRowsBf16), SNAP_BLOCK_APPEND(128, kRowsFp8), SNAP_BLOCK_APPEND(128, kRowsInt8)}};
+#undef SNAP_BLOCK_APPEND
+  hipLaunchKernelGGL(kernels[p.d_qk == 128][kind_of(p.kv_dtype)][a.c.block_shift - 5], dim3((blocks + 1) / 2, p.n_kv_heads, n),
+                     dim3(256), 0, stream, a);
   return hipGetLastError() == hipSuccess ? SNAP_OK : SNAP_ERR_HIP;
 }
 

@@ -1136,25 +1136,37 @@ struct PagedMapArgs {
 };
 template <typename In, typename Out>
 __global__ __launch_bounds__(256) void paged_append_mapped(PagedMapArgs a) {
+  __shared__ int64_t rows[kAppendTokens];  // of this KV head among those of all pages, or -1
+  __shared__ float scales[2][kAppendTokens];
   const int g = bid_y(), kc = a.dk / 8, vc = a.v_new ? a.dv / 8 : 0, t0 = bid_x() * kAppendTokens;
-  for (int i = tid(); i < kAppendTokens * (kc + vc); i += 256) {
-    const int t = t0 + i / (kc + vc), c = i % (kc + vc);
-    if (t >= a.tokens) break;
-    const int r = a.row_of[t], b = a.seq_of[t];
-    if (r < 0 || r >= a.rows || b < 0 || b >= a.n) continue;
-    const int slot = a.slot_ids[b];
-    if (slot < 0 || slot >= a.n_slots) continue;
-    const int64_t row = (((int64_t)(r >> a.page_shift) * a.Hkv + g) << a.page_shift) + (r & ((1 << a.page_shift) - 1));
-    if (c < kc)
-      store8<In, Out>((const In*)a.k_new + t * a.ks[0] + g * a.ks[1] + 8 * c, (Out*)a.ck + row * a.dk + 8 * c,
-                      sizeof(Out) == 1 ? a.k_scale[(size_t)slot * a.Hkv + g] : 1.f);
-    else
-      store8<In, Out>((const In*)a.v_new + t * a.vs[0] + g * a.vs[1] + 8 * (c - kc), (Out*)a.cv + row * a.dv + 8 * (c - kc),
-                      sizeof(Out) == 1 ? a.v_scale[(size_t)slot * a.Hkv + g] : 1.f);
-    if (c == 0) {
+  if (tid() < kAppendTokens) {
+    const int t = t0 + tid();
+    const int r = t < a.tokens ? a.row_of[t] : -1, b = t < a.tokens ? a.seq_of[t] : -1;
+    const int slot = b >= 0 && b < a.n ? a.slot_ids[b] : -1;
+    int64_t row = -1;
+    if (r >= 0 && r < a.rows && slot >= 0 && slot < a.n_slots) {
+      row = (((int64_t)(r >> a.page_shift) * a.Hkv + g) << a.page_shift) + (r & ((1 << a.page_shift) - 1));
+      if (sizeof(Out) == 1) {
+        scales[0][tid()] = a.k_scale[(size_t)slot * a.Hkv + g];
+        if (vc) scales[1][tid()] = a.v_scale[(size_t)slot * a.Hkv + g];
+      }
       if (a.token) a.token[row] = a.pos_of[t];
       if (a.weight) a.weight[row] = 0.f;
     }
+    rows[tid()] = row;
+  }
+  __syncthreads();
+#pragma unroll 4
+  for (int i = tid(); i < kAppendTokens * (kc + vc); i += 256) {
+    const int at = i / (kc + vc), c = i % (kc + vc), t = t0 + at;
+    const int64_t row = rows[at];
+    if (row < 0) continue;
+    if (c < kc)
+      store8<In, Out>((const In*)a.k_new + t * a.ks[0] + g * a.ks[1] + 8 * c, (Out*)a.ck + row * a.dk + 8 * c,
+                      sizeof(Out) == 1 ? scales[0][at] : 1.f);
+    else
+      store8<In, Out>((const In*)a.v_new + t * a.vs[0] + g * a.vs[1] + 8 * (c - kc), (Out*)a.cv + row * a.dv + 8 * (c - kc),
+                      sizeof(Out) == 1 ? scales[1][at] : 1.f);
   }
 }
 
