@@ -9,7 +9,9 @@
 //                 newest token's own block (with the token stored)
 //   block_join    the items of a (sequence, query head) -> out
 #include <math.h>
+#include <stdlib.h>
 
+#include "lds_dma.h"
 #include "snap_internal.h"
 
 namespace snap {
@@ -39,10 +41,11 @@ struct BlockArgs {
   float2* ml;      // [items][G]  (max in log2 units, sum)
   int32_t* list;   // [units][list_ld] places of the selected blocks, ascending by block, then -1; NULL: all
   int32_t* sel_out;
+  uint32_t* keys;  // [units][key_ld] the blocks' scores, where block_score forms them
   void* out;
   const void* k_new;  // a step's token, [n][Hkv][d]; NULL: the launch only attends
   const void* v_new;
-  int n, Hq, Hkv, G, n_slots, n_pages, page_shift, block_shift, max_pages, max_rows, chosen, list_ld, out_bf16;
+  int n, Hq, Hkv, G, n_slots, n_pages, page_shift, block_shift, max_pages, max_rows, chosen, list_ld, key_ld, out_bf16;
   int waves, target, max_items;  // the cut (paged_cut.h)
   int sink, recent, best;  // selection: rows, rows, blocks
   float scale2, scale2_lo;
@@ -81,11 +84,12 @@ __device__ __forceinline__ int block_at(const BlockArgs& a, int slot, int g, int
 // item0 + g items on.
 struct BlockCut {
   int b, items, item0;
+  int slot, blocks;  // (not where blocks are selected)
 };
 
 // The whole blocks of sequence b.
-__device__ __forceinline__ int blocks_of(const BlockArgs& a, int b) {
-  const int slot = a.slot_ids[b];
+__device__ __forceinline__ int blocks_of(const BlockArgs& a, int b, int& slot) {
+  slot = a.slot_ids[b];
   const bool ok = slot >= 0 && slot < a.n_slots;
   const int r = a.rows[ok ? slot : 0];  // no branch: the loads of several sequences go out together
   return !ok || r < 0 ? 0 : (r < a.max_rows ? r : a.max_rows) >> a.block_shift;
@@ -102,11 +106,15 @@ __device__ __forceinline__ bool block_cut(const BlockArgs& a, int key, bool by_i
     return c.b < a.n;
   }
   int64_t mine = 0;
-  int nb0 = 0;
+  int nb0 = 0, slot0 = 0;
 #pragma unroll 4
   for (int b0 = 0; b0 < a.n; b0 += 64) {
-    const int b = b0 + lane, nb = b < a.n ? blocks_of(a, min(b, a.n - 1)) : 0;
-    if (b0 == 0) nb0 = nb;
+    int slot;
+    const int b = b0 + lane, blocks = blocks_of(a, min(b, a.n - 1), slot), nb = b < a.n ? blocks : 0;
+    if (b0 == 0) {
+      nb0 = nb;
+      slot0 = slot;
+    }
     mine += nb;
   }
   const int64_t total = wave_total((int)(mine & 0xfffff)) + ((int64_t)wave_total((int)(mine >> 20)) << 20);
@@ -114,7 +122,13 @@ __device__ __forceinline__ bool block_cut(const BlockArgs& a, int key, bool by_i
                             [&](int x) { return wave_total(x > 0 ? (nb0 + x - 1) / x : 0); });
   int before = 0;
   for (int b0 = 0; b0 < a.n; b0 += 64) {
-    const int b = b0 + lane, nb = b < a.n ? blocks_of(a, min(b, a.n - 1)) : 0, ni = (nb + C - 1) / C;
+    int slot = slot0, nb = nb0;
+    const int b = b0 + lane;
+    if (b0) {
+      const int blocks = blocks_of(a, min(b, a.n - 1), slot);
+      nb = b < a.n ? blocks : 0;
+    }
+    const int ni = (nb + C - 1) / C;
     const int si = wave_scan(ni), first = before + a.Hkv * (si - ni);
     const bool here = b < a.n && (by_item ? key >= first && key < first + a.Hkv * ni : key == b);
     const uint64_t m = __builtin_amdgcn_ballot_w64(here);
@@ -123,6 +137,8 @@ __device__ __forceinline__ bool block_cut(const BlockArgs& a, int key, bool by_i
       c.b = b0 + at;
       c.items = __builtin_amdgcn_readlane(ni, at);
       c.item0 = __builtin_amdgcn_readlane(first, at);
+      c.slot = __builtin_amdgcn_readlane(slot, at);
+      c.blocks = __builtin_amdgcn_readlane(nb, at);
       return debug_check(c.item0 + a.Hkv * c.items <= a.max_items, kDbgPagedItem);
     }
     before += a.Hkv * __builtin_amdgcn_readlane(si, 63);
@@ -194,10 +210,24 @@ __device__ __forceinline__ uint32_t amax8(u32x4 x, uint32_t m) {
   }
   return m;
 }
+// Largest over rows of 16 lanes (to all of them) and over the wave, by lane shifts.
+template <int CTRL>
+__device__ __forceinline__ uint32_t turned(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, false);
+}
+__device__ __forceinline__ float row_max(float v) {
+  v = fmaxf(v, __uint_as_float(turned<0x128>(__float_as_uint(v))));
+  v = fmaxf(v, __uint_as_float(turned<0x124>(__float_as_uint(v))));
+  v = fmaxf(v, __uint_as_float(turned<0x122>(__float_as_uint(v))));
+  return fmaxf(v, __uint_as_float(turned<0x121>(__float_as_uint(v))));
+}
 __device__ __forceinline__ uint32_t wave_max(uint32_t m) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
-  return m;
+  m = max(m, turned<0x128>(m));
+  m = max(m, turned<0x124>(m));
+  m = max(m, turned<0x122>(m));
+  m = max(m, turned<0x121>(m));
+  return max(max((uint32_t)__builtin_amdgcn_readlane((int)m, 0), (uint32_t)__builtin_amdgcn_readlane((int)m, 16)),
+             max((uint32_t)__builtin_amdgcn_readlane((int)m, 32), (uint32_t)__builtin_amdgcn_readlane((int)m, 48)));
 }
 
 // bf16 in an order of whole numbers (and back: its own inverse)
@@ -350,7 +380,7 @@ __device__ __forceinline__ u32x2 quick_codes8(u32x4 raw, float scale, float inv)
 }
 
 template <int D, int KIND, int B, typename Row>
-__device__ __forceinline__ void put_block_at_once(const BlockArgs& a, int at, bool keys, Row row) {
+__device__ __forceinline__ void put_block_at_once(const BlockArgs& a, int place, bool keys, Row row) {
   constexpr int P = D / 8, R = 64 / P, NP = B / R;
   const int lane = tid() & 63, col = lane % P, r0 = lane / P;
   const bool bounds = keys && a.bound;
@@ -358,6 +388,8 @@ __device__ __forceinline__ void put_block_at_once(const BlockArgs& a, int at, bo
   u32x4 x[NP];
 #pragma unroll
   for (int p = 0; p < NP; ++p) x[p] = *((const u32x4*)row(p * R + r0) + col);
+  const int at = uniform(place);  // (looked up while the rows are in flight)
+  if (at < 0) return;
   i16x2 lo[4], hi[4], m = {0, 0};
   if (bounds) {
 #pragma unroll
@@ -459,16 +491,18 @@ __global__ __launch_bounds__(256) void block_append(BlockAppend p) {
   const int w = uniform(tid() >> 6), lane = tid() & 63, col = lane % P, r0 = lane / P;
   const int g = bid_y(), b = __builtin_amdgcn_workgroup_id_z(), j = 2 * bid_x() + (w >> 1);
   const bool keys = !(w & 1);
-  const int slot = uniform(a.slot_ids[b]);
-  if (slot < 0 || slot >= a.n_slots) return;
-  const int row0 = uniform(a.rows[slot]);
-  if (row0 < 0) return;
-  int len, t0 = 0;
+  // (loads that do not wait for one another go out together)
+  int slot = a.slot_ids[b];
+  int t0 = p.starts ? p.starts[b] : 0, len = p.starts ? p.starts[b + 1] : (p.lengths ? p.lengths[b] : p.max_len);
+  const bool ok = slot >= 0 && slot < a.n_slots;
+  const int row0 = uniform(a.rows[ok ? slot : 0]);
+  slot = uniform(slot);
+  if (!ok || row0 < 0) return;
+  t0 = uniform(t0);
+  len = uniform(len);
   if (p.starts) {
-    t0 = min(max(uniform(p.starts[b]), 0), p.tokens);
-    len = min(max(uniform(p.starts[b + 1]), 0), p.tokens) - t0;
-  } else {
-    len = p.lengths ? uniform(p.lengths[b]) : p.max_len;
+    t0 = min(max(t0, 0), p.tokens);
+    len = min(max(len, 0), p.tokens) - t0;
   }
   len = min(len, p.max_len);
   const int64_t room = ((int64_t)a.max_pages << a.page_shift) - row0;
@@ -481,15 +515,14 @@ __global__ __launch_bounds__(256) void block_append(BlockAppend p) {
   unsigned char* tail = KIND == kRowsBf16 ? nullptr : (keys ? a.kt : a.vt) + ((((size_t)slot * a.Hkv + g) << a.block_shift) * D) * 2;
   // rows [from, upto) of block i come from the input
   auto block = [&](int i) {
-    const int at = uniform(block_at(a, slot, g, first + i));
-    if (at < 0) return;
+    const int at = block_at(a, slot, g, first + i);
     const int from = i ? 0 : skip, upto = min(B, skip + len - i * B);
-    unsigned char* old = KIND == kRowsBf16 ? (keys ? a.ck : a.cv) + ((size_t)at << a.block_shift) * D * 2 : tail;
+    unsigned char* old = KIND == kRowsBf16 ? (keys ? a.ck : a.cv) + ((size_t)max(at, 0) << a.block_shift) * D * 2 : tail;
     auto row = [&](int r) -> const unsigned char* {
       return r < from ? old + (size_t)r * D * 2 : in + (t0 + (int64_t)i * B + r - skip) * st[2];
     };
     if (upto == B && i == j) put_block_at_once<D, KIND, B>(a, at, keys, row);
-    if (KIND == kRowsBf16 || i == last)
+    if (uniform(at) >= 0 && (KIND == kRowsBf16 || i == last))
       for (int r = r0; r < upto; r += R)
         if (r >= from) *((u32x4*)(old + (size_t)r * D * 2) + col) = *((const u32x4*)row(r) + col);
   };
@@ -498,8 +531,8 @@ __global__ __launch_bounds__(256) void block_append(BlockAppend p) {
   } else {
     if (j != last || j == 0) block(j);
     else if (skip + len == (last + 1) * B) {  // a whole last block: its codes here, its tail rows by the first block's wave
-      const int at = uniform(block_at(a, slot, g, first + j));
-      if (at >= 0) put_block_at_once<D, KIND, B>(a, at, keys, [&](int r) { return in + (t0 + (int64_t)j * B + r - skip) * st[2]; });
+      put_block_at_once<D, KIND, B>(a, block_at(a, slot, g, first + j), keys,
+                                    [&](int r) { return in + (t0 + (int64_t)j * B + r - skip) * st[2]; });
     }
     if (j == 0 && last > 0) block(last);
   }
@@ -547,153 +580,259 @@ __device__ __forceinline__ void find_bin(const int* hist, int rem, int* out) {
   }
 }
 
-// The scores are products of 8-bit whole numbers on the matrix units, exact in 32 bits,
-// so that the choice does not depend on the order of sums.  Wave w scores 16 blocks at a
-// time, kGroups of them in flight; the keys stay in LDS.  The last score taken is found by
-// a histogram over the range that the scores span, then over the bin that holds it, and so
-// on until a bin is taken whole or is one score: two rounds, mostly.
-template <int D>
-__global__ __launch_bounds__(kSelThreadsB) void block_select(BlockArgs a) {
-  constexpr int NK = 2 * D / 64, kGroups = D == 128 ? 2 : 4;
-  extern __shared__ __align__(16) uint32_t key[];  // one a block
-  __shared__ __align__(16) int8_t qa[16][2 * D];
-  __shared__ __align__(16) int hist[2][1024];
-  __shared__ float qu[16];
-  __shared__ uint32_t range[kSelWaves][2];
-  __shared__ int cnt[kSelWaves][2], out[3];
-  const int t = tid(), lane = t & 63, w = uniform(t >> 6), l16 = lane & 15, lg = lane >> 4, unit = bid_x();
-  const int b = unit / a.Hkv, g = unit % a.Hkv, B = 1 << a.block_shift;
-  const BlockSeq s = block_seq(a, b);
-  int32_t* list = a.list + (size_t)unit * a.list_ld;
-  int32_t* sel = a.sel_out ? a.sel_out + (size_t)unit * a.chosen : nullptr;
-  // blocks [0, f0) and [f1, nb) are selected whatever their scores
-  const int nb = s.blocks, f0 = min(nb, (int)(((int64_t)a.sink + B - 1) >> a.block_shift));
-  int f1 = s.row + 1 - a.recent;
-  f1 = max(f0, min(nb, f1 <= 0 ? 0 : f1 >> a.block_shift));
-  const bool scored = f1 - f0 > a.best && a.best > 0;
-  uint32_t T = 0;  // taken: above T, and the first `rem` of T
-  int rem = a.best;
-  if (scored) {
-    hist[0][t] = 0;
-    {
-      const int h = w;
-      const bool ok = h < a.G;
-      float x[D / 64];
+// What a unit's selection goes by: blocks [0, f0) and [f1, nb) are selected whatever
+// their scores; those between are scored where there are more than `best` of them.
+struct BlockChoice {
+  const int32_t* table;  // the slot's pages
+  int g, per, nb, f0, f1;
+  bool scored;
+  __device__ __forceinline__ int page(const BlockArgs& a, int j) const { return table[min(j >> per, a.max_pages - 1)]; }
+  // index of block j among the blocks of all pages, from its page; -1: not there
+  __device__ __forceinline__ int place(const BlockArgs& a, int j, int page) const {
+    return page < 0 || page >= a.n_pages ? -1 : (int)((((int64_t)page * a.Hkv + g) << per) + (j & ((1 << per) - 1)));
+  }
+  __device__ __forceinline__ bool there(const BlockArgs& a, int j) const { return place(a, j, page(a, j)) >= 0; }
+};
+// The slot's pages first; its rows (whose loads wait for the slot's id as well) by limits().
+__device__ __forceinline__ BlockChoice choice_of(const BlockArgs& a, int unit, int& held) {
+  BlockChoice c;
+  c.g = unit % a.Hkv;
+  c.per = a.page_shift - a.block_shift;
+  const int slot = a.slot_ids[unit / a.Hkv];
+  const bool ok = slot >= 0 && slot < a.n_slots;
+  c.table = a.table + (size_t)(ok ? slot : 0) * a.max_pages;
+  held = a.rows[ok ? slot : 0];
+  held = ok ? held : -1;
+  c.f0 = (int)(((int64_t)a.sink + (1 << a.block_shift) - 1) >> a.block_shift);
+  return c;
+}
+__device__ __forceinline__ void limits(const BlockArgs& a, int held, BlockChoice& c) {
+  const int row = uniform(held);
+  c.nb = row < 0 ? 0 : min(row, a.max_rows) >> a.block_shift;
+  c.f0 = min(c.nb, c.f0);
+  const int f1 = row + 1 - a.recent;
+  c.f1 = max(c.f0, min(c.nb, f1 <= 0 ? 0 : f1 >> a.block_shift));
+  c.scored = c.f1 - c.f0 > a.best && a.best > 0;
+}
+
+// The keys of blocks [first, end) of a unit, by a workgroup of W waves: wave w scores 16
+// blocks at a time, N times 16 of them in flight.  The scores are products of 8-bit whole
+// numbers on the matrix units, exact in 32 bits, so that a choice does not depend on the
+// order of sums.  qraw: wave w's share of the queries, [(G + W - 1) / W]; pages: those of
+// the wave's first blocks.
+template <int D, int W>
+struct BlockScores {
+  static constexpr int NK = 2 * D / 64, N = D == 128 ? 4 : 8, kStep = 16 * W, Q = 16 / W;
+  static constexpr int P = 2 * D / 16;  // 16-byte pieces of a block's bounds
+  struct Shared {
+    int8_t a[16][2 * D];  // a query's codes: those below zero, then those above
+    float u[16];
+    u32x4 x[W][16 * P];  // a wave's 16 blocks
+  };
+  // Where piece p of block r of 16 stands: turned, so that neither the rows that are
+  // written nor the columns that are read meet on a bank.
+  static __device__ __forceinline__ int spot(int r, int p) { return r * P + (p ^ (P == 16 ? r : (r >> 1) & 7)); }
+  int pages[N];
+  uint32_t qraw[Q][D / 64];
+  __device__ __forceinline__ void load_q(const BlockArgs& a, int unit) {
+    const int w = tid() >> 6, lane = tid() & 63, b = unit / a.Hkv, g = unit % a.Hkv;
+#pragma unroll
+    for (int k = 0; k < Q; ++k)
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i)
+        qraw[k][i] = ((const uint16_t*)a.q)[((size_t)b * a.Hq + g * a.G + min(w + W * k, a.G - 1)) * D + i * 64 + lane];
+  }
+  __device__ __forceinline__ void load_pages(const BlockArgs& a, const BlockChoice& c, int j) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) pages[i] = c.page(a, j + kStep * i + (tid() & 15));
+  }
+  template <typename Emit>
+  __device__ __forceinline__ void run(const BlockArgs& a, const BlockChoice& c, int first, int end, Shared& sh, Emit emit) {
+    const int lane = tid() & 63, w = uniform(tid() >> 6), l16 = lane & 15, lg = lane >> 4;
+    int at[N];
+    float bs[N];
+    // Loads take 1 KB of neighbouring bytes (with the rows of a matrix operand a lane each,
+    // 64 bytes of 16 blocks, the L1 passes 16 bytes a clock); the operand is made in LDS.
+    u32x4 x[N][NK];
+    auto load = [&](int j0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int j = j0 + kStep * i + l16;
+        if (j - l16 >= end) continue;  // (of the whole wave)
+        at[i] = j < end ? c.place(a, j, pages[i]) : -1;
+        bs[i] = a.bscale[max(at[i], 0)];
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {
+          const int piece = 64 * k + lane, block = __shfl(at[i], piece / P);
+          x[i][k] = *(const u32x4*)(a.bound + ((size_t)max(block, 0) * P + piece % P) * 16);
+        }
+      }
+      if (j0 + kStep * N < end) load_pages(a, c, j0 + kStep * N);
+    };
+    int j0 = first + 16 * w;
+    load(j0);
+#pragma unroll
+    for (int k = 0; k < Q; ++k) {
+      const int h = w + W * k;
       uint32_t m = 0;
 #pragma unroll
       for (int i = 0; i < D / 64; ++i) {
-        const uint32_t v = ok ? ((const uint16_t*)a.q)[((size_t)b * a.Hq + g * a.G + h) * D + i * 64 + lane] : 0u;
-        x[i] = bf16_bits_to_f32(v);
-        const uint32_t mag = v & 0x7fffu;
+        const uint32_t mag = h < a.G ? qraw[k][i] & 0x7fffu : 0u;
         m = max(m, mag < 0x7f80u ? mag : 0u);
       }
       const float u = block_scale(wave_max(m), 127.f);
-      if (lane == 0) qu[h] = u;
+      if (lane == 0) sh.u[h] = u;
 #pragma unroll
       for (int i = 0; i < D / 64; ++i) {
-        const float z[4] = {x[i], 0.f, 0.f, 0.f};
-        const int c = (int)(int8_t)(int8x4(z, u) & 0xffu);
-        qa[h][i * 64 + lane] = (int8_t)min(c, 0);
-        qa[h][D + i * 64 + lane] = (int8_t)max(c, 0);
+        const uint32_t v = h < a.G ? qraw[k][i] : 0u;
+        const float y = fminf(fmaxf(__builtin_rintf(bf16_bits_to_f32(v) / u), -127.f), 127.f);
+        const int z = (v & 0x7fffu) > 0x7f80u ? 0 : (int)y;  // (NaN)
+        sh.a[h][i * 64 + lane] = (int8_t)min(z, 0);
+        sh.a[h][D + i * 64 + lane] = (int8_t)max(z, 0);
       }
     }
-    __syncthreads();
+    lds_barrier();  // (the blocks' loads stay in flight)
     i32x4 q[NK];
 #pragma unroll
-    for (int i = 0; i < NK; ++i) q[i] = *(const i32x4*)(&qa[l16][64 * i + 16 * lg]);
-    const float u = qu[l16];
-    uint32_t least = kForced, most = 0;
-    for (int j0 = f0 + 16 * w; j0 < f1; j0 += 16 * kSelWaves * kGroups) {
-      int at[kGroups];
+    for (int i = 0; i < NK; ++i) q[i] = *(const i32x4*)(&sh.a[l16][64 * i + 16 * lg]);
+    const float u = sh.u[l16];
+    for (; j0 < end; j0 += kStep * N) {
 #pragma unroll
-      for (int i = 0; i < kGroups; ++i) at[i] = block_at(a, s.slot, g, min(j0 + 16 * kSelWaves * i + l16, f1 - 1));
-      float bs[kGroups];
-      i32x4 x[kGroups][NK];
+      for (int i = 0; i < N; ++i) {
+        const int j1 = j0 + kStep * i;
+        if (j1 >= end) continue;
+        i32x4 s = {0, 0, 0, 0};
+        // (one wave's LDS operations take effect in order)
 #pragma unroll
-      for (int i = 0; i < kGroups; ++i) {
-        bs[i] = a.bscale[max(at[i], 0)];
-        const int8_t* from = a.bound + (size_t)max(at[i], 0) * 2 * D + 16 * lg;
+        for (int k = 0; k < NK; ++k) sh.x[w][spot((64 * k + lane) / P, (64 * k + lane) % P)] = x[i][k];
+        asm volatile("" ::: "memory");
 #pragma unroll
-        for (int k = 0; k < NK; ++k) x[i][k] = *(const i32x4*)(from + 64 * k);
-      }
-#pragma unroll
-      for (int i = 0; i < kGroups; ++i) {
-        const int j1 = j0 + 16 * kSelWaves * i;
-        i32x4 c = {0, 0, 0, 0};
-#pragma unroll
-        for (int k = 0; k < NK; ++k) c = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[i][k], q[k], c, 0, 0, 0);
+        for (int k = 0; k < NK; ++k)
+          s = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, sh.x[w][spot(l16, 4 * k + lg)]), q[k], s, 0, 0, 0);
+        asm volatile("" ::: "memory");
         float best[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          best[e] = l16 < a.G ? (float)c[e] * u : -INFINITY;
-#pragma unroll
-          for (int o = 8; o >= 1; o >>= 1) best[e] = fmaxf(best[e], __shfl_xor(best[e], o));
-        }
+        for (int e = 0; e < 4; ++e) best[e] = row_max(l16 < a.G ? (float)s[e] * u : -INFINITY);
         // lane (l16 < 4, lg) keeps block 4 lg + l16's; its scale and place are lane 4 lg + l16's
         const int from_lane = 4 * lg + (l16 & 3);
         const float mine = l16 == 0 ? best[0] : (l16 == 1 ? best[1] : (l16 == 2 ? best[2] : best[3]));
         const float scale = __shfl(bs[i], from_lane);
         const int place = __shfl(at[i], from_lane);
-        if (l16 < 4 && j1 + from_lane < f1) {
-          const uint32_t k = place < 0 ? 0u : score_key(mine * scale);
-          key[j1 + from_lane] = k;
-          if (k) {
-            least = min(least, k);
-            most = max(most, k);
-          }
-        }
+        if (l16 < 4 && j1 + from_lane < end) emit(j1 + from_lane, place < 0 ? 0u : score_key(mine * scale));
       }
+      if (j0 + kStep * N < end) load(j0 + kStep * N);
     }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-      least = min(least, (uint32_t)__shfl_xor((int)least, o));
-      most = max(most, (uint32_t)__shfl_xor((int)most, o));
+  }
+};
+
+// The keys of a unit's blocks, cut over several workgroups where they are many.
+constexpr int kScoreThreads = 256;
+template <int D>
+__global__ __launch_bounds__(kScoreThreads) void block_score(BlockArgs a, int chunk) {
+  typedef BlockScores<D, kScoreThreads / 64> Scores;
+  __shared__ __align__(16) typename Scores::Shared sh;
+  const int unit = bid_y();
+  Scores s;
+  s.load_q(a, unit);
+  int held;
+  BlockChoice c = choice_of(a, unit, held);
+  const int first = c.f0 + bid_x() * chunk;
+  s.load_pages(a, c, first + 16 * (tid() >> 6));
+  limits(a, held, c);
+  const int end = min(c.f1, first + chunk);
+  if (!c.scored || first >= end) return;
+  uint32_t* keys = a.keys + (size_t)unit * a.key_ld;
+  s.run(a, c, first, end, sh, [&](int j, uint32_t k) { keys[j] = k; });
+}
+
+// One workgroup a unit.  The keys are in LDS.  The last score taken is found by a
+// histogram over the range that the scores span, then over the bin that holds it, and so
+// on until a bin is taken whole or is one score: two rounds, mostly.  GIVEN: the keys are
+// block_score's.
+template <int D, bool GIVEN>
+__global__ __launch_bounds__(kSelThreadsB) void block_select(BlockArgs a) {
+  extern __shared__ __align__(16) uint32_t key[];  // one a block
+  typedef BlockScores<D, kSelWaves> Scores;
+  __shared__ __align__(16) typename Scores::Shared sh;
+  __shared__ __align__(16) int hist[2][1024];
+  __shared__ uint32_t range[kSelWaves][2];
+  __shared__ int cnt[kSelWaves][2], out[3];
+  const int t = tid(), lane = t & 63, w = uniform(t >> 6), unit = bid_x();
+  Scores s;
+  if constexpr (!GIVEN) s.load_q(a, unit);
+  int held;
+  BlockChoice c = choice_of(a, unit, held);
+  if constexpr (!GIVEN) s.load_pages(a, c, c.f0 + 16 * w);
+  hist[0][t] = 0;
+  limits(a, held, c);
+  const int nb = c.nb, f0 = c.f0, f1 = c.f1;
+  int32_t* list = a.list + (size_t)unit * a.list_ld;
+  int32_t* sel = a.sel_out ? a.sel_out + (size_t)unit * a.chosen : nullptr;
+  uint32_t T = 0;  // taken: above T, and the first `rem` of T
+  int rem = a.best;
+  uint32_t least = kForced, most = 0;
+  auto keep = [&](int j, uint32_t k) {
+    key[j] = k;
+    if (k) {
+      least = min(least, k);
+      most = max(most, k);
     }
+  };
+  if (!c.scored) {
+    for (int j = f0 + t; j < f1; j += kSelThreadsB) key[j] = a.best > 0 && c.there(a, j) ? kForced : 0u;
+  } else if constexpr (GIVEN) {
+    const uint32_t* keys = a.keys + (size_t)unit * a.key_ld;
+#pragma unroll 4
+    for (int j = f0 + t; j < f1; j += kSelThreadsB) keep(j, keys[j]);
+  } else {
+    s.run(a, c, f0, f1, sh, keep);
+  }
+  for (int i = t; i < f0 + nb - f1; i += kSelThreadsB) {
+    const int j = i < f0 ? i : f1 + i - f0;
+    key[j] = c.there(a, j) ? kForced : 0u;
+  }
+  if (c.scored) {
+    least = ~wave_max(~least);
+    most = wave_max(most);
     if (lane == 0) {
       range[w][0] = least;
       range[w][1] = most;
     }
-  } else {
-    for (int j = f0 + t; j < f1; j += kSelThreadsB) key[j] = a.best > 0 && block_at(a, s.slot, g, j) >= 0 ? kForced : 0u;
-  }
-  for (int i = t; i < f0 + nb - f1; i += kSelThreadsB) {
-    const int j = i < f0 ? i : f1 + i - f0;
-    key[j] = block_at(a, s.slot, g, j) >= 0 ? kForced : 0u;
   }
   __syncthreads();
-  if (scored) {
+  if (c.scored) {
     uint32_t lo = kForced, hi = 0;
 #pragma unroll
     for (int i = 0; i < kSelWaves; ++i) {
       lo = min(lo, range[i][0]);
       hi = max(hi, range[i][1]);
     }
-    for (int round = 0;; ++round) {
+    for (int turn = 0;; ++turn) {
       if (lo > hi) break;  // no block is there: nothing is above T that is not forced
-      const int span = 32 - __builtin_clz((hi - lo) | 1u), sh = span > 10 ? span - 10 : 0;
-      int* h = hist[round & 1];
+      const int span = 32 - __builtin_clz((hi - lo) | 1u), shift = span > 10 ? span - 10 : 0;
+      int* h = hist[turn & 1];
       for (int j = f0 + t; j < f1; j += kSelThreadsB) {
         const uint32_t k = key[j];
-        if (k >= lo && k <= hi) atomicAdd(&h[(k - lo) >> sh], 1);
+        if (k >= lo && k <= hi) atomicAdd(&h[(k - lo) >> shift], 1);
       }
-      hist[~round & 1][t] = 0;
+      hist[~turn & 1][t] = 0;
       __syncthreads();
       if (w == 0) find_bin(h, rem, out);
       __syncthreads();
       const int bin = out[0];
       if (bin < 0) break;  // fewer than wanted are there at all: all of them are taken (T = 0)
       rem -= out[1];
-      lo += (uint32_t)bin << sh;
+      lo += (uint32_t)bin << shift;
       if (rem == out[2]) {  // all of the bin
         T = lo - 1;
         rem = 0;
         break;
       }
-      if (sh == 0) {
+      if (shift == 0) {
         T = lo;
         break;
       }
-      const uint32_t top = lo + ((1u << sh) - 1u);
+      const uint32_t top = lo + ((1u << shift) - 1u);
       hi = top < hi ? top : hi;
       __syncthreads();  // (out is read before it is written again)
     }
@@ -729,7 +868,7 @@ __global__ __launch_bounds__(kSelThreadsB) void block_select(BlockArgs a) {
     const int e = equal0 + __builtin_popcountll(em & below), i = above0 + __builtin_popcountll(am & below) + min(e, rem);
     const bool take = k > T || (k != 0 && k == T && e < rem);
     if (take && debug_check(i < a.list_ld, kDbgBlockList)) {
-      list[i] = block_at(a, s.slot, g, j);
+      list[i] = c.place(a, j, c.page(a, j));
       if (sel) sel[i] = j;
     }
     above0 += __builtin_popcountll(am);
@@ -892,9 +1031,8 @@ __global__ __launch_bounds__(64) void block_attn(BlockArgs a) {
     if (!block_cut(a, item, true, c)) return;
     place = (size_t)parts * units + item;
     const int local = item - c.item0, g = local / c.items, chunk = local % c.items, b = c.b;
-    const int slot = uniform(a.slot_ids[b]);
     const int32_t* list = a.list ? a.list + (size_t)(b * a.Hkv + g) * a.list_ld : nullptr;
-    const int nb = a.list ? a.list_ld : uniform(blocks_of(a, b));
+    const int nb = a.list ? a.list_ld : c.blocks;
     const int e0 = (int)((int64_t)chunk * nb / c.items), e1 = (int)((int64_t)(chunk + 1) * nb / c.items);
     const unsigned char* qp = (const unsigned char*)a.q + ((size_t)b * a.Hq + g * a.G + (hval ? l16 : 0)) * D * 2;
     u32x4 q[D / 32];
@@ -910,7 +1048,7 @@ __global__ __launch_bounds__(64) void block_attn(BlockArgs a) {
     uint64_t left = 0;
     auto look = [&]() {
       const int i = e + lane;
-      at = i >= e1 ? -1 : (list ? list[i] : block_at(a, slot, g, i));
+      at = i >= e1 ? -1 : (list ? list[i] : block_at(a, c.slot, g, i));
       if constexpr (KIND != kRowsBf16) {
         ksc = a.ks[max(at, 0)];
         vsc = a.vs[max(at, 0)];
@@ -1166,8 +1304,20 @@ BlockGeometry block_geometry(const snap_params& p, int n, int max_rows, int bloc
   off = align256(off + items * G * sizeof(float2));
   g.off_list = off;
   if (select) off = align256(off + (size_t)units * g.list_ld * sizeof(int32_t));
+  g.off_keys = off;
+  if (select) off = align256(off + (size_t)units * most * sizeof(uint32_t));
   g.bytes = off;
   return g;
+}
+
+// Blocks whose keys stand in LDS beside what scoring needs there (78 KB of 160).
+constexpr int kFusedBlocks = 8192;
+// The workgroups that score a unit's blocks before they are chosen among; 1: the one that
+// chooses.
+static int score_splits(const snap_params& p, int units, int blocks) {
+  const int least = blocks > kFusedBlocks ? 2 : 1;
+  if (const char* e = getenv("SPLITS")) return atoi(e) > least ? atoi(e) : least;
+  return least;
 }
 
 snap_status launch_block_append(const snap_params& p, const snap_block_cache& c, const int32_t* rows, int n,
@@ -1221,8 +1371,19 @@ snap_status launch_block_decode(const snap_params& p, const snap_block_cache& c,
     a.sink = p.sink;
     a.recent = p.recent;
     a.best = (p.topk + c.block - 1) / c.block;
+    const int splits = score_splits(p, units, geo.blocks);
+    if (splits > 1) {
+      const int chunk = ((geo.blocks + splits - 1) / splits + 63) / 64 * 64;
+      a.keys = (uint32_t*)((unsigned char*)ws + geo.off_keys);
+      a.key_ld = geo.blocks;
+      hipLaunchKernelGGL((p.d_qk == 128 ? block_score<128> : block_score<64>), dim3((geo.blocks + chunk - 1) / chunk, units),
+                         dim3(kScoreThreads), 0, stream, a, chunk);
+      if (hipGetLastError() != hipSuccess) return SNAP_ERR_HIP;
+    }
     const size_t lds = (size_t)(geo.blocks < 1 ? 1 : geo.blocks) * sizeof(uint32_t);
-    hipLaunchKernelGGL((p.d_qk == 128 ? block_select<128> : block_select<64>), dim3(units), dim3(kSelThreadsB), lds, stream, a);
+    static constexpr void (*choose[2][2])(BlockArgs) = {{block_select<64, false>, block_select<64, true>},
+                                                        {block_select<128, false>, block_select<128, true>}};
+    hipLaunchKernelGGL(choose[p.d_qk == 128][splits > 1], dim3(units), dim3(kSelThreadsB), lds, stream, a);
     if (hipGetLastError() != hipSuccess) return SNAP_ERR_HIP;
   }
   // streaming loads where the blocks read are more than half the last-level cache

@@ -17,6 +17,7 @@ namespace {
 
 constexpr int kPoolThreads = 1024;
 constexpr int kPoolWaves = kPoolThreads / 64;
+constexpr int kAtOnce = 4;  // pages that a thread has in flight
 
 struct PoolArgs {
   int32_t* table;
@@ -95,9 +96,16 @@ __global__ __launch_bounds__(kPoolThreads) void pages_reserve(PoolArgs a) {
     slots[t] = slot;
     if (take) a.held[slot] = h + take;
     __syncthreads();
-    for (int e = t; e < (int)chunk; e += kPoolThreads) {
-      const int s = find_last<10>(first, e);
-      a.table[(size_t)slots[s] * a.max_pages + to[s] + e] = a.free_pages[free0 - 1 - taken - e];
+    for (int e0 = t; e0 < (int)chunk; e0 += kAtOnce * kPoolThreads) {
+      int page[kAtOnce], s[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) page[i] = a.free_pages[free0 - 1 - taken - min(e0 + i * kPoolThreads, (int)chunk - 1)];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) s[i] = find_last<10>(first, e0 + i * kPoolThreads);
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i)
+        if (e0 + i * kPoolThreads < (int)chunk)
+          a.table[(size_t)slots[s[i]] * a.max_pages + to[s[i]] + e0 + i * kPoolThreads] = page[i];
     }
     taken += (int)chunk;
     before += total;
@@ -133,11 +141,22 @@ __global__ __launch_bounds__(kPoolThreads) void pages_release(PoolArgs a) {
     from[t] = keep - rank;
     slots[t] = slot;
     __syncthreads();
-    for (int e = t; e < m; e += kPoolThreads) {
-      const int s = find_last<10>(first, e);
-      int32_t* at = a.table + (size_t)slots[s] * a.max_pages + from[s] + e;
-      a.free_pages[end + m - 1 - e] = *at;
-      *at = -1;
+    for (int e0 = t; e0 < m; e0 += kAtOnce * kPoolThreads) {
+      int32_t* at[kAtOnce];
+      int page[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int e = min(e0 + i * kPoolThreads, m - 1), s = find_last<10>(first, e);
+        at[i] = a.table + (size_t)slots[s] * a.max_pages + from[s] + e;
+      }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) page[i] = *at[i];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i)
+        if (e0 + i * kPoolThreads < m) {
+          a.free_pages[end + m - 1 - (e0 + i * kPoolThreads)] = page[i];
+          *at[i] = -1;
+        }
     }
     end += m;
     __syncthreads();

@@ -319,7 +319,7 @@ struct BlockGeometry : PagedCut {
   int blocks;   // whole blocks of a sequence at most
   int chosen;   // blocks that a selection lists at most
   int list_ld;  // of which there are at most this many
-  size_t off_part, off_ml, off_list, bytes;
+  size_t off_part, off_ml, off_list, off_keys, bytes;
 };
 constexpr int kBlockMost = 32768;  // blocks that one workgroup selects among (their scores in LDS)
 int block_chosen(const snap_params& p, int block);
