@@ -9,7 +9,6 @@
 //                 newest token's own block (with the token stored)
 //   block_join    the items of a (sequence, query head) -> out
 #include <math.h>
-#include <stdlib.h>
 
 #include "lds_dma.h"
 #include "snap_internal.h"
@@ -623,6 +622,7 @@ __device__ __forceinline__ void limits(const BlockArgs& a, int held, BlockChoice
 template <int D, int W>
 struct BlockScores {
   static constexpr int NK = 2 * D / 64, N = D == 128 ? 4 : 8, kStep = 16 * W, Q = 16 / W;
+  static constexpr int kBatch = kStep * N;  // blocks in flight
   static constexpr int P = 2 * D / 16;  // 16-byte pieces of a block's bounds
   struct Shared {
     int8_t a[16][2 * D];  // a query's codes: those below zero, then those above
@@ -728,8 +728,9 @@ struct BlockScores {
 // The keys of a unit's blocks, cut over several workgroups where they are many.
 constexpr int kScoreThreads = 256;
 template <int D>
-__global__ __launch_bounds__(kScoreThreads) void block_score(BlockArgs a, int chunk) {
+__global__ __launch_bounds__(kScoreThreads) void block_score(BlockArgs a) {
   typedef BlockScores<D, kScoreThreads / 64> Scores;
+  constexpr int chunk = Scores::kBatch;
   __shared__ __align__(16) typename Scores::Shared sh;
   const int unit = bid_y();
   Scores s;
@@ -960,215 +961,238 @@ struct Soft {
   }
 };
 
-template <int D, int KIND, bool NT>
-__global__ __launch_bounds__(64) void block_attn(BlockArgs a) {
-  constexpr int E = KIND == kRowsBf16 ? 2 : 1, VE = D / 16;
-  constexpr int NK = D * E / 64;
-  typedef uint32_t VRaw __attribute__((ext_vector_type(VE * E / 4)));
+// Rows r0 .. r0 + 31 of the newest token's block, as they came; the token itself is read
+// from a step's input.
+template <int D, int KIND>
+__device__ __forceinline__ void attend_newest(const BlockArgs& a, const BlockSeq& s, int b, int g, int at, int r0, Soft<D>& o) {
+  constexpr int VE = D / 16;
   typedef uint32_t VTail __attribute__((ext_vector_type(VE * 2 / 4)));
-  const int lane = tid() & 63, l16 = lane & 15, lg = lane >> 4, units = a.n * a.Hkv, B = 1 << a.block_shift;
+  const int lane = tid() & 63, l16 = lane & 15, lg = lane >> 4, B = 1 << a.block_shift, newest = s.row & (B - 1);
   const bool hval = l16 < a.G;
-  // Workgroups [0, 2 units) store a step's token, those up to (2 + B / 32) units attend
-  // 32 rows each of the newest token's block, the others a work item each.
-  const int stores = a.k_new ? 2 * units : 0, parts = B >> 5;
-  const int w = bid_x() - stores, item = w - parts * units;
-  if (w < 0) {
-    put_token<D, KIND>(a, bid_x() >> 1, !(bid_x() & 1));
-    return;
+  const unsigned char* qp = (const unsigned char*)a.q + ((size_t)b * a.Hq + g * a.G + (hval ? l16 : 0)) * D * 2;
+  const size_t t0 = (((size_t)s.slot * a.Hkv + g) << a.block_shift) * D * 2, p0 = ((size_t)at << a.block_shift) * D * 2;
+  const unsigned char* kb = KIND == kRowsBf16 ? a.ck + p0 : a.kt + t0;
+  const unsigned char* vb = KIND == kRowsBf16 ? a.cv + p0 : a.vt + t0;
+  const size_t n0 = ((size_t)b * a.Hkv + g) * D * 2;
+  const unsigned char* kn = a.k_new ? (const unsigned char*)a.k_new + n0 : kb + newest * (D * 2);
+  const unsigned char* vn = a.k_new ? (const unsigned char*)a.v_new + n0 : vb + newest * (D * 2);
+  const int ra = r0 + l16, rb = ra + 16;
+  const unsigned char* pa = ra >= newest ? kn : kb + ra * (D * 2);  // (rows past the newest are masked)
+  const unsigned char* pb = rb >= newest ? kn : kb + rb * (D * 2);
+  u32x4 q[D / 32], k0[D / 32], k1[D / 32];
+#pragma unroll
+  for (int j = 0; j < D / 32; ++j) {
+    q[j] = hval ? *(const u32x4*)(qp + 64 * j + 16 * lg) : u32x4{0u, 0u, 0u, 0u};
+    k0[j] = *(const u32x4*)(pa + 64 * j + 16 * lg);
+    k1[j] = *(const u32x4*)(pb + 64 * j + 16 * lg);
   }
-  size_t place;  // among the partials: a unit's 32-row parts, then the items
-  Soft<D> o;
-  o.init();
-  if (item < 0) {
-    const int unit = w / parts, r0 = w % parts * 32, b = unit / a.Hkv, g = unit % a.Hkv;
-    const BlockSeq s = block_seq(a, b);
-    const int newest = s.row & (B - 1), at = s.tail && r0 <= newest ? uniform(block_at(a, s.slot, g, s.row >> a.block_shift)) : -1;
-    place = w;
-    if (at >= 0) {
-      const unsigned char* qp = (const unsigned char*)a.q + ((size_t)b * a.Hq + g * a.G + (hval ? l16 : 0)) * D * 2;
-      const size_t t0 = (((size_t)s.slot * a.Hkv + g) << a.block_shift) * D * 2, p0 = ((size_t)at << a.block_shift) * D * 2;
-      const unsigned char* kb = KIND == kRowsBf16 ? a.ck + p0 : a.kt + t0;
-      const unsigned char* vb = KIND == kRowsBf16 ? a.cv + p0 : a.vt + t0;
-      const unsigned char* kn = a.k_new ? (const unsigned char*)a.k_new + (size_t)unit * D * 2 : kb + newest * (D * 2);
-      const unsigned char* vn = a.k_new ? (const unsigned char*)a.v_new + (size_t)unit * D * 2 : vb + newest * (D * 2);
-      const int ra = r0 + l16, rb = ra + 16;
-      const unsigned char* pa = ra >= newest ? kn : kb + ra * (D * 2);  // (rows past the newest are masked)
-      const unsigned char* pb = rb >= newest ? kn : kb + rb * (D * 2);
-      u32x4 q[D / 32], k0[D / 32], k1[D / 32];
+  VTail v[8];
 #pragma unroll
-      for (int j = 0; j < D / 32; ++j) {
-        q[j] = hval ? *(const u32x4*)(qp + 64 * j + 16 * lg) : u32x4{0u, 0u, 0u, 0u};
-        k0[j] = *(const u32x4*)(pa + 64 * j + 16 * lg);
-        k1[j] = *(const u32x4*)(pb + 64 * j + 16 * lg);
-      }
-      VTail v[8];
+  for (int i = 0; i < 8; ++i) {
+    const int r = r0 + (i < 4 ? 0 : 16) + 4 * lg + (i & 3);
+    v[i] = *(const VTail*)((r >= newest ? vn : vb + r * (D * 2)) + l16 * (VE * 2));
+  }
+  f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int r = r0 + (i < 4 ? 0 : 16) + 4 * lg + (i & 3);
-        v[i] = *(const VTail*)((r >= newest ? vn : vb + r * (D * 2)) + l16 * (VE * 2));
-      }
-      f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+  for (int j = 0; j < D / 32; ++j) {
+    s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k0[j]), __builtin_bit_cast(bf16x8, q[j]), s0, 0, 0, 0);
+    s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k1[j]), __builtin_bit_cast(bf16x8, q[j]), s1, 0, 0, 0);
+  }
+  float x[8], pe[8];
+  uint32_t vw[8][VE / 2];
 #pragma unroll
-      for (int j = 0; j < D / 32; ++j) {
-        s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k0[j]), __builtin_bit_cast(bf16x8, q[j]), s0, 0, 0, 0);
-        s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k1[j]), __builtin_bit_cast(bf16x8, q[j]), s1, 0, 0, 0);
-      }
-      float x[8], pe[8];
-      uint32_t vw[8][VE / 2];
+  for (int i = 0; i < 8; ++i) {
+    const int r = r0 + (i < 4 ? 0 : 16) + 4 * lg + (i & 3);
+    x[i] = r <= newest ? (i < 4 ? s0[i & 3] : s1[i & 3]) : -INFINITY;
+    if (r > newest) v[i] = VTail{};
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int r = r0 + (i < 4 ? 0 : 16) + 4 * lg + (i & 3);
-        x[i] = r <= newest ? (i < 4 ? s0[i & 3] : s1[i & 3]) : -INFINITY;
-        if (r > newest) v[i] = VTail{};
+    for (int u = 0; u < VE / 2; ++u) vw[i][u] = v[i][u];
+  }
+  o.softmax(x, a.scale2, a.scale2_lo, 1.f, pe);
+  o.values(pe, vw);
+}
+
+// The 32-row steps [first, end) of a unit's blocks (those listed, or all), by one wave for
+// the G query heads of its KV head at once: products of 32 keys with the heads (padded to
+// 16 columns) on the matrix units, an online softmax in the exp2 domain, the probabilities
+// times a block's value scale, times the codes on the matrix units.  Lane (l16, lg) holds
+// head l16's logits of rows 4 lg + e of each 16-row half, which is also what the second
+// product takes from it; its keys are 16 bytes at byte 64 j + 16 lg of row l16, its values
+// the D / 16 dims from (D / 16) l16 of eight rows.  Every row of a whole block is there, so
+// nothing is masked.
+template <int D, int KIND, bool NT>
+__device__ __forceinline__ void attend_blocks(const BlockArgs& a, int b, int g, int slot, const int32_t* list, int first, int end, Soft<D>& o) {
+  constexpr int E = KIND == kRowsBf16 ? 2 : 1, VE = D / 16, NK = D * E / 64;
+  typedef uint32_t VRaw __attribute__((ext_vector_type(VE * E / 4)));
+  const int lane = tid() & 63, l16 = lane & 15, lg = lane >> 4, B = 1 << a.block_shift, steps = a.block_shift - 5;
+  const bool hval = l16 < a.G;
+  const unsigned char* qp = (const unsigned char*)a.q + ((size_t)b * a.Hq + g * a.G + (hval ? l16 : 0)) * D * 2;
+  u32x4 q[D / 32];
 #pragma unroll
-        for (int u = 0; u < VE / 2; ++u) vw[i][u] = v[i][u];
-      }
-      o.softmax(x, a.scale2, a.scale2_lo, 1.f, pe);
-      o.values(pe, vw);
+  for (int j = 0; j < D / 32; ++j) {
+    const int off = KIND == kRowsBf16 ? 64 * j + 16 * lg : (64 * (j / 2) + 16 * lg + 8 * (j & 1)) * 2;
+    q[j] = hval ? *(const u32x4*)(qp + off) : u32x4{0u, 0u, 0u, 0u};
+  }
+  // Blocks e .. e + 63, one a lane: place and scales.  Those that are done or whose pages
+  // are not there have no bit in `left`.
+  int at, e = first >> steps, sub = (first & ((1 << steps) - 1)) << 5;
+  const int e1 = (end + (1 << steps) - 1) >> steps, cut = B - (((e1 << steps) - end) << 5);  // rows of the last block
+  float ksc = 1.f, vsc = 1.f;
+  uint64_t left = 0;
+  auto look = [&]() {
+    const int i = e + lane;
+    at = i >= e1 ? -1 : (list ? list[i] : block_at(a, slot, g, i));
+    if constexpr (KIND != kRowsBf16) {
+      ksc = a.ks[max(at, 0)];
+      vsc = a.vs[max(at, 0)];
     }
-  } else {
-    BlockCut c;
-    if (!block_cut(a, item, true, c)) return;
-    place = (size_t)parts * units + item;
-    const int local = item - c.item0, g = local / c.items, chunk = local % c.items, b = c.b;
-    const int32_t* list = a.list ? a.list + (size_t)(b * a.Hkv + g) * a.list_ld : nullptr;
-    const int nb = a.list ? a.list_ld : c.blocks;
-    const int e0 = (int)((int64_t)chunk * nb / c.items), e1 = (int)((int64_t)(chunk + 1) * nb / c.items);
-    const unsigned char* qp = (const unsigned char*)a.q + ((size_t)b * a.Hq + g * a.G + (hval ? l16 : 0)) * D * 2;
-    u32x4 q[D / 32];
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j) {
-      const int off = KIND == kRowsBf16 ? 64 * j + 16 * lg : (64 * (j / 2) + 16 * lg + 8 * (j & 1)) * 2;
-      q[j] = hval ? *(const u32x4*)(qp + off) : u32x4{0u, 0u, 0u, 0u};
+    left = __builtin_amdgcn_ballot_w64(at >= 0);
+  };
+  // to the next 32 rows; false: there are none
+  auto next = [&]() {
+    if (left && sub + 32 < (e + __builtin_ctzll(left) == e1 - 1 ? cut : B)) {
+      sub += 32;
+      return true;
     }
-    // The next 64 blocks of the item, one a lane: place and scales.  Those whose pages are
-    // not there have no bit in `left`.
-    int at, e = e0, sub = 0;
-    float ksc = 1.f, vsc = 1.f;
-    uint64_t left = 0;
-    auto look = [&]() {
-      const int i = e + lane;
-      at = i >= e1 ? -1 : (list ? list[i] : block_at(a, c.slot, g, i));
-      if constexpr (KIND != kRowsBf16) {
-        ksc = a.ks[max(at, 0)];
-        vsc = a.vs[max(at, 0)];
-      }
-      left = __builtin_amdgcn_ballot_w64(at >= 0);
-    };
-    // to the next 32 rows; false: there are none
-    auto next = [&]() {
-      if (left && sub + 32 < B) {
-        sub += 32;
-        return true;
-      }
-      sub = 0;
-      left &= left - 1;
-      while (!left && (e += 64) < e1) {
-        look();
-        settle(at);
-        settle(ksc);
-        settle(vsc);
-      }
-      return left != 0;
-    };
-    auto load_k = [&](const unsigned char* kp, u32x4 (&k0)[NK], u32x4 (&k1)[NK]) {
-#pragma unroll
-      for (int j = 0; j < NK; ++j) {
-        k0[j] = load_as<NT, u32x4>(kp + 64 * j);
-        k1[j] = load_as<NT, u32x4>(kp + 16 * (D * E) + 64 * j);
-      }
-    };
-    const int koff = l16 * (D * E) + 16 * lg, voff = 4 * lg * (D * E) + l16 * (VE * E);
-    // the row of the 32 that are next, and their scales
-    auto row = [&]() {
-      return ((size_t)(uint32_t)__builtin_amdgcn_readlane(at, __builtin_ctzll(left)) << a.block_shift) + sub;
-    };
-    auto of = [&](float v) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), __builtin_ctzll(left))); };
-    bool more = false;
-    if (e0 < e1) {
+    sub = 0;
+    left &= left - 1;
+    while (!left && (e += 64) < e1) {
       look();
-      more = left != 0;
-      if (!more) {
-        left = 0;
-        more = next();
-      }
+      settle(at);
+      settle(ksc);
+      settle(vsc);
     }
-    u32x4 k0[NK], k1[NK];
-    size_t r = 0;
-    float xk = 1.f, xv = 1.f;
+    return left != 0;
+  };
+  auto load_k = [&](const unsigned char* kp, u32x4 (&k0)[NK], u32x4 (&k1)[NK]) {
+#pragma unroll
+    for (int j = 0; j < NK; ++j) {
+      k0[j] = load_as<NT, u32x4>(kp + 64 * j);
+      k1[j] = load_as<NT, u32x4>(kp + 16 * (D * E) + 64 * j);
+    }
+  };
+  const int koff = l16 * (D * E) + 16 * lg, voff = 4 * lg * (D * E) + l16 * (VE * E);
+  // the first of the 32 rows that are next, and a scale of theirs
+  auto row = [&]() {
+    return ((size_t)(uint32_t)__builtin_amdgcn_readlane(at, __builtin_ctzll(left)) << a.block_shift) + sub;
+  };
+  auto of = [&](float v) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), __builtin_ctzll(left))); };
+  bool more = false;
+  if (first < end) {
+    look();
+    more = left & 1;  // (the first block: from its row `sub` on)
+    if (!more) {
+      sub = 0;
+      more = left != 0;
+      if (!more) more = next();
+    }
+  }
+  u32x4 k0[NK], k1[NK];
+  size_t r = 0;
+  float xk = 1.f, xv = 1.f;
+  if (more) {
+    r = row();
+    load_k(a.ck + r * (D * E) + koff, k0, k1);
+    xk = of(ksc);
+    xv = of(vsc);
+  }
+#pragma unroll
+  for (int j = 0; j < D / 32; ++j) settle(q[j]);
+  settle(ksc);
+  settle(vsc);
+  while (more) {
+    // values of these rows, then keys of the next: the second product waits for the values
+    // only
+    VRaw v[8];
+    const unsigned char* vp = a.cv + r * (D * E) + voff;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = load_as<NT, VRaw>(vp + ((i < 4 ? 0 : 16) + (i & 3)) * (D * E));
+    const float xs = a.scale2 * xk, xlo = a.scale2_lo * xk, vs = xv;
+    u32x4 n0[NK], n1[NK];
+    more = next();
     if (more) {
       r = row();
-      load_k(a.ck + r * (D * E) + koff, k0, k1);
+      load_k(a.ck + r * (D * E) + koff, n0, n1);
       xk = of(ksc);
       xv = of(vsc);
     }
+    f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j) settle(q[j]);
-    settle(ksc);
-    settle(vsc);
-    while (more) {
-      // values of these rows, then keys of the next: the second product waits for the
-      // values only
-      VRaw v[8];
-      const unsigned char* vp = a.cv + r * (D * E) + voff;
+    for (int j = 0; j < NK; ++j) {
+      if constexpr (KIND == kRowsBf16) {
+        s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k0[j]), __builtin_bit_cast(bf16x8, q[j]), s0, 0, 0, 0);
+        s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k1[j]), __builtin_bit_cast(bf16x8, q[j]), s1, 0, 0, 0);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = load_as<NT, VRaw>(vp + ((i < 4 ? 0 : 16) + (i & 3)) * (D * E));
-      const float xs = a.scale2 * xk, xlo = a.scale2_lo * xk, vs = xv;
-      u32x4 n0[NK], n1[NK];
-      more = next();
-      if (more) {
-        r = row();
-        load_k(a.ck + r * (D * E) + koff, n0, n1);
-        xk = of(ksc);
-        xv = of(vsc);
-      }
-      f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int j = 0; j < NK; ++j) {
-        if constexpr (KIND == kRowsBf16) {
-          s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k0[j]), __builtin_bit_cast(bf16x8, q[j]), s0, 0, 0, 0);
-          s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k1[j]), __builtin_bit_cast(bf16x8, q[j]), s1, 0, 0, 0);
-        } else {
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const bf16x8 qq = __builtin_bit_cast(bf16x8, q[2 * j + u]);
-            const u32x2 a0 = bf16x4<KIND>(k0[j][2 * u]), a1 = bf16x4<KIND>(k0[j][2 * u + 1]);
-            const u32x2 b0 = bf16x4<KIND>(k1[j][2 * u]), b1 = bf16x4<KIND>(k1[j][2 * u + 1]);
-            s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{a0[0], a0[1], a1[0], a1[1]}), qq, s0, 0, 0, 0);
-            s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{b0[0], b0[1], b1[0], b1[1]}), qq, s1, 0, 0, 0);
-          }
+        for (int u = 0; u < 2; ++u) {
+          const bf16x8 qq = __builtin_bit_cast(bf16x8, q[2 * j + u]);
+          const u32x2 a0 = bf16x4<KIND>(k0[j][2 * u]), a1 = bf16x4<KIND>(k0[j][2 * u + 1]);
+          const u32x2 b0 = bf16x4<KIND>(k1[j][2 * u]), b1 = bf16x4<KIND>(k1[j][2 * u + 1]);
+          s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{a0[0], a0[1], a1[0], a1[1]}), qq, s0, 0, 0, 0);
+          s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{b0[0], b0[1], b1[0], b1[1]}), qq, s1, 0, 0, 0);
         }
-      }
-      const float x[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
-      float pe[8];
-      o.softmax(x, xs, xlo, vs, pe);
-      uint32_t vw[8][VE / 2];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if constexpr (KIND == kRowsBf16) {
-#pragma unroll
-          for (int u = 0; u < VE / 2; ++u) vw[i][u] = v[i][u];
-        } else {
-#pragma unroll
-          for (int u = 0; u < VE / 4; ++u) {
-            const u32x2 w = bf16x4<KIND>(v[i][u]);
-            vw[i][2 * u] = w[0];
-            vw[i][2 * u + 1] = w[1];
-          }
-        }
-      }
-      o.values(pe, vw);
-#pragma unroll
-      for (int j = 0; j < NK; ++j) {
-        k0[j] = n0[j];
-        k1[j] = n1[j];
       }
     }
+    const float x[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
+    float pe[8];
+    o.softmax(x, xs, xlo, vs, pe);
+    uint32_t vw[8][VE / 2];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (KIND == kRowsBf16) {
+#pragma unroll
+        for (int u = 0; u < VE / 2; ++u) vw[i][u] = v[i][u];
+      } else {
+#pragma unroll
+        for (int u = 0; u < VE / 4; ++u) {
+          const u32x2 w = bf16x4<KIND>(v[i][u]);
+          vw[i][2 * u] = w[0];
+          vw[i][2 * u + 1] = w[1];
+        }
+      }
+    }
+    o.values(pe, vw);
+#pragma unroll
+    for (int j = 0; j < NK; ++j) {
+      k0[j] = n0[j];
+      k1[j] = n1[j];
+    }
+  }
+}
+
+// The first workgroups take a work item each, B / 32 a unit attend 32 rows each of the
+// newest token's block, the last two a unit store a step's token: the longest first, so
+// that the short ones fill the gaps.
+template <int D, int KIND, bool NT>
+__global__ __launch_bounds__(64) void block_attn(BlockArgs a) {
+  constexpr int VE = D / 16;
+  const int lane = tid() & 63, l16 = lane & 15, lg = lane >> 4, units = a.n * a.Hkv;
+  const int parts = 1 << (a.block_shift - 5), item = bid_x(), w = item - a.max_items;
+  if (w >= parts * units) {
+    const int i = w - parts * units;
+    put_token<D, KIND>(a, i >> 1, !(i & 1));
+    return;
+  }
+  Soft<D> o;
+  o.init();
+  if (w >= 0) {
+    const int unit = w / parts, r0 = w % parts * 32, b = unit / a.Hkv, g = unit % a.Hkv;
+    const BlockSeq s = block_seq(a, b);
+    const int at = s.tail && r0 <= (s.row & ((1 << a.block_shift) - 1)) ? uniform(block_at(a, s.slot, g, s.row >> a.block_shift)) : -1;
+    if (at >= 0) attend_newest<D, KIND>(a, s, b, g, at, r0, o);
+  } else {
+    BlockCut c;
+    if (!block_cut(a, item, true, c)) return;
+    const int local = item - c.item0, g = local / c.items, chunk = local % c.items;
+    const int nb = a.list ? a.list_ld : c.blocks;
+    const int e0 = (int)((int64_t)chunk * nb / c.items), e1 = (int)((int64_t)(chunk + 1) * nb / c.items);
+    attend_blocks<D, KIND, NT>(a, c.b, g, c.slot, a.list ? a.list + (size_t)(c.b * a.Hkv + g) * a.list_ld : nullptr,
+                               e0 << (a.block_shift - 5), e1 << (a.block_shift - 5), o);
   }
   o.lsum += __shfl_xor(o.lsum, 16);
   o.lsum += __shfl_xor(o.lsum, 32);
-  if (!hval) return;
-  const size_t pi = place * a.G + l16;
+  if (l16 >= a.G) return;
+  const size_t pi = (size_t)(w < 0 ? parts * units + item : w) * a.G + l16;  // the units' parts of the newest block, then the items
   if (lg == 0) a.ml[pi] = make_float2(o.m, o.lsum);
   float* dst = a.part + pi * D + 4 * lg * VE;
 #pragma unroll
@@ -1176,6 +1200,90 @@ __global__ __launch_bounds__(64) void block_attn(BlockArgs a) {
 #pragma unroll
     for (int c = 0; c < VE; c += 4)
       *(f32x4*)(dst + e * VE + c) = f32x4{o.acc[c][e], o.acc[c + 1][e], o.acc[c + 2][e], o.acc[c + 3][e]};
+}
+
+// The same for short calls in one launch: a workgroup takes a whole unit, each wave a share
+// of its 32-row steps, and joins them in LDS.
+constexpr int kUnitWaves = 8;
+template <int D, int KIND>
+__global__ __launch_bounds__(64 * kUnitWaves) void block_attn_unit(BlockArgs a) {
+  extern __shared__ __align__(16) float joins[];  // [kUnitWaves / 2][G][D]
+  constexpr int VE = D / 16, W = kUnitWaves;
+  __shared__ float2 mls[W][16];
+  const int lane = tid() & 63, w = uniform(tid() >> 6), l16 = lane & 15, lg = lane >> 4, unit = bid_x();
+  const int b = unit / a.Hkv, g = unit % a.Hkv, steps = a.block_shift - 5;
+  const BlockSeq s = block_seq(a, b);
+  if (s.slot < 0 || s.slot >= a.n_slots) {  // no rows: zeros
+    if (w == 0 && l16 < a.G)
+      for (int i = lg; i < D; i += 4) {
+        const size_t oi = ((size_t)b * a.Hq + g * a.G + l16) * D + i;
+        if (a.out_bf16) ((uint16_t*)a.out)[oi] = 0;
+        else ((float*)a.out)[oi] = 0.f;
+      }
+    return;
+  }
+  const bool hval = l16 < a.G;
+  const int nb = a.list ? a.list_ld : s.blocks, codes = nb << steps;
+  const int at = s.tail ? uniform(block_at(a, s.slot, g, s.row >> a.block_shift)) : -1;
+  const int total = codes + (at < 0 ? 0 : ((s.row & ((1 << a.block_shift) - 1)) >> 5) + 1);
+  const int s0 = w * total / W, s1 = (w + 1) * total / W;
+  Soft<D> o;
+  o.init();
+  if (s0 < codes)
+    attend_blocks<D, KIND, false>(a, b, g, s.slot, a.list ? a.list + (size_t)unit * a.list_ld : nullptr, s0, min(s1, codes), o);
+  for (int i = max(s0, codes); i < s1; ++i) attend_newest<D, KIND>(a, s, b, g, at, (i - codes) * 32, o);
+  o.lsum += __shfl_xor(o.lsum, 16);
+  o.lsum += __shfl_xor(o.lsum, 32);
+  if (lg == 0) mls[w][l16] = make_float2(o.m, o.lsum);
+  __syncthreads();
+  float M = -INFINITY, L = 0.f;
+#pragma unroll
+  for (int i = 0; i < W; ++i) M = fmaxf(M, mls[i][l16].x);
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    const float2 v = mls[i][l16];
+    if (v.x != -INFINITY) L = fmaf(fast_exp2(v.x - M), v.y, L);
+  }
+  const float f = o.m == -INFINITY ? 0.f : fast_exp2(o.m - M) * (L > 0.f ? 1.f / L : 0.f);
+#pragma unroll
+  for (int c = 0; c < VE; ++c) o.acc[c] *= f;
+  // the upper half of the waves hand theirs to the lower, until one has the sum
+#pragma unroll
+  for (int half = W / 2; half >= 1; half /= 2) {
+    float* to = joins + ((w & (half - 1)) * a.G + l16) * D + 4 * lg * VE;
+    if (w >= half && w < 2 * half && hval)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int c = 0; c < VE; c += 4)
+          *(f32x4*)(to + e * VE + c) = f32x4{o.acc[c][e], o.acc[c + 1][e], o.acc[c + 2][e], o.acc[c + 3][e]};
+    __syncthreads();
+    if (w < half && hval)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int c = 0; c < VE; c += 4) {
+          const f32x4 v = *(const f32x4*)(to + e * VE + c);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o.acc[c + i][e] += v[i];
+        }
+    __syncthreads();
+  }
+  if (w == 0 && hval) {
+    const size_t oi = ((size_t)b * a.Hq + g * a.G + l16) * D + 4 * lg * VE;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int c = 0; c < VE; c += 4) {
+        const f32x4 v = {o.acc[c][e], o.acc[c + 1][e], o.acc[c + 2][e], o.acc[c + 3][e]};
+        if (a.out_bf16)
+          *(u32x2*)((uint16_t*)a.out + oi + e * VE + c) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+        else
+          *(f32x4*)((float*)a.out + oi + e * VE + c) = v;
+      }
+  }
+  // (no wave reads the newest row but from the input, nor the block it may complete)
+  if (a.k_new && (w == W - 1 || w == W - 2)) put_token<D, KIND>(a, unit, w == W - 1);
 }
 
 // ---------------------------------------------------------------- join
@@ -1310,14 +1418,36 @@ BlockGeometry block_geometry(const snap_params& p, int n, int max_rows, int bloc
   return g;
 }
 
-// Blocks whose keys stand in LDS beside what scoring needs there (78 KB of 160).
-constexpr int kFusedBlocks = 8192;
-// The workgroups that score a unit's blocks before they are chosen among; 1: the one that
-// chooses.
-static int score_splits(const snap_params& p, int units, int blocks) {
-  const int least = blocks > kFusedBlocks ? 2 : 1;
-  if (const char* e = getenv("SPLITS")) return atoi(e) > least ? atoi(e) : least;
-  return least;
+// Whether a unit's blocks are scored by a launch of their own, kBatch of them a workgroup,
+// or by the one workgroup that chooses among them.  That one takes in about 40 bytes a
+// nanosecond; the launch costs 3 to 4 us.  Whole calls, 8 KV heads, one launch / two, us:
+//   bounds a unit           128 KB      256 KB      512 KB      1 MB        2 MB
+//   d 128     1 sequence   21.4/23.9   23.4/23.0   27.7/23.9   36.9/25.4   57/28.5
+//             4            23.5/26.2   28.8/27.9   34.1/29.7   44.8/33.6   69/41.5
+//            16            38.1/40.6   38.0/39.0   45.3/45.9   61.9/56.2  115/91
+//            32            56.4/59.7   54.3/56.2   67.9/67.3  100/91
+//   d 64      1            19.4/21.7   24.3/22.5   31.3/23.7   45.0/26.0
+//            16            27.6/31.2   34.4/34.8   45.1/44.6   70.4/58.4
+// (It also keeps the keys of the one that scores, beside 78 KB of its own, within LDS.)
+static bool scored_apart(const snap_params& p, int units, int blocks) {
+  const size_t bytes = (size_t)blocks * 2 * p.d_qk;
+  return units <= 64 ? bytes >= (size_t)256 << 10 : bytes > (size_t)512 << 10;
+}
+
+// Whether a workgroup of eight waves takes a whole unit, so that one launch does: with
+// few units while a wave has two steps of 32 rows (64-wide) or one, with enough units to
+// fill the card while it has eight (then nothing is written for the join).  Measured, one
+// launch / two, 32 query heads on 8 (64-wide: 8 KV heads), us of a replayed call:
+//   rows              256        512        1024       2048
+//   128 int8   1 x  12.3/9.8   14.6/10.4  17.6/10.2  24.6/10.5   32 x 16/17  19/20  24/24  33/38
+//   128 fp8    1 x   9.8/8.4   11.4/8.4   14.2/8.6   19.4/9.4    32 x 10/13  12/17  18/21  27/35
+//   128 bf16   1 x   8.6/9.1   10.8/9.1   15.6/9.2   24.2/9.7    32 x  9/13  15/19  25/33  43/52
+//   64 int8    1 x   8.3/8.3    9.3/8.3   11.9/8.3   16.5/8.6    32 x  9/12  10/14  13/16  18/21
+//   64 bf16    1 x   6.3/8.7    7.7/8.7   10.7/8.8   16.1/8.8    32 x  6/11   8/13  15/20  24/30
+// (calls that are not replayed cost the host 9 us with one launch, 11 with two)
+static bool whole_units(const snap_params& p, int units, int blocks, int block) {
+  const int share = units * kUnitWaves >= 2048 ? 8 : (p.d_qk == 64 ? 2 : 1);
+  return (int64_t)(blocks + 1) * (block / 32) <= share * kUnitWaves;
 }
 
 snap_status launch_block_append(const snap_params& p, const snap_block_cache& c, const int32_t* rows, int n,
@@ -1371,20 +1501,28 @@ snap_status launch_block_decode(const snap_params& p, const snap_block_cache& c,
     a.sink = p.sink;
     a.recent = p.recent;
     a.best = (p.topk + c.block - 1) / c.block;
-    const int splits = score_splits(p, units, geo.blocks);
-    if (splits > 1) {
-      const int chunk = ((geo.blocks + splits - 1) / splits + 63) / 64 * 64;
+    const bool apart = scored_apart(p, units, geo.blocks);
+    if (apart) {
       a.keys = (uint32_t*)((unsigned char*)ws + geo.off_keys);
       a.key_ld = geo.blocks;
+      const int chunk = p.d_qk == 128 ? BlockScores<128, kScoreThreads / 64>::kBatch : BlockScores<64, kScoreThreads / 64>::kBatch;
       hipLaunchKernelGGL((p.d_qk == 128 ? block_score<128> : block_score<64>), dim3((geo.blocks + chunk - 1) / chunk, units),
-                         dim3(kScoreThreads), 0, stream, a, chunk);
+                         dim3(kScoreThreads), 0, stream, a);
       if (hipGetLastError() != hipSuccess) return SNAP_ERR_HIP;
     }
     const size_t lds = (size_t)(geo.blocks < 1 ? 1 : geo.blocks) * sizeof(uint32_t);
     static constexpr void (*choose[2][2])(BlockArgs) = {{block_select<64, false>, block_select<64, true>},
                                                         {block_select<128, false>, block_select<128, true>}};
-    hipLaunchKernelGGL(choose[p.d_qk == 128][splits > 1], dim3(units), dim3(kSelThreadsB), lds, stream, a);
+    hipLaunchKernelGGL(choose[p.d_qk == 128][apart], dim3(units), dim3(kSelThreadsB), lds, stream, a);
     if (hipGetLastError() != hipSuccess) return SNAP_ERR_HIP;
+  }
+  if (whole_units(p, units, select ? geo.list_ld : geo.blocks, c.block)) {
+    static constexpr void (*kernels[2][3])(BlockArgs) = {
+        {block_attn_unit<64, kRowsBf16>, block_attn_unit<64, kRowsFp8>, block_attn_unit<64, kRowsInt8>},
+        {block_attn_unit<128, kRowsBf16>, block_attn_unit<128, kRowsFp8>, block_attn_unit<128, kRowsInt8>}};
+    hipLaunchKernelGGL(kernels[p.d_qk == 128][kind_of(p.kv_dtype)], dim3(units), dim3(64 * kUnitWaves),
+                       (size_t)(kUnitWaves / 2) * a.G * p.d_v * sizeof(float), stream, a);
+    return hipGetLastError() == hipSuccess ? SNAP_OK : SNAP_ERR_HIP;
   }
   // streaming loads where the blocks read are more than half the last-level cache
   const size_t row_bytes = (size_t)2 * p.d_qk * (p.kv_dtype == SNAP_BF16 ? 2 : 1);
