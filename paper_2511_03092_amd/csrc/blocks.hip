@@ -882,6 +882,10 @@ __global__ __launch_bounds__(kSelThreadsB) void block_select(BlockArgs a) {
 
 // ---------------------------------------------------------------- attention
 constexpr float kStaleMax = 8.f;
+// Sums of values are in units of 2^40: a probability is up to 2^8 beside a reference that
+// lags, and 2^28 rows of them times a value of 2^127 are then finite, as the mean is.  What
+// that flushes is below 2^-86 of a unit value.
+constexpr float kDown = 0x1p-40f, kUp = 0x1p40f;
 
 // Eight probabilities as three bf16 terms, whose sum they are (pe is used up).
 __device__ __forceinline__ void three_terms(float (&pe)[8], bf16x8 (&p)[3]) {
@@ -1008,7 +1012,7 @@ __device__ __forceinline__ void attend_newest(const BlockArgs& a, const BlockSeq
 #pragma unroll
     for (int u = 0; u < VE / 2; ++u) vw[i][u] = v[i][u];
   }
-  o.softmax(x, a.scale2, a.scale2_lo, 1.f, pe);
+  o.softmax(x, a.scale2, a.scale2_lo, kDown, pe);
   o.values(pe, vw);
 }
 
@@ -1107,7 +1111,7 @@ __device__ __forceinline__ void attend_blocks(const BlockArgs& a, int b, int g, 
     const unsigned char* vp = a.cv + r * (D * E) + voff;
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = load_as<NT, VRaw>(vp + ((i < 4 ? 0 : 16) + (i & 3)) * (D * E));
-    const float xs = a.scale2 * xk, xlo = a.scale2_lo * xk, vs = xv;
+    const float xs = a.scale2 * xk, xlo = a.scale2_lo * xk, vs = xv * kDown;
     u32x4 n0[NK], n1[NK];
     more = next();
     if (more) {
@@ -1275,7 +1279,7 @@ __global__ __launch_bounds__(64 * kUnitWaves) void block_attn_unit(BlockArgs a) 
     for (int e = 0; e < 4; ++e)
 #pragma unroll
       for (int c = 0; c < VE; c += 4) {
-        const f32x4 v = {o.acc[c][e], o.acc[c + 1][e], o.acc[c + 2][e], o.acc[c + 3][e]};
+        const f32x4 v = f32x4{o.acc[c][e], o.acc[c + 1][e], o.acc[c + 2][e], o.acc[c + 3][e]} * kUp;
         if (a.out_bf16)
           *(u32x2*)((uint16_t*)a.out + oi + e * VE + c) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
         else
@@ -1337,6 +1341,7 @@ __global__ __launch_bounds__(kJoinThreads) void block_join(BlockArgs a) {
 #pragma unroll
   for (int i = 1; i < CL; ++i) o += sacc[dg + DG * i];
   o *= L > 0.f ? 1.f / L : 0.f;
+  o *= kUp;
   const size_t oi = (size_t)bh * D + 4 * dg;
   if (a.out_bf16)
     *(u32x2*)((uint16_t*)a.out + oi) = u32x2{f32_to_bf16_bits(o[0]) | (f32_to_bf16_bits(o[1]) << 16),
