@@ -654,23 +654,22 @@ struct BlockScores {
     // Loads take 1 KB of neighbouring bytes (with the rows of a matrix operand a lane each,
     // 64 bytes of 16 blocks, the L1 passes 16 bytes a clock); the operand is made in LDS.
     u32x4 x[N][NK];
-    auto load = [&](int j0) {
+    // blocks j1 + l16 into place i, and the page of those that follow there
+    auto load = [&](int i, int j1) {
+      if (j1 >= end) return;  // (the whole wave)
+      const int j = j1 + l16;
+      at[i] = j < end ? c.place(a, j, pages[i]) : -1;
+      bs[i] = a.bscale[max(at[i], 0)];
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int j = j0 + kStep * i + l16;
-        if (j - l16 >= end) continue;  // (of the whole wave)
-        at[i] = j < end ? c.place(a, j, pages[i]) : -1;
-        bs[i] = a.bscale[max(at[i], 0)];
-#pragma unroll
-        for (int k = 0; k < NK; ++k) {
-          const int piece = 64 * k + lane, block = __shfl(at[i], piece / P);
-          x[i][k] = *(const u32x4*)(a.bound + ((size_t)max(block, 0) * P + piece % P) * 16);
-        }
+      for (int k = 0; k < NK; ++k) {
+        const int piece = 64 * k + lane, block = __shfl(at[i], piece / P);
+        x[i][k] = *(const u32x4*)(a.bound + ((size_t)max(block, 0) * P + piece % P) * 16);
       }
-      if (j0 + kStep * N < end) load_pages(a, c, j0 + kStep * N);
+      if (j1 + kBatch < end) pages[i] = c.page(a, j + kBatch);
     };
     int j0 = first + 16 * w;
-    load(j0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) load(i, j0 + kStep * i);
 #pragma unroll
     for (int k = 0; k < Q; ++k) {
       const int h = w + W * k;
@@ -696,7 +695,7 @@ struct BlockScores {
 #pragma unroll
     for (int i = 0; i < NK; ++i) q[i] = *(const i32x4*)(&sh.a[l16][64 * i + 16 * lg]);
     const float u = sh.u[l16];
-    for (; j0 < end; j0 += kStep * N) {
+    for (; j0 < end; j0 += kBatch) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int j1 = j0 + kStep * i;
@@ -719,8 +718,8 @@ struct BlockScores {
         const float scale = __shfl(bs[i], from_lane);
         const int place = __shfl(at[i], from_lane);
         if (l16 < 4 && j1 + from_lane < end) emit(j1 + from_lane, place < 0 ? 0u : score_key(mine * scale));
+        load(i, j1 + kBatch);
       }
-      if (j0 + kStep * N < end) load(j0 + kStep * N);
     }
   }
 };
@@ -1024,7 +1023,9 @@ __device__ __forceinline__ void attend_newest(const BlockArgs& a, const BlockSeq
 // product takes from it; its keys are 16 bytes at byte 64 j + 16 lg of row l16, its values
 // the D / 16 dims from (D / 16) l16 of eight rows.  Every row of a whole block is there, so
 // nothing is masked.
-template <int D, int KIND, bool NT>
+// AHEAD: the values are loaded a step before they are needed, as the keys are; that changes
+// nothing where the card is full of waves.
+template <int D, int KIND, bool NT, bool AHEAD>
 __device__ __forceinline__ void attend_blocks(const BlockArgs& a, int b, int g, int slot, const int32_t* list, int first, int end, Soft<D>& o) {
   constexpr int E = KIND == kRowsBf16 ? 2 : 1, VE = D / 16, NK = D * E / 64;
   typedef uint32_t VRaw __attribute__((ext_vector_type(VE * E / 4)));
@@ -1091,12 +1092,19 @@ __device__ __forceinline__ void attend_blocks(const BlockArgs& a, int b, int g, 
       if (!more) more = next();
     }
   }
+  auto load_v = [&](size_t r, VRaw (&v)[8]) {
+    const unsigned char* vp = a.cv + r * (D * E) + voff;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = load_as<NT, VRaw>(vp + ((i < 4 ? 0 : 16) + (i & 3)) * (D * E));
+  };
   u32x4 k0[NK], k1[NK];
+  VRaw v[8];
   size_t r = 0;
   float xk = 1.f, xv = 1.f;
   if (more) {
     r = row();
     load_k(a.ck + r * (D * E) + koff, k0, k1);
+    if (AHEAD) load_v(r, v);
     xk = of(ksc);
     xv = of(vsc);
   }
@@ -1107,16 +1115,15 @@ __device__ __forceinline__ void attend_blocks(const BlockArgs& a, int b, int g, 
   while (more) {
     // values of these rows, then keys of the next: the second product waits for the values
     // only
-    VRaw v[8];
-    const unsigned char* vp = a.cv + r * (D * E) + voff;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = load_as<NT, VRaw>(vp + ((i < 4 ? 0 : 16) + (i & 3)) * (D * E));
+    if (!AHEAD) load_v(r, v);
+    VRaw nv[8];
     const float xs = a.scale2 * xk, xlo = a.scale2_lo * xk, vs = xv * kDown;
     u32x4 n0[NK], n1[NK];
     more = next();
     if (more) {
       r = row();
       load_k(a.ck + r * (D * E) + koff, n0, n1);
+      if (AHEAD) load_v(r, nv);
       xk = of(ksc);
       xv = of(vsc);
     }
@@ -1161,6 +1168,9 @@ __device__ __forceinline__ void attend_blocks(const BlockArgs& a, int b, int g, 
       k0[j] = n0[j];
       k1[j] = n1[j];
     }
+    if (AHEAD)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = nv[i];
   }
 }
 
@@ -1190,7 +1200,7 @@ __global__ __launch_bounds__(64) void block_attn(BlockArgs a) {
     const int local = item - c.item0, g = local / c.items, chunk = local % c.items;
     const int nb = a.list ? a.list_ld : c.blocks;
     const int e0 = (int)((int64_t)chunk * nb / c.items), e1 = (int)((int64_t)(chunk + 1) * nb / c.items);
-    attend_blocks<D, KIND, NT>(a, c.b, g, c.slot, a.list ? a.list + (size_t)(c.b * a.Hkv + g) * a.list_ld : nullptr,
+    attend_blocks<D, KIND, NT, false>(a, c.b, g, c.slot, a.list ? a.list + (size_t)(c.b * a.Hkv + g) * a.list_ld : nullptr,
                                e0 << (a.block_shift - 5), e1 << (a.block_shift - 5), o);
   }
   o.lsum += __shfl_xor(o.lsum, 16);
@@ -1234,7 +1244,7 @@ __global__ __launch_bounds__(64 * kUnitWaves) void block_attn_unit(BlockArgs a) 
   Soft<D> o;
   o.init();
   if (s0 < codes)
-    attend_blocks<D, KIND, false>(a, b, g, s.slot, a.list ? a.list + (size_t)unit * a.list_ld : nullptr, s0, min(s1, codes), o);
+    attend_blocks<D, KIND, false, true>(a, b, g, s.slot, a.list ? a.list + (size_t)unit * a.list_ld : nullptr, s0, min(s1, codes), o);
   for (int i = max(s0, codes); i < s1; ++i) attend_newest<D, KIND>(a, s, b, g, at, (i - codes) * 32, o);
   o.lsum += __shfl_xor(o.lsum, 16);
   o.lsum += __shfl_xor(o.lsum, 32);
@@ -1440,19 +1450,28 @@ static bool scored_apart(const snap_params& p, int units, int blocks) {
 }
 
 // Whether a workgroup of eight waves takes a whole unit, so that one launch does: with
-// few units while a wave has two steps of 32 rows (64-wide) or one, with enough units to
-// fill the card while it has eight (then nothing is written for the join).  Measured, one
-// launch / two, 32 query heads on 8 (64-wide: 8 KV heads), us of a replayed call:
-//   rows              256        512        1024       2048
-//   128 int8   1 x  12.3/9.8   14.6/10.4  17.6/10.2  24.6/10.5   32 x 16/17  19/20  24/24  33/38
-//   128 fp8    1 x   9.8/8.4   11.4/8.4   14.2/8.6   19.4/9.4    32 x 10/13  12/17  18/21  27/35
-//   128 bf16   1 x   8.6/9.1   10.8/9.1   15.6/9.2   24.2/9.7    32 x  9/13  15/19  25/33  43/52
-//   64 int8    1 x   8.3/8.3    9.3/8.3   11.9/8.3   16.5/8.6    32 x  9/12  10/14  13/16  18/21
-//   64 bf16    1 x   6.3/8.7    7.7/8.7   10.7/8.8   16.1/8.8    32 x  6/11   8/13  15/20  24/30
+// few units while a wave has two steps of 32 rows (64-wide) or one, with 128 while it has
+// four, with enough units to fill the card while it has eight, or 16 of 128 bytes a row
+// (then nothing is written for the join).  Measured, one launch / two, 32 query heads on 8,
+// us of a replayed call:
+//   rows                250         500        1000        2000        3900
+//   128 int8   1 x   8.9/9.7   10.7/9.8   14.4/9.8   21.6/10.3   35.5/11.4
+//             16     9.0/10.6  10.8/11.8  15.3/15.1  22.7/21.1   37.0/29.7
+//             32     9.0/12.6  11.7/15.9  17.9/21.8  27.3/31.2   45.6/52.6
+//             64    18.2/18.5  24.5/25.7  34.1/37.2  52.6/62.4   104/101
+//   128 bf16   1     8.7/9.0   10.8/9.1   16.2/9.2   24.1/9.7    40.6/11.0
+//             16     8.7/10.3  11.3/12.6  17.8/19.0  26.4/28.4   44.3/48.1
+//             32     9.5/13.2  15.7/19.4  25.0/30.0  43.2/50.7   91.8/90.9
+//             64    21.2/20.8  29.4/32.0  48.2/54.4  98.3/93.6   182/167
+//   64 int8    1     6.5/8.2    7.8/8.3   10.2/8.3   15.1/8.7    24.5/10.9
+//             16     6.5/9.3    7.9/10.4  10.3/12.1  16.0/15.1   26.0/19.9
+//             32     6.6/11.1   8.0/13.0  11.1/15.7  17.0/20.6   26.7/29.4
+//             64     8.2/14.8  11.2/17.4  18.2/22.4  27.9/31.6   45.7/53.4
 // (calls that are not replayed cost the host 9 us with one launch, 11 with two)
 static bool whole_units(const snap_params& p, int units, int blocks, int block) {
-  const int share = units * kUnitWaves >= 2048 ? 8 : (p.d_qk == 64 ? 2 : 1);
-  return (int64_t)(blocks + 1) * (block / 32) <= share * kUnitWaves;
+  const int row_bytes = 2 * p.d_qk * (p.kv_dtype == SNAP_BF16 ? 2 : 1);
+  const int share = units >= 256 ? (row_bytes > 128 ? 8 : 16) : (units >= 128 ? 4 : (p.d_qk == 64 ? 2 : 1));
+  return (int64_t)blocks * (block / 32) <= share * kUnitWaves;
 }
 
 snap_status launch_block_append(const snap_params& p, const snap_block_cache& c, const int32_t* rows, int n,

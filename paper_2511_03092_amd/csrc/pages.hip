@@ -31,16 +31,12 @@ struct PoolArgs {
   int n, len, n_slots, n_pages, page_shift, max_pages;
 };
 
-// Inclusive prefix sum over a workgroup of W waves (every thread calls); `total`: of
-// all.  64 bits: a thousand sequences may lack 2^24 pages each.
+// Inclusive prefix sum of numbers that are not negative over a workgroup of W waves (every
+// thread calls); `total`: of all.  64 bits: a thousand sequences may lack 2^24 pages each.
 template <int W>
-__device__ __forceinline__ int64_t group_scan(int64_t v, int64_t* red, int64_t& total) {
+__device__ __forceinline__ int64_t group_scan(int x, int64_t* red, int64_t& total) {
   const int lane = tid() & 63, w = tid() >> 6;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t u = __shfl_up((long long)v, o);
-    if (lane >= o) v += u;
-  }
+  int64_t v = wave_scan(x & 0xffff) + ((int64_t)wave_scan(x >> 16) << 16);
   __syncthreads();
   if (lane == 63) red[w] = v;
   __syncthreads();
@@ -84,8 +80,8 @@ __global__ __launch_bounds__(kPoolThreads) void pages_reserve(PoolArgs a) {
     const int64_t want = ((int64_t)(r < 0 ? 0 : r) + (add < 0 ? 0 : add) + (1 << a.page_shift) - 1) >> a.page_shift;
     const int64_t lack = slot >= 0 && r >= 0 && want > h ? want - h : 0;
     const bool fits = want <= a.max_pages;
-    int64_t total, mine = fits ? lack : 0;
-    const int64_t upto = before + group_scan<kPoolWaves>(mine, red, total);
+    int64_t total;
+    const int64_t upto = before + group_scan<kPoolWaves>(fits ? (int)lack : 0, red, total);
     const bool served = fits && (lack == 0 || upto <= free0);
     if (b < a.n && a.short_out) a.short_out[b] = served ? 0 : (int)(lack < 0x7fffffff ? lack : 0x7fffffff);
     const int take = served ? (int)lack : 0;
