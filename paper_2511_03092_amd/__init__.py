@@ -634,13 +634,15 @@ def _pool(pool: SnapPagePool, rows, slot_ids) -> int:
 def snap_pages_reserve(pool: SnapPagePool, rows, slot_ids, lengths, short_out=None, stream=None):
     """Pages for lengths (int32 [n], or one number for all) more rows of each sequence; short_out [n]: the pages it lacks."""
     n, index = _pool(pool, rows, slot_ids), pool.index
-    one = lengths if isinstance(lengths, int) else 0
+    one = lengths if isinstance(lengths, int) else -1
     lengths = None if isinstance(lengths, int) else lengths
-    if lengths is not None or one < 0:
+    if lengths is not None:
         _want(lengths, "lengths", pool.i32, (n,), index)
+    elif not 0 <= one <= 0x7fffffff:
+        _bad(f"lengths must be int32 [n] or a number in [0, 2^31) (got {one})")
     if short_out is not None:
         _want(short_out, "short_out", pool.i32, (n,), index)
-    _launch(index, stream, lib().snap_pages_reserve, ctypes.byref(pool), _ptr(rows), n, _ptr(slot_ids), _ptr(lengths), one,
+    _launch(index, stream, lib().snap_pages_reserve, ctypes.byref(pool), _ptr(rows), n, _ptr(slot_ids), _ptr(lengths), max(one, 0),
             _ptr(short_out))
 
 

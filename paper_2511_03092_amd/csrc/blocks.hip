@@ -609,7 +609,7 @@ __device__ __forceinline__ void limits(const BlockArgs& a, int held, BlockChoice
   const int row = uniform(held);
   c.nb = row < 0 ? 0 : min(row, a.max_rows) >> a.block_shift;
   c.f0 = min(c.nb, c.f0);
-  const int f1 = row + 1 - a.recent;
+  const int f1 = row - (a.recent - 1);
   c.f1 = max(c.f0, min(c.nb, f1 <= 0 ? 0 : f1 >> a.block_shift));
   c.scored = c.f1 - c.f0 > a.best && a.best > 0;
 }
@@ -867,7 +867,7 @@ __global__ __launch_bounds__(kSelThreadsB) void block_select(BlockArgs a) {
     const uint64_t am = __builtin_amdgcn_ballot_w64(k > T), em = __builtin_amdgcn_ballot_w64(k != 0 && k == T);
     const int e = equal0 + __builtin_popcountll(em & below), i = above0 + __builtin_popcountll(am & below) + min(e, rem);
     const bool take = k > T || (k != 0 && k == T && e < rem);
-    if (take && debug_check(i < a.list_ld, kDbgBlockList)) {
+    if (take && debug_check(i < a.list_ld, kDbgBlockList) && i < a.list_ld) {
       list[i] = c.place(a, j, c.page(a, j));
       if (sel) sel[i] = j;
     }

@@ -75,11 +75,13 @@ __global__ __launch_bounds__(kPoolThreads) void pages_reserve(PoolArgs a) {
     const int b = b0 + t;
     int slot = b < a.n ? a.slot_ids[b] : -1;
     if (slot < 0 || slot >= a.n_slots) slot = -1;
-    const int r = slot >= 0 ? a.rows[slot] : -1, h = slot >= 0 ? clamp_int(a.held[slot], 0, a.max_pages) : 0;
+    const int r = slot >= 0 ? a.rows[slot] : -1;
     const int add = b < a.n ? (a.lengths ? a.lengths[b] : a.len) : 0;
     const int64_t want = ((int64_t)(r < 0 ? 0 : r) + (add < 0 ? 0 : add) + (1 << a.page_shift) - 1) >> a.page_shift;
-    const int64_t lack = slot >= 0 && r >= 0 && want > h ? want - h : 0;
-    const bool fits = want <= a.max_pages;
+    const bool fits = want <= a.max_pages, live = slot >= 0 && r >= 0;
+    // (claimed at once, so that a slot named twice lacks its pages once)
+    const int was = !live ? 0 : (fits ? atomicMax(&a.held[slot], (int)want) : a.held[slot]), h = clamp_int(was, 0, a.max_pages);
+    const int64_t lack = live && want > h ? want - h : 0;
     int64_t total;
     const int64_t upto = before + group_scan<kPoolWaves>(fits ? (int)lack : 0, red, total);
     const bool served = fits && (lack == 0 || upto <= free0);
@@ -90,7 +92,7 @@ __global__ __launch_bounds__(kPoolThreads) void pages_reserve(PoolArgs a) {
     first[t] = rank;
     to[t] = h - rank;
     slots[t] = slot;
-    if (take) a.held[slot] = h + take;
+    if (lack && fits && !served) a.held[slot] = h;
     __syncthreads();
     for (int e0 = t; e0 < (int)chunk; e0 += kAtOnce * kPoolThreads) {
       int page[kAtOnce], s[kAtOnce];
@@ -123,11 +125,12 @@ __global__ __launch_bounds__(kPoolThreads) void pages_release(PoolArgs a) {
     if (slot < 0 || slot >= a.n_slots) slot = -1;
     int keep = 0, give = 0;
     if (slot >= 0) {
-      const int r = a.rows[slot], h = clamp_int(a.held[slot], 0, a.max_pages);
-      const int64_t k = ((int64_t)(r < 0 ? 0 : r) + (1 << a.page_shift) - 1) >> a.page_shift;
-      keep = k < h ? (int)k : h;
+      const int r = a.rows[slot];
+      const int k = (int)(((int64_t)(r < 0 ? 0 : r) + (1 << a.page_shift) - 1) >> a.page_shift);
+      // (claimed at once, so that a slot named twice gives its pages once)
+      const int h = clamp_int(atomicMin(&a.held[slot], k), 0, a.max_pages);
+      keep = min(k, h);
       give = h - keep;
-      a.held[slot] = keep;
     }
     int64_t all, chunk;
     // more than there are pages would be entries that were handed back twice: left out

@@ -284,6 +284,27 @@ def test_selection_of_equal_and_odd_scores(what):
         check_out(c, [0], [n - 1], q.cuda(), out, c.max_pages * c.page, True, sel)
 
 
+@pytest.mark.parametrize("kv", ["i8", "bf16"])
+def test_counters_far_past_the_cache(kv):
+    """A slot whose counter is the largest number, beside a sound one: its whole blocks below the bound, nothing stored."""
+    print(f"\n[case] block step {kv}: counters past the cache", flush=True)
+    p = params(4, 2, 64, kv, sink=40, recent=1 << 23, topk=100)
+    c = Blocks(p, kv, 32, 64, [256, 256], 9, max_pages=4)
+    before = c.state()
+    _load(c, [0, 1], [256, 100], 2)
+    c.rows[0] = 2 ** 31 - 1
+    g = torch.Generator().manual_seed(5)
+    q, new = _rand(g, 2, 4, 64).cuda(), [_rand(g, 2, 2, 1, 64).cuda() for _ in range(2)]
+    for n in (0, 1):
+        c.put(1, *(x[1].cpu().transpose(0, 1) for x in new)) if n else None
+        for select, recent in ((False, 1), (True, 1 << 23), (True, 5)):
+            p.recent = recent
+            out, sel = _call(c, [0, 1], q, select=select, new=new if not n else None, dtype=torch.float32)
+            if n:
+                check_out(c, [0, 1], [2 ** 31 - 1, 100], q, out, 256, select, sel)
+    c.check(before)
+
+
 def test_selection_among_the_most_blocks():
     """32768 blocks of one sequence; more are refused."""
     print("\n[case] block select among 32768 blocks", flush=True)

@@ -151,6 +151,25 @@ def test_requests_that_cannot_be_served():
     pool.check()
 
 
+def test_a_slot_named_twice():
+    """Its pages are handed out and taken back once."""
+    print("\n[case] pages: a slot named twice", flush=True)
+    pool = Pool(5, 20, 16, 8)
+    slots = [1, 3, 1, 4, 3]
+    snap.snap_pages_reserve(pool.c, _i32([0] * 5), _i32(slots), _i32([50, 30, 20, 10, 64]))
+    torch.cuda.synchronize()
+    held, table = pool.t["held"].cpu().tolist(), pool.t["table"].cpu()
+    assert held == [0, 4, 0, 4, 1] and int(pool.t["n"]) == 20 - 9
+    used = [int(table[s, j]) for s in (1, 3, 4) for j in range(held[s])]
+    left = pool.t["free"][:11].cpu().tolist()
+    assert sorted(used + left) == list(range(20)) and int((table >= 0).sum()) == 9
+    snap.snap_pages_release(pool.c, _i32([0, 17, 0, 0, 16]), _i32([1, 3, 3, 1, 1]))
+    torch.cuda.synchronize()
+    assert pool.t["held"].cpu().tolist() == [0, 2, 0, 0, 1] and int(pool.t["n"]) == 17
+    table = pool.t["table"].cpu()
+    assert sorted(pool.t["free"][:17].cpu().tolist() + table[table >= 0].tolist()) == list(range(20))
+
+
 @pytest.mark.parametrize("n,tokens", [(1, 1), (1, 0), (3, 5), (300, 5000), (2, 4096), (600, 1), (5, 100000)])
 def test_maps(n, tokens):
     print(f"\n[case] map of {n} sequences, room for {tokens} tokens", flush=True)
