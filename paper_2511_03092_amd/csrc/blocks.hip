@@ -480,15 +480,17 @@ struct BlockAppend {
   int tokens, max_len;
 };
 
-// Wave w of workgroup x takes block 2 x + w / 2 of the sequence's new ones, keys (w even)
-// or values.  The wave of the first block, which may read the tail's old rows, writes the
-// last one's afterwards, so that no other wave's writes meet those reads.
+// Even waves take keys, odd ones values.  Workgroup 0: the sequence's first new block, and
+// (8 bits, where that is not the last one) the last block's rows into the tail, stored
+// after the barrier, behind which nobody reads the tail's old rows any more; workgroup x:
+// blocks 2 x - 1 and 2 x.  HBM bound: four prompts of 32k tokens or fewer out of the packed
+// projection into int8 (465 MB) 103 us, 4.5 TB/s (a copy: 4.7 to 4.9).
 template <int D, int KIND, int B>
 __global__ __launch_bounds__(256) void block_append(BlockAppend p) {
   const BlockArgs& a = p.c;
   constexpr int P = D / 8, R = 64 / P;
   const int w = uniform(tid() >> 6), lane = tid() & 63, col = lane % P, r0 = lane / P;
-  const int g = bid_y(), b = __builtin_amdgcn_workgroup_id_z(), j = 2 * bid_x() + (w >> 1);
+  const int g = bid_y(), b = __builtin_amdgcn_workgroup_id_z(), j = bid_x() ? 2 * bid_x() - 1 + (w >> 1) : 0;
   const bool keys = !(w & 1);
   // (loads that do not wait for one another go out together)
   int slot = a.slot_ids[b];
@@ -512,28 +514,32 @@ __global__ __launch_bounds__(256) void block_append(BlockAppend p) {
   const int64_t* st = keys ? p.ks : p.vs;
   const unsigned char* in = (const unsigned char*)(keys ? a.k_new : a.v_new) + (p.starts ? 0 : b * st[0]) + g * st[1];
   unsigned char* tail = KIND == kRowsBf16 ? nullptr : (keys ? a.kt : a.vt) + ((((size_t)slot * a.Hkv + g) << a.block_shift) * D) * 2;
-  // rows [from, upto) of block i come from the input
-  auto block = [&](int i) {
-    const int at = block_at(a, slot, g, first + i);
-    const int from = i ? 0 : skip, upto = min(B, skip + len - i * B);
-    unsigned char* old = KIND == kRowsBf16 ? (keys ? a.ck : a.cv) + ((size_t)max(at, 0) << a.block_shift) * D * 2 : tail;
-    auto row = [&](int r) -> const unsigned char* {
-      return r < from ? old + (size_t)r * D * 2 : in + (t0 + (int64_t)i * B + r - skip) * st[2];
-    };
-    if (upto == B && i == j) put_block_at_once<D, KIND, B>(a, at, keys, row);
-    if (uniform(at) >= 0 && (KIND == kRowsBf16 || i == last))
-      for (int r = r0; r < upto; r += R)
-        if (r >= from) *((u32x4*)(old + (size_t)r * D * 2) + col) = *((const u32x4*)row(r) + col);
+  auto given = [&](int i, int r) { return in + (t0 + (int64_t)i * B + r - skip) * st[2]; };
+  // rows [from, upto) of block i, which come from the input, to their places behind `to`
+  auto copy = [&](int i, unsigned char* to, int from, int upto, bool wait) {
+    constexpr int NP = B / R;
+    u32x4 x[NP];
+#pragma unroll
+    for (int q = 0; q < NP; ++q)
+      if (q * R + r0 >= from && q * R + r0 < upto) x[q] = *((const u32x4*)given(i, q * R + r0) + col);
+    if (wait) __syncthreads();
+#pragma unroll
+    for (int q = 0; q < NP; ++q)
+      if (q * R + r0 >= from && q * R + r0 < upto) *((u32x4*)(to + (size_t)(q * R + r0) * D * 2) + col) = x[q];
   };
-  if (KIND == kRowsBf16) {
-    block(j);
-  } else {
-    if (j != last || j == 0) block(j);
-    else if (skip + len == (last + 1) * B) {  // a whole last block: its codes here, its tail rows by the first block's wave
-      put_block_at_once<D, KIND, B>(a, block_at(a, slot, g, first + j), keys,
-                                    [&](int r) { return in + (t0 + (int64_t)j * B + r - skip) * st[2]; });
-    }
-    if (j == 0 && last > 0) block(last);
+  const int upto = min(B, skip + len - j * B), from = j ? 0 : skip;
+  const int at = block_at(a, slot, g, first + (bid_x() == 0 && w >= 2 ? last : j));
+  if (bid_x() == 0 && w >= 2) {
+    if (KIND != kRowsBf16 && last > 0) copy(last, tail, 0, uniform(at) < 0 ? 0 : skip + len - last * B, true);
+    return;
+  }
+  unsigned char* old = KIND == kRowsBf16 ? (keys ? a.ck : a.cv) + ((size_t)max(at, 0) << a.block_shift) * D * 2 : tail;
+  if (upto == B)
+    put_block_at_once<D, KIND, B>(a, at, keys, [&](int r) -> const unsigned char* { return r < from ? old + (size_t)r * D * 2 : given(j, r); });
+  if (KIND == kRowsBf16 || last == 0) {
+    if (uniform(at) >= 0) copy(j, old, from, upto, false);
+  } else if (bid_x() == 0) {
+    __syncthreads();
   }
 }
 
@@ -947,6 +953,25 @@ struct Soft {
 #pragma unroll
     for (int i = 0; i < 8; ++i) pe[i] *= vs;
   }
+  // their sum over the rows' values, int8 codes: made bf16 in the operand's order
+  template <typename Raw>
+  __device__ __forceinline__ void values8(float (&pe)[8], const Raw (&v)[8]) {
+    bf16x8 p[3];
+    three_terms(pe, p);
+#pragma unroll
+    for (int c = 0; c < VE; ++c) {
+      u32x4 av;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = (float)(int)(int8_t)(v[2 * i][c >> 2] >> (8 * (c & 3)));
+        const float y = (float)(int)(int8_t)(v[2 * i + 1][c >> 2] >> (8 * (c & 3)));
+        av[i] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+      }
+#pragma unroll
+      for (int part = 2; part >= 0; --part)
+        acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, av), p[part], acc[c], 0, 0, 0);
+    }
+  }
   // their sum over the rows' values (two bf16 a word)
   __device__ __forceinline__ void values(float (&pe)[8], const uint32_t (&vw)[8][VE / 2]) {
     bf16x8 p[3];
@@ -1147,22 +1172,26 @@ __device__ __forceinline__ void attend_blocks(const BlockArgs& a, int b, int g, 
     const float x[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
     float pe[8];
     o.softmax(x, xs, xlo, vs, pe);
-    uint32_t vw[8][VE / 2];
+    if constexpr (KIND == kRowsInt8) {
+      o.values8(pe, v);
+    } else {
+      uint32_t vw[8][VE / 2];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if constexpr (KIND == kRowsBf16) {
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (KIND == kRowsBf16) {
 #pragma unroll
-        for (int u = 0; u < VE / 2; ++u) vw[i][u] = v[i][u];
-      } else {
+          for (int u = 0; u < VE / 2; ++u) vw[i][u] = v[i][u];
+        } else {
 #pragma unroll
-        for (int u = 0; u < VE / 4; ++u) {
-          const u32x2 w = bf16x4<KIND>(v[i][u]);
-          vw[i][2 * u] = w[0];
-          vw[i][2 * u + 1] = w[1];
+          for (int u = 0; u < VE / 4; ++u) {
+            const u32x2 w = bf16x4<KIND>(v[i][u]);
+            vw[i][2 * u] = w[0];
+            vw[i][2 * u + 1] = w[1];
+          }
         }
       }
+      o.values(pe, vw);
     }
-    o.values(pe, vw);
 #pragma unroll
     for (int j = 0; j < NK; ++j) {
       k0[j] = n0[j];
@@ -1496,7 +1525,7 @@ snap_status launch_block_append(const snap_params& p, const snap_block_cache& c,
       {SNAP_BLOCK_APPEND(64, kRowsBf16), SNAP_BLOCK_APPEND(64, kRowsFp8), SNAP_BLOCK_APPEND(64, kRowsInt8)},
       {SNAP_BLOCK_APPEND(128, kRowsBf16), SNAP_BLOCK_APPEND(128, kRowsFp8), SNAP_BLOCK_APPEND(128, kRowsInt8)}};
 #undef SNAP_BLOCK_APPEND
-  hipLaunchKernelGGL(kernels[p.d_qk == 128][kind_of(p.kv_dtype)][a.c.block_shift - 5], dim3((blocks + 1) / 2, p.n_kv_heads, n),
+  hipLaunchKernelGGL(kernels[p.d_qk == 128][kind_of(p.kv_dtype)][a.c.block_shift - 5], dim3(1 + blocks / 2, p.n_kv_heads, n),
                      dim3(256), 0, stream, a);
   return hipGetLastError() == hipSuccess ? SNAP_OK : SNAP_ERR_HIP;
 }
