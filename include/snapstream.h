@@ -534,7 +534,7 @@ typedef struct {
  * Sequences with a slot id out of range or rows[slot] < 0 are skipped (short 0).
  * The slots must be distinct (a slot named twice gets the pages of the longer wish
  * once, but short_out then tells of one of the two).  One workgroup: a call is a few
- * microseconds. */
+ * microseconds, 20 where it hands out 48000 pages. */
 snap_status snap_pages_reserve(const snap_page_pool* pool, const int32_t* rows, int32_t n, const int32_t* slot_ids,
                                const int32_t* lengths, int32_t len, int32_t* short_out, void* stream);
 

@@ -627,7 +627,7 @@ __device__ __forceinline__ void limits(const BlockArgs& a, int held, BlockChoice
 // the wave's first blocks.
 template <int D, int W>
 struct BlockScores {
-  static constexpr int NK = 2 * D / 64, N = D == 128 ? 4 : 8, kStep = 16 * W, Q = 16 / W;
+  static constexpr int NK = 2 * D / 64, N = (D == 128 ? 2 : 4) * (W == kSelWaves ? 1 : 2), kStep = 16 * W, Q = 16 / W;
   static constexpr int kBatch = kStep * N;  // blocks in flight
   static constexpr int P = 2 * D / 16;  // 16-byte pieces of a block's bounds
   struct Shared {
@@ -774,6 +774,11 @@ __global__ __launch_bounds__(kSelThreadsB) void block_select(BlockArgs a) {
   hist[0][t] = 0;
   limits(a, held, c);
   const int nb = c.nb, f0 = c.f0, f1 = c.f1;
+  // in flight with the bounds: the pages of the thread's forced block and of the first one
+  // that it may write (wave w writes its share of the blocks, in order)
+  const int share = ((nb + kSelWaves - 1) / kSelWaves + 63) & ~63, a0 = min(nb, w * share), a1 = min(nb, a0 + share);
+  auto forced = [&](int i) { return i < f0 ? i : f1 + i - f0; };
+  const int forced_page = c.page(a, forced(t)), own_page = c.page(a, a0 + lane);
   int32_t* list = a.list + (size_t)unit * a.list_ld;
   int32_t* sel = a.sel_out ? a.sel_out + (size_t)unit * a.chosen : nullptr;
   uint32_t T = 0;  // taken: above T, and the first `rem` of T
@@ -796,8 +801,8 @@ __global__ __launch_bounds__(kSelThreadsB) void block_select(BlockArgs a) {
     s.run(a, c, f0, f1, sh, keep);
   }
   for (int i = t; i < f0 + nb - f1; i += kSelThreadsB) {
-    const int j = i < f0 ? i : f1 + i - f0;
-    key[j] = c.there(a, j) ? kForced : 0u;
+    const int j = forced(i);
+    key[j] = c.place(a, j, i == t ? forced_page : c.page(a, j)) >= 0 ? kForced : 0u;
   }
   if (c.scored) {
     least = ~wave_max(~least);
@@ -845,8 +850,6 @@ __global__ __launch_bounds__(kSelThreadsB) void block_select(BlockArgs a) {
       __syncthreads();  // (out is read before it is written again)
     }
   }
-  // in order; wave w writes its share of the blocks
-  const int share = ((nb + kSelWaves - 1) / kSelWaves + 63) & ~63, a0 = min(nb, w * share), a1 = min(nb, a0 + share);
   int above = 0, equal = 0;
   for (int j = a0 + lane; j - lane < a1; j += 64) {
     const uint32_t k = j < a1 ? key[j] : 0u;
@@ -876,7 +879,7 @@ __global__ __launch_bounds__(kSelThreadsB) void block_select(BlockArgs a) {
     const int e = equal0 + __builtin_popcountll(em & below), i = above0 + __builtin_popcountll(am & below) + min(e, rem);
     const bool take = k > T || (k != 0 && k == T && e < rem);
     if (take && debug_check(i < a.list_ld, kDbgBlockList) && i < a.list_ld) {
-      list[i] = c.place(a, j, c.page(a, j));
+      list[i] = c.place(a, j, j == a0 + lane ? own_page : c.page(a, j));
       if (sel) sel[i] = j;
     }
     above0 += __builtin_popcountll(am);
