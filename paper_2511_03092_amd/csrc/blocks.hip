@@ -1448,7 +1448,12 @@ BlockGeometry block_geometry(const snap_params& p, int n, int max_rows, int bloc
   (PagedCut&)g = paged_cut(units, kResident, (int64_t)units * most);
   size_t items = (size_t)units * (block / 32) + g.max_items;
   if (select) {  // the same items for every unit
-    int each = kResident / units;
+    // Of 128-wide rows, which keep more bytes in flight a wave, half the card's waves are
+    // enough, with half the partials to join.  All / half of them, 8 KV heads, us a call:
+    // 128 int8 16 x 4096 rows 55.9/54.2, 8 x 4096 36.9/35.2, 4 x 30000 66.0/62.8, 32 x 4096
+    // 78.0/78.9, bf16 16 x 4096 65.2/63.1, E4M3 16 x 2000 40.6/39.8; 64 E4M3 64 x 7500
+    // 122/149.
+    int each = (p.d_qk == 128 ? kResident / 2 : kResident) / units;
     each = each < 1 ? 1 : (each > g.list_ld ? g.list_ld : each);
     g.max_items = units * each;
     // (a bound that does not fall as sequences or rows grow, and serves calls without)
