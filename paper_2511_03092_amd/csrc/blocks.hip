@@ -752,7 +752,7 @@ __global__ __launch_bounds__(kScoreThreads) void block_score(BlockArgs a) {
 }
 
 // One workgroup a unit, bound by dependent steps: 8 units of 512 blocks 11.5 us (queries,
-// pages and bounds 5.5, the histograms 1.5, the list 1), 128 units of 2048 blocks 25 us, then
+// pages and bounds 5.5, the histograms 1.5, the list 1), 128 units of 2048 blocks 23 us, then
 // mostly the bounds' 67 MB by 128 of 256 CUs.  The keys are in LDS.  The last score taken is found by a
 // histogram over the range that the scores span, then over the bin that holds it, and so
 // on until a bin is taken whole or is one score: two rounds, mostly.  GIVEN: the keys are
@@ -1474,19 +1474,20 @@ BlockGeometry block_geometry(const snap_params& p, int n, int max_rows, int bloc
 }
 
 // Whether a unit's blocks are scored by a launch of their own, kBatch of them a workgroup,
-// or by the one workgroup that chooses among them.  That one takes in about 40 bytes a
-// nanosecond; the launch costs 3 to 4 us.  Whole calls, 8 KV heads, one launch / two, us:
-//   bounds a unit           128 KB      256 KB      512 KB      1 MB        2 MB
-//   d 128     1 sequence   21.4/23.9   23.4/23.0   27.7/23.9   36.9/25.4   57/28.5
-//             4            23.5/26.2   28.8/27.9   34.1/29.7   44.8/33.6   69/41.5
-//            16            38.1/40.6   38.0/39.0   45.3/45.9   61.9/56.2  115/91
-//            32            56.4/59.7   54.3/56.2   67.9/67.3  100/91
-//   d 64      1            19.4/21.7   24.3/22.5   31.3/23.7   45.0/26.0
-//            16            27.6/31.2   34.4/34.8   45.1/44.6   70.4/58.4
-// (It also keeps the keys of the one that scores, beside 78 KB of its own, within LDS.)
+// or by the one workgroup that chooses among them.  That one takes in 30 to 50 bytes a
+// nanosecond; the launch costs 3 to 5 us.  Whole calls, 8 KV heads, one launch / two, us:
+//   bounds a unit           128 KB      256 KB      512 KB      1 MB
+//   d 128     1 sequence   18.7/20.9   21.8/21.8   26.8/22.9   36.4/24.2
+//             4            21.2/23.5   24.4/24.6   30.5/25.9   41.7/31.5
+//            16            29.4/31.4   33.5/36.1   40.3/48.4   57.2/60.7
+//            32            43.6/47.3   49.4/60.8   63.9/72.9   95.4/97.7
+//   d 64      1            19.8/23.2   24.0/23.9   30.4/25.4
+//             4            22.2/25.2   26.1/27.2   34.5/28.6
+//            16            27.0/30.5   31.8/34.8   42.3/42.8
+//            32            33.5/37.1   41.4/44.8   61.4/58.4
+// (Past 8192 blocks the one that scores would not have its keys in LDS.)
 static bool scored_apart(const snap_params& p, int units, int blocks) {
-  const size_t bytes = (size_t)blocks * 2 * p.d_qk;
-  return units <= 64 ? bytes >= (size_t)256 << 10 : bytes > (size_t)512 << 10;
+  return units <= 64 ? (size_t)blocks * 2 * p.d_qk >= (size_t)512 << 10 : blocks > 4096;
 }
 
 // Whether a workgroup of eight waves takes a whole unit, so that one launch does: with
@@ -1495,18 +1496,18 @@ static bool scored_apart(const snap_params& p, int units, int blocks) {
 // (then nothing is written for the join).  Measured, one launch / two, 32 query heads on 8,
 // us of a replayed call:
 //   rows                250         500        1000        2000        3900
-//   128 int8   1 x   8.9/9.7   10.7/9.8   14.4/9.8   21.6/10.3   35.5/11.4
-//             16     9.0/10.6  10.8/11.8  15.3/15.1  22.7/21.1   37.0/29.7
-//             32     9.0/12.6  11.7/15.9  17.9/21.8  27.3/31.2   45.6/52.6
-//             64    18.2/18.5  24.5/25.7  34.1/37.2  52.6/62.4   104/101
-//   128 bf16   1     8.7/9.0   10.8/9.1   16.2/9.2   24.1/9.7    40.6/11.0
-//             16     8.7/10.3  11.3/12.6  17.8/19.0  26.4/28.4   44.3/48.1
-//             32     9.5/13.2  15.7/19.4  25.0/30.0  43.2/50.7   91.8/90.9
-//             64    21.2/20.8  29.4/32.0  48.2/54.4  98.3/93.6   182/167
-//   64 int8    1     6.5/8.2    7.8/8.3   10.2/8.3   15.1/8.7    24.5/10.9
-//             16     6.5/9.3    7.9/10.4  10.3/12.1  16.0/15.1   26.0/19.9
-//             32     6.6/11.1   8.0/13.0  11.1/15.7  17.0/20.6   26.7/29.4
-//             64     8.2/14.8  11.2/17.4  18.2/22.4  27.9/31.6   45.7/53.4
+//   128 int8   1 x   8.7/9.7   10.4/9.7   14.0/9.8   20.7/10.2   33.6/11.3
+//             16     8.8/10.6  10.5/11.6  14.8/14.8  21.7/20.8   35.0/30.0
+//             32     8.8/12.5  11.3/15.7  17.5/22.0  26.7/31.1   46.0/52.7
+//             64    17.8/18.2  23.9/23.9  33.4/33.5  52.1/56.7   103/92.5
+//   128 bf16   1     8.8/9.1   10.9/9.2   16.3/9.2   24.2/9.7    40.8/11.0
+//             16     8.7/10.2  11.3/12.8  17.8/19.0  26.5/28.4   44.5/48.3
+//             32     9.6/13.2  15.9/19.5  25.2/29.5  43.2/50.6   92.4/90.3
+//             64    21.1/20.8  29.8/32.1  48.4/54.1  99.0/93.0   181/166
+//   64 int8    1     6.4/8.2    7.7/8.2    9.9/8.4   14.6/8.8    23.5/10.8
+//             16     6.5/9.4    7.8/10.4  10.0/12.4  15.5/15.0   24.8/19.6
+//             32     6.6/10.9   7.9/13.0  10.8/15.5  16.6/20.4   25.9/28.6
+//             64     8.3/14.5  11.0/17.2  17.9/22.0  27.5/31.1   45.5/52.4
 // (calls that are not replayed cost the host 9 us with one launch, 11 with two)
 static bool whole_units(const snap_params& p, int units, int blocks, int block) {
   const int row_bytes = 2 * p.d_qk * (p.kv_dtype == SNAP_BF16 ? 2 : 1);

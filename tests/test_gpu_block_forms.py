@@ -63,7 +63,7 @@ def test_many_sequences(kv, d, block, n, longest):
 def test_selection_scored_apart(kv, d, block, hq):
     """So many blocks that they are scored by a launch of their own; holes, a short and an empty sequence beside."""
     print(f"\n[case] select, scored apart: {kv} d {d} block {block}", flush=True)
-    rows = 33000 if d == 128 else 66000
+    rows = 66000 if d == 128 else 132000  # 512 KB of bounds a unit
     p = params(hq, 2, d, kv, sink=70, recent=300, topk=1000)
     c = Blocks(p, kv, block, 256, [rows, 1, 700, rows - 5], 4, holes=[(0, 3), (0, 60), (3, 0)])
     _load(c, [0, 1, 2, 3], [rows, 0, 700, rows - 5], 5)
