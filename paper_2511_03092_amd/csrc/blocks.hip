@@ -2,12 +2,14 @@
 // a scale for each block and KV head, or in bf16, and attention of one new token over
 // all of them or over those that a score selects.
 //
-//   block_append  a wave for each block of new keys or values
-//   block_select  one workgroup for each (sequence, KV head): the blocks' scores from
-//                 their bounds, and the best of them
-//   block_attn    one wave for each work item: a share of a unit's blocks, or the
-//                 newest token's own block (with the token stored)
-//   block_join    the items of a (sequence, query head) -> out
+//   block_append     a wave for each block of new keys or values
+//   block_select     one workgroup for each (sequence, KV head), a unit: the blocks' scores
+//                    from their bounds, and the best of them
+//   block_score      the scores alone, where a unit's blocks are many
+//   block_attn       one wave for each work item: a share of a unit's blocks, 32 rows of
+//                    the newest token's own block, or that token stored
+//   block_join       the items of a (sequence, query head) -> out
+//   block_attn_unit  both for short calls, a workgroup a unit
 #include <math.h>
 
 #include "lds_dma.h"
@@ -21,7 +23,6 @@ enum { kRowsBf16 = 0, kRowsFp8 = 1, kRowsInt8 = 2 };
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef short i16x2 __attribute__((ext_vector_type(2)));
-typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
 struct BlockArgs {
   const void* q;  // [n][Hq][d]
@@ -755,7 +756,7 @@ __global__ __launch_bounds__(kScoreThreads) void block_score(BlockArgs a) {
 // pages and bounds 5.5, the histograms 1.5, the list 1), 128 units of 2048 blocks 23 us, then
 // mostly the bounds' 67 MB by 128 of 256 CUs.  The keys are in LDS.  The last score taken is found by a
 // histogram over the range that the scores span, then over the bin that holds it, and so
-// on until a bin is taken whole or is one score: two rounds, mostly.  GIVEN: the keys are
+// on until a bin is taken whole or is one score: two turns, mostly.  GIVEN: the keys are
 // block_score's.
 template <int D, bool GIVEN>
 __global__ __launch_bounds__(kSelThreadsB) void block_select(BlockArgs a) {

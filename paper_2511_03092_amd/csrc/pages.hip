@@ -8,7 +8,8 @@
 //                   prefix sums of the lengths
 //
 // All are bound by latency: a handful of dependent loads, no more than 12 bytes a
-// token written.
+// token written.  One token each of 64 sequences 3 us a call; 24 prompts of up to 32k
+// tokens (6200 pages of 64) 6.5 us, and about 20 for 48000 pages, by what one CU stores.
 #include "snap_internal.h"
 
 namespace snap {

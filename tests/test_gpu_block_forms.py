@@ -73,6 +73,19 @@ def test_selection_scored_apart(kv, d, block, hq):
     check_out(c, [3, 1, 2, 0], [rows - 6, -1, 699, rows - 1], q, out, rows, True, sel)
 
 
+def test_selections_of_many_short_sequences_in_a_long_table():
+    """Keys of 4096 blocks beside the scoring, few of them there; lists as long as the longest selection."""
+    print("\n[case] select, 80 units, a bound of 131072 rows", flush=True)
+    p = params(4, 2, 64, "i8", sink=4, recent=64, topk=640)
+    lengths = [5000, 0, 1] + [40 * b for b in range(3, 40)]
+    c = Blocks(p, "i8", 32, 64, [max(1, n) for n in lengths], 5, max_pages=2048)
+    _load(c, list(range(40)), lengths, 6)
+    c.rows -= 1
+    q = _rand(torch.Generator().manual_seed(7), 40, 4, 64).cuda()
+    out, sel = _call(c, list(range(40)), q, max_rows=131072, select=True)
+    check_out(c, list(range(40)), [n - 1 for n in lengths], q, out, 131072, True, sel)
+
+
 def test_slots_that_share_whole_pages():
     """Two slots whose first pages are one slot's: both attend them, and grow into pages of their own."""
     print("\n[case] block cache: shared pages", flush=True)
