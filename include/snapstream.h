@@ -609,9 +609,9 @@ typedef struct {
  *     sizes of more than 1; NULL: contiguous);
  *   starts [n + 1] (device int32, as snap_pages_map's): a packed batch of `tokens`
  *     tokens, k_new [tokens][n_kv_heads][d]; sequence b has tokens starts[b] ..
- *     starts[b + 1] - 1 (at most max_len of them; starts outside [0, tokens] are
- *     clamped); lengths is then NULL, and of the strides the sequence's is not read
- *     (NULL: contiguous).
+ *     starts[b + 1] - 1 (at most max_len of them, a bound that sizes the launch: a
+ *     near one spares workgroups; starts outside [0, tokens] are clamped); lengths
+ *     is then NULL, and of the strides the sequence's is not read (NULL: contiguous).
  * Sequences with rows[slot] < 0 and rows past the page table are skipped.  rows is
  * left as it is.  The slots must be distinct. */
 snap_status snap_block_append(const snap_params* p, const snap_block_cache* cache, const int32_t* rows, int32_t n,

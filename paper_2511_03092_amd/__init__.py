@@ -704,7 +704,8 @@ def block_cache_struct(k, v, page_table, block: int, k_scale=None, v_scale=None,
 def snap_block_append(p: Params, cache: SnapBlockCache, rows, slot_ids, k_new, v_new, lengths=None, starts=None,
                       max_len=None, stream=None):
     """Stores k_new and v_new (any strides but the last) behind the rows held: [n, n_kv_heads, tokens, d], or with starts
-    [n + 1] a packed batch [tokens, n_kv_heads, d] whose sequences have at most max_len tokens (default: all of them)."""
+    [n + 1] a packed batch [tokens, n_kv_heads, d] whose sequences have at most max_len tokens (default: all of them; it
+    sizes the launch, so a near bound is faster where there are many sequences)."""
     (n, cp), index, heads = _paged(p, cache, rows, None, slot_ids), cache.index, p.n_kv_heads
     dims = 4 if starts is None else 3
     if k_new is None or v_new is None or k_new.dim() != dims:

@@ -86,6 +86,36 @@ def test_selections_of_many_short_sequences_in_a_long_table():
     check_out(c, list(range(40)), [n - 1 for n in lengths], q, out, 131072, True, sel)
 
 
+@pytest.mark.parametrize("kv", ["i8", "bf16"])
+def test_a_packed_batch_of_many_short_sequences_and_a_long_one(kv):
+    """No bound on the lengths."""
+    print(f"\n[case] packed append {kv}: 70 sequences, one long", flush=True)
+    p = params(2, 2, 64, kv)
+    lengths = [(7 * b) % 50 for b in range(70)]
+    lengths[33] = 4001
+    held = [(11 * b) % 40 for b in range(70)]
+    c = Blocks(p, kv, 32, 64, [n + m + 1 for n, m in zip(lengths, held)], 5)
+    before = c.state()
+    _load(c, list(range(70)), held, 6)
+    g = torch.Generator().manual_seed(8)
+    x = _rand(g, sum(lengths), 4, 64)
+    starts = [0]
+    for n in lengths:
+        starts.append(starts[-1] + n)
+    slots = torch.randperm(70, generator=g).tolist()
+    dev = x.cuda()
+    order = torch.cat([torch.arange(starts[s], starts[s + 1]) for s in slots])
+    at = [0]
+    for s in slots:
+        at.append(at[-1] + lengths[s])
+    y = dev[order.cuda()]
+    snap.snap_block_append(p, c.c, c.rows, _i32(slots), y[:, :2], y[:, 2:], starts=_i32(at))
+    torch.cuda.synchronize()
+    for s in range(70):
+        c.put(s, x[starts[s]:starts[s + 1], :2], x[starts[s]:starts[s + 1], 2:])
+    c.check(before)
+
+
 def test_slots_that_share_whole_pages():
     """Two slots whose first pages are one slot's: both attend them, and grow into pages of their own."""
     print("\n[case] block cache: shared pages", flush=True)
