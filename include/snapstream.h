@@ -633,6 +633,9 @@ size_t snap_block_decode_workspace(const snap_params* p, int32_t n, int32_t max_
  * over the rows [0, r] of its slot (select = 0): out[b][h] = sum_j softmax_j(sm_scale
  * q.k_j) v_j, zero for a sequence without rows; blocks before the new token's by
  * their codes, its own by its rows as they came.
+ * Values of every size carry the errors of fp32 sums.  Rows whose share of the
+ * softmax is below 2^-120 may count as none; an infinite value makes its dim of out
+ * infinite, or NaN beside one of the other sign or where its share is below 2^-90.
  * select = 1: over the new token's block and, of the blocks before it,
  *   those with one of the first `sink` rows or of the last `recent` ones, and
  *   the ceil(topk / block) others of the largest score (equal scores: the lower

@@ -37,7 +37,7 @@ struct BlockArgs {
   const int32_t* rows;
   const int32_t* slot_ids;
   const int32_t* table;
-  float* part;     // [items][G][d]
+  float* part;     // [items][G][d]  means of the items' values
   float2* ml;      // [items][G]  (max in log2 units, sum)
   int32_t* list;   // [units][list_ld] places of the selected blocks, ascending by block, then -1; NULL: all
   int32_t* sel_out;
@@ -893,20 +893,23 @@ __global__ __launch_bounds__(kSelThreadsB) void block_select(BlockArgs a) {
 
 // ---------------------------------------------------------------- attention
 constexpr float kStaleMax = 8.f;
-// Sums of values are in units of 2^40: a probability is up to 2^8 beside a reference that
-// lags, and 2^28 rows of them times a value of 2^127 are then finite, as the mean is.  What
-// that flushes is below 2^-86 of a unit value.
-constexpr float kDown = 0x1p-40f, kUp = 0x1p40f;
 
-// Eight probabilities as three bf16 terms, whose sum they are (pe is used up).
+// Eight weights as three bf16 terms, whose sum they are (pe is used up).  INF, for values
+// that may be infinite: the second and third are kept off zero, so that an infinite value
+// times them stays infinite, by 2^-32 of the weight itself (a floor that is the same for
+// every weight would give large finite values a share that they do not have).
+template <bool INF>
 __device__ __forceinline__ void three_terms(float (&pe)[8], bf16x8 (&p)[3]) {
+  float least[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) least[i] = INF ? pe[i] * 0x1p-32f : 0.f;
 #pragma unroll
   for (int part = 0; part < 3; ++part) {
     u32x4 pw;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float lo = part ? fmaxf(pe[2 * i], 0x1p-126f) : pe[2 * i];
-      const float hi = part ? fmaxf(pe[2 * i + 1], 0x1p-126f) : pe[2 * i + 1];
+      const float lo = INF && part ? fmaxf(pe[2 * i], least[2 * i]) : pe[2 * i];
+      const float hi = INF && part ? fmaxf(pe[2 * i + 1], least[2 * i + 1]) : pe[2 * i + 1];
       pe[2 * i] -= __uint_as_float(__float_as_uint(pe[2 * i]) & 0xffff0000u);
       pe[2 * i + 1] -= __uint_as_float(__float_as_uint(pe[2 * i + 1]) & 0xffff0000u);
       pw[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
@@ -929,41 +932,86 @@ __device__ __forceinline__ u32x2 bf16x4(uint32_t c) {
   }
 }
 
+// The softmax of a query head (column l16) and its sum of values.  acc is in units of
+// 2^unit, a power that each column has of its own, so that weights reach the matrix units
+// in the middle of their range and acc stays finite where the mean of the values is:
+//   codes: a weight is probability times scale; the unit is that of the largest product so
+//     far (to within 2^8), whatever the size of the scales, and follows the reference as
+//     that rises.  What is lost is below 2^-126 of the largest product.
+//   rows as they came: a weight is a probability; the unit is at least the sum of them, so
+//     that acc is at most the largest value, and 2^5 or that of the sum (to within 2^4).
+//     What is lost is below 2^-121 of the sum.
+constexpr int kRowsUnit = 5;        // 32 rows of a probability of at most 1
+constexpr float kLeastRise = -110.f;  // so that scale / 2^unit is finite where the probabilities are next to nothing
 template <int D>
 struct Soft {
   static constexpr int VE = D / 16;  // value dims a lane
-  float m = -INFINITY, mref = 0.f, lsum = 0.f;
+  float m = -INFINITY, mref = 0.f, lsum = 0.f, unit = kRowsUnit;
   f32x4 acc[VE];
   __device__ __forceinline__ void init() {
 #pragma unroll
     for (int c = 0; c < VE; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  // products x of eight rows at xs a unit (xlo: its low part) -> probabilities times vs
-  __device__ __forceinline__ void softmax(const float (&x)[8], float xs, float xlo, float vs, float (&pe)[8]) {
+  __device__ __forceinline__ float total() const {  // of lsum, over the lanes of a column
+    const float s = lsum + __shfl_xor(lsum, 16);
+    return s + __shfl_xor(s, 32);
+  }
+  // acc in the unit that rows as they came go by, from whatever it is in.
+  __device__ __forceinline__ void by_total() {
+    const int e = (int)(__float_as_uint(total()) >> 23) - 127;
+    const float now = (float)(max(e, 0) + 4);
+#pragma unroll
+    for (int c = 0; c < VE; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[c][i] = __builtin_ldexpf(acc[c][i], (int)(unit - now));
+    unit = now;
+  }
+  // Products x of eight rows at xs a unit (xlo: its low part) -> weights: probabilities times
+  // scale (CODES), in units of 2^unit.
+  template <bool CODES>
+  __device__ __forceinline__ void softmax(const float (&x)[8], float xs, float xlo, float scale, float (&pe)[8]) {
     float bm = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
     bm = fmaxf(bm, __shfl_xor(bm, 16));
     bm = fmaxf(bm, __shfl_xor(bm, 32));
     bm *= xs;
-    const bool up = bm > m + kStaleMax;
-    if (wave_any(up)) {
-      const float mnew = up ? bm : m, alpha = up ? fast_exp2(m - mnew) : 1.f;
-#pragma unroll
-      for (int c = 0; c < VE; ++c) acc[c] *= alpha;
-      lsum *= alpha;
+    const float es = (float)((int)(__float_as_uint(scale) >> 23) - 127);
+    const bool up = bm > m + kStaleMax, far = CODES && fmaxf(bm - mref, kLeastRise) + es > unit + kStaleMax;
+    if (wave_any(up || far)) {
+      const float mnew = up ? bm : m, rise = up ? mnew - m : 0.f;  // (infinite at the first rows)
       m = mnew;
       mref = m == -INFINITY ? 0.f : m;
+      const float least = CODES ? es + fmaxf(__builtin_ceilf(bm - mref), kLeastRise) : (float)kRowsUnit;
+      const float alpha = fast_exp2(-rise), now = fmaxf(unit - __builtin_floorf(rise), least);
+      const float beta = __builtin_ldexpf(alpha, (int)(unit - now));
+#pragma unroll
+      for (int c = 0; c < VE; ++c) acc[c] *= beta;
+      lsum *= alpha;
+      unit = now;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) pe[i] = fast_exp2(fmaf(x[i], xs, fmaf(x[i], xlo, -mref)));
     lsum += ((pe[0] + pe[1]) + (pe[2] + pe[3])) + ((pe[4] + pe[5]) + (pe[6] + pe[7]));
+    // (a quarter of the unit in each of a column's four lanes)
+    if (!CODES && wave_any(lsum > __builtin_ldexpf(0.25f, (int)unit))) by_total();
+    const float w = __builtin_ldexpf(CODES ? scale : 1.f, -(int)unit);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) pe[i] *= vs;
+    for (int i = 0; i < 8; ++i) pe[i] *= w;
+  }
+  // acc times f, in units of 1.  (CODES: by a middling power of two first, so that what is
+  // between stays in range)
+  template <bool CODES>
+  __device__ __forceinline__ void by(float f) {
+    const float h = CODES ? fminf(fmaxf(unit, -40.f), 40.f) : unit, g = __builtin_ldexpf(f, (int)h);
+#pragma unroll
+    for (int c = 0; c < VE; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[c][i] = CODES ? __builtin_ldexpf(acc[c][i] * g, (int)(unit - h)) : acc[c][i] * g;
   }
   // their sum over the rows' values, int8 codes: made bf16 in the operand's order
   template <typename Raw>
   __device__ __forceinline__ void values8(float (&pe)[8], const Raw (&v)[8]) {
     bf16x8 p[3];
-    three_terms(pe, p);
+    three_terms<false>(pe, p);
 #pragma unroll
     for (int c = 0; c < VE; ++c) {
       u32x4 av;
@@ -979,9 +1027,10 @@ struct Soft {
     }
   }
   // their sum over the rows' values (two bf16 a word)
+  template <bool INF>
   __device__ __forceinline__ void values(float (&pe)[8], const uint32_t (&vw)[8][VE / 2]) {
     bf16x8 p[3];
-    three_terms(pe, p);
+    three_terms<INF>(pe, p);
 #pragma unroll
     for (int c = 0; c < VE; ++c) {
       const uint32_t sel = (c & 1) ? 0x07060302u : 0x05040100u;
@@ -1042,8 +1091,8 @@ __device__ __forceinline__ void attend_newest(const BlockArgs& a, const BlockSeq
 #pragma unroll
     for (int u = 0; u < VE / 2; ++u) vw[i][u] = v[i][u];
   }
-  o.softmax(x, a.scale2, a.scale2_lo, kDown, pe);
-  o.values(pe, vw);
+  o.template softmax<false>(x, a.scale2, a.scale2_lo, 1.f, pe);
+  o.template values<true>(pe, vw);
 }
 
 // The 32-row steps [first, end) of a unit's blocks (those listed, or all), by one wave for
@@ -1149,7 +1198,7 @@ __device__ __forceinline__ void attend_blocks(const BlockArgs& a, int b, int g, 
     // only
     if (!AHEAD) load_v(r, v);
     VRaw nv[8];
-    const float xs = a.scale2 * xk, xlo = a.scale2_lo * xk, vs = xv * kDown;
+    const float xs = a.scale2 * xk, xlo = a.scale2_lo * xk, vs = xv;
     u32x4 n0[NK], n1[NK];
     more = next();
     if (more) {
@@ -1178,7 +1227,7 @@ __device__ __forceinline__ void attend_blocks(const BlockArgs& a, int b, int g, 
     }
     const float x[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
     float pe[8];
-    o.softmax(x, xs, xlo, vs, pe);
+    o.template softmax<KIND != kRowsBf16>(x, xs, xlo, vs, pe);
     if constexpr (KIND == kRowsInt8) {
       o.values8(pe, v);
     } else {
@@ -1197,7 +1246,7 @@ __device__ __forceinline__ void attend_blocks(const BlockArgs& a, int b, int g, 
           }
         }
       }
-      o.values(pe, vw);
+      o.template values<KIND == kRowsBf16>(pe, vw);
     }
 #pragma unroll
     for (int j = 0; j < NK; ++j) {
@@ -1239,11 +1288,11 @@ __global__ __launch_bounds__(64) void block_attn(BlockArgs a) {
     attend_blocks<D, KIND, NT, false>(a, c.b, g, c.slot, a.list ? a.list + (size_t)(c.b * a.Hkv + g) * a.list_ld : nullptr,
                                e0 << (a.block_shift - 5), e1 << (a.block_shift - 5), o);
   }
-  o.lsum += __shfl_xor(o.lsum, 16);
-  o.lsum += __shfl_xor(o.lsum, 32);
+  const float L = o.total();
+  o.template by<KIND != kRowsBf16>(L > 0.f ? 1.f / L : 0.f);
   if (l16 >= a.G) return;
   const size_t pi = (size_t)(w < 0 ? parts * units + item : w) * a.G + l16;  // the units' parts of the newest block, then the items
-  if (lg == 0) a.ml[pi] = make_float2(o.m, o.lsum);
+  if (lg == 0) a.ml[pi] = make_float2(o.m, L);
   float* dst = a.part + pi * D + 4 * lg * VE;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
@@ -1281,10 +1330,10 @@ __global__ __launch_bounds__(64 * kUnitWaves) void block_attn_unit(BlockArgs a) 
   o.init();
   if (s0 < codes)
     attend_blocks<D, KIND, false, true>(a, b, g, s.slot, a.list ? a.list + (size_t)unit * a.list_ld : nullptr, s0, min(s1, codes), o);
+  if (KIND != kRowsBf16 && s0 < codes && codes < s1) o.by_total();
   for (int i = max(s0, codes); i < s1; ++i) attend_newest<D, KIND>(a, s, b, g, at, (i - codes) * 32, o);
-  o.lsum += __shfl_xor(o.lsum, 16);
-  o.lsum += __shfl_xor(o.lsum, 32);
-  if (lg == 0) mls[w][l16] = make_float2(o.m, o.lsum);
+  const float mine = o.total();
+  if (lg == 0) mls[w][l16] = make_float2(o.m, mine);
   __syncthreads();
   float M = -INFINITY, L = 0.f;
 #pragma unroll
@@ -1294,9 +1343,7 @@ __global__ __launch_bounds__(64 * kUnitWaves) void block_attn_unit(BlockArgs a) 
     const float2 v = mls[i][l16];
     if (v.x != -INFINITY) L = fmaf(fast_exp2(v.x - M), v.y, L);
   }
-  const float f = o.m == -INFINITY ? 0.f : fast_exp2(o.m - M) * (L > 0.f ? 1.f / L : 0.f);
-#pragma unroll
-  for (int c = 0; c < VE; ++c) o.acc[c] *= f;
+  o.template by<KIND != kRowsBf16>(o.m == -INFINITY ? 0.f : fast_exp2(o.m - M) * (L > 0.f ? 1.f / L : 0.f));
   // the upper half of the waves hand theirs to the lower, until one has the sum
 #pragma unroll
   for (int half = W / 2; half >= 1; half /= 2) {
@@ -1325,7 +1372,7 @@ __global__ __launch_bounds__(64 * kUnitWaves) void block_attn_unit(BlockArgs a) 
     for (int e = 0; e < 4; ++e)
 #pragma unroll
       for (int c = 0; c < VE; c += 4) {
-        const f32x4 v = f32x4{o.acc[c][e], o.acc[c + 1][e], o.acc[c + 2][e], o.acc[c + 3][e]} * kUp;
+        const f32x4 v = f32x4{o.acc[c][e], o.acc[c + 1][e], o.acc[c + 2][e], o.acc[c + 3][e]};
         if (a.out_bf16)
           *(u32x2*)((uint16_t*)a.out + oi + e * VE + c) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
         else
@@ -1352,12 +1399,12 @@ __global__ __launch_bounds__(kJoinThreads) void block_join(BlockArgs a) {
   auto place = [&](int i) { return (size_t)(i < parts ? parts * unit + i : first + i) * a.G + h; };
   // the first partials of the thread are in flight with the references
   f32x4 held[kHeld];
-  float mheld[kHeld];
+  float2 mheld[kHeld];
 #pragma unroll
   for (int j = 0; j < kHeld; ++j) {
     const size_t pi = place(min(cl + j * CL, items - 1));
     held[j] = *(const f32x4*)(a.part + pi * D + 4 * dg);
-    mheld[j] = a.ml[pi].x;
+    mheld[j] = a.ml[pi];
   }
   float m = -INFINITY, l = 0.f;
   for (int i = lane; i < items; i += 64) {
@@ -1371,23 +1418,23 @@ __global__ __launch_bounds__(kJoinThreads) void block_join(BlockArgs a) {
   for (int x = 32; x >= 1; x >>= 1) M = fmaxf(M, __shfl_xor(M, x));
   const float L = warp_sum(m == -INFINITY ? 0.f : l * fast_exp2(m - M));
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  // (an item without a row holds zeros)
-  auto add = [&](f32x4 v, float mi) { o += v * (mi == -INFINITY ? 0.f : fast_exp2(mi - M)); };
+  // the items' means by their shares: finite where the mean of all is (an item without a row
+  // holds zeros)
+  const float each = L > 0.f ? 1.f / L : 0.f;
+  auto add = [&](f32x4 v, float2 i) { o += v * (i.x == -INFINITY ? 0.f : fast_exp2(i.x - M) * i.y * each); };
 #pragma unroll
   for (int j = 0; j < kHeld; ++j)
     if (cl + j * CL < items) add(held[j], mheld[j]);
 #pragma unroll 4
   for (int i = cl + kHeld * CL; i < items; i += CL) {
     const size_t pi = place(i);
-    add(*(const f32x4*)(a.part + pi * D + 4 * dg), a.ml[pi].x);
+    add(*(const f32x4*)(a.part + pi * D + 4 * dg), a.ml[pi]);
   }
   sacc[t] = o;
   __syncthreads();
   if (cl) return;
 #pragma unroll
   for (int i = 1; i < CL; ++i) o += sacc[dg + DG * i];
-  o *= L > 0.f ? 1.f / L : 0.f;
-  o *= kUp;
   const size_t oi = (size_t)bh * D + 4 * dg;
   if (a.out_bf16)
     *(u32x2*)((uint16_t*)a.out + oi) = u32x2{f32_to_bf16_bits(o[0]) | (f32_to_bf16_bits(o[1]) << 16),
