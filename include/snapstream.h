@@ -532,16 +532,17 @@ typedef struct {
  * one that wants more than max_pages is not and does not count.
  *   short_out [n] int32: the pages b lacks (0: served), optional.
  * Sequences with a slot id out of range or rows[slot] < 0 are skipped (short 0).
- * The slots must be distinct (a slot named twice gets the pages of the longer wish
- * once, but short_out then tells of one of the two).  One workgroup: a call is a few
- * microseconds, 20 where it hands out 48000 pages. */
+ * A slot named again is served as by a call of its own behind: the sequence lacks what
+ * those before it left it to lack.  One workgroup: a call is a few microseconds, 20 where
+ * it hands out 48000 pages, and longer where it names a slot twice. */
 snap_status snap_pages_reserve(const snap_page_pool* pool, const int32_t* rows, int32_t n, const int32_t* slot_ids,
                                const int32_t* lengths, int32_t len, int32_t* short_out, void* stream);
 
 /* Takes back the pages behind the rows[slot] rows that each slot holds (all of them
  * where that is 0 or less): their entries become -1, and they go to the end of the
  * free list in the order that undoes snap_pages_reserve.  After an eviction, or with
- * rows = 0 at a sequence's end.  (A slot named twice gives them once.) */
+ * rows = 0 at a sequence's end.  (A slot named twice gives them once, where it is named
+ * last.) */
 snap_status snap_pages_release(const snap_page_pool* pool, const int32_t* rows, int32_t n, const int32_t* slot_ids,
                                void* stream);
 

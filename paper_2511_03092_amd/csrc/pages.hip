@@ -10,6 +10,7 @@
 // All are bound by latency: a handful of dependent loads, no more than 12 bytes a
 // token written.  One token each of 64 sequences 3 us a call; 24 prompts of up to 32k
 // tokens (6200 pages of 64) 6.5 us, and about 20 for 48000 pages, by what one CU stores.
+#include "lds_dma.h"
 #include "snap_internal.h"
 
 namespace snap {
@@ -62,12 +63,32 @@ __device__ __forceinline__ int find_last(const int* at, int x) {
 
 __device__ __forceinline__ int clamp_int(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
 
+// Whether the workgroup's threads name a slot (>= 0) twice, by a table of open addresses in
+// LDS (all its entries -1 before, at a barrier).
+constexpr int kSeen = 2 * kPoolThreads;
+__device__ __forceinline__ void note_slot(int* seen, int* twice, int slot) {
+  if (slot < 0) return;
+  uint32_t at = ((uint32_t)slot * 2654435761u) >> 21;  // (half full at most: a free entry is met)
+  for (;; at = (at + 1) & (kSeen - 1)) {
+    const int was = atomicCAS(&seen[at], -1, slot);
+    if (was == -1) return;
+    if (was == slot) {
+      *twice = 1;
+      return;
+    }
+  }
+}
+
 // Sequence t of a chunk is thread t.  Where all sequences of the chunk before it fit,
 // so do their pages' ranks: page e of the chunk is rank e of those taken.
+// A slot named again: pages are handed out up to some sequence and to none behind it.  Up
+// to there all earlier wishes of the slot were granted, so that the sequence lacks what its
+// own exceeds the largest of them by; behind it is served only if the slot holds enough.
+// (A search of the chunk for each sequence, where a slot is named twice.)
 __global__ __launch_bounds__(kPoolThreads) void pages_reserve(PoolArgs a) {
   __shared__ int64_t red[kPoolWaves];
   __shared__ int first[kPoolThreads], to[kPoolThreads];  // rank of a sequence's first page, its table entry less that rank
-  __shared__ int slots[kPoolThreads];
+  __shared__ int slots[kPoolThreads], wants[kPoolThreads], seen[kSeen], twice;
   const int t = tid();
   const int free0 = clamp_int(*a.n_free, 0, a.n_pages);
   int64_t before = 0;  // pages lacked by the chunks before
@@ -75,25 +96,49 @@ __global__ __launch_bounds__(kPoolThreads) void pages_reserve(PoolArgs a) {
   for (int b0 = 0; b0 < a.n; b0 += kPoolThreads) {
     const int b = b0 + t;
     int slot = b < a.n ? a.slot_ids[b] : -1;
-    if (slot < 0 || slot >= a.n_slots) slot = -1;
-    const int r = slot >= 0 ? a.rows[slot] : -1;
     const int add = b < a.n ? (a.lengths ? a.lengths[b] : a.len) : 0;
+    for (int i = t; i < kSeen; i += kPoolThreads) seen[i] = -1;
+    if (t == 0) twice = 0;
+    if (slot < 0 || slot >= a.n_slots) slot = -1;
+    const int r = slot >= 0 ? a.rows[slot] : -1, held = slot >= 0 ? a.held[slot] : 0;
+    lds_barrier();  // (the loads stay in flight)
+    note_slot(seen, &twice, slot);
+    const int h0 = clamp_int(held, 0, a.max_pages);
     const int64_t want = ((int64_t)(r < 0 ? 0 : r) + (add < 0 ? 0 : add) + (1 << a.page_shift) - 1) >> a.page_shift;
     const bool fits = want <= a.max_pages, live = slot >= 0 && r >= 0;
-    // (claimed at once, so that a slot named twice lacks its pages once)
-    const int was = !live ? 0 : (fits ? atomicMax(&a.held[slot], (int)want) : a.held[slot]), h = clamp_int(was, 0, a.max_pages);
-    const int64_t lack = live && want > h ? want - h : 0;
+    slots[t] = slot;
+    wants[t] = live && fits ? (int)want : 0;
+    lds_barrier();
+    const bool again = twice != 0;
+    // the most of the wishes of this slot, before this one or of all, and what the slot holds
+    auto most = [&](int upto) {
+      int h = h0;
+      for (int i = 0; i < upto; ++i)
+        if (slots[i] == slot) h = max(h, wants[i]);
+      return h;
+    };
+    int h = again && live ? most(t) : h0;
+    int64_t lack = live && want > h ? want - h : 0;
     int64_t total;
     const int64_t upto = before + group_scan<kPoolWaves>(fits ? (int)lack : 0, red, total);
-    const bool served = fits && (lack == 0 || upto <= free0);
-    if (b < a.n && a.short_out) a.short_out[b] = served ? 0 : (int)(lack < 0x7fffffff ? lack : 0x7fffffff);
+    bool served = fits && (lack == 0 || upto <= free0), last = true;
     const int take = served ? (int)lack : 0;
     int64_t chunk;
     const int rank = (int)group_scan<kPoolWaves>(take, red, chunk) - take;
+    if (again) {  // by the wishes that were granted
+      wants[t] = take ? (int)want : 0;
+      __syncthreads();
+      if (live) {
+        h = most(t);
+        lack = want > h ? want - h : 0;
+        served = fits && (take || lack == 0);
+        last = take && (int)want == most(kPoolThreads);
+      }
+    }
+    if (b < a.n && a.short_out) a.short_out[b] = served ? 0 : (int)(lack < 0x7fffffff ? lack : 0x7fffffff);
+    if (take && last) a.held[slot] = (int)want;
     first[t] = rank;
     to[t] = h - rank;
-    slots[t] = slot;
-    if (lack && fits && !served) a.held[slot] = h;
     __syncthreads();
     for (int e0 = t; e0 < (int)chunk; e0 += kAtOnce * kPoolThreads) {
       int page[kAtOnce], s[kAtOnce];
@@ -117,29 +162,33 @@ __global__ __launch_bounds__(kPoolThreads) void pages_reserve(PoolArgs a) {
 // order in which pages_reserve would take them again.
 __global__ __launch_bounds__(kPoolThreads) void pages_release(PoolArgs a) {
   __shared__ int64_t red[kPoolWaves];
-  __shared__ int first[kPoolThreads], from[kPoolThreads], slots[kPoolThreads];
+  __shared__ int first[kPoolThreads], from[kPoolThreads], slots[kPoolThreads], seen[kSeen], twice;
   const int t = tid();
   int64_t end = clamp_int(*a.n_free, 0, a.n_pages);
   for (int b0 = (a.n - 1) / kPoolThreads * kPoolThreads; b0 >= 0; b0 -= kPoolThreads) {
     const int b = b0 + t;
     int slot = b < a.n ? a.slot_ids[b] : -1;
     if (slot < 0 || slot >= a.n_slots) slot = -1;
-    int keep = 0, give = 0;
-    if (slot >= 0) {
-      const int r = a.rows[slot];
-      const int k = (int)(((int64_t)(r < 0 ? 0 : r) + (1 << a.page_shift) - 1) >> a.page_shift);
-      // (claimed at once, so that a slot named twice gives its pages once)
-      const int h = clamp_int(atomicMin(&a.held[slot], k), 0, a.max_pages);
-      keep = min(k, h);
-      give = h - keep;
-    }
+    for (int i = t; i < kSeen; i += kPoolThreads) seen[i] = -1;
+    if (t == 0) twice = 0;
+    slots[t] = slot;
+    const int r = slot >= 0 ? a.rows[slot] : 0, held = slot >= 0 ? a.held[slot] : 0;
+    lds_barrier();  // (the loads stay in flight)
+    note_slot(seen, &twice, slot);
+    const int h = clamp_int(held, 0, a.max_pages);
+    lds_barrier();
+    const int keep = min((int)(((int64_t)(r < 0 ? 0 : r) + (1 << a.page_shift) - 1) >> a.page_shift), h);
+    int give = h - keep;
+    if (twice)  // (the last of those that name the slot)
+      for (int i = t + 1; i < kPoolThreads; ++i)
+        if (slots[i] == slot) give = 0;
     int64_t all, chunk;
     // more than there are pages would be entries that were handed back twice: left out
     if (end + group_scan<kPoolWaves>(give, red, all) > a.n_pages) give = 0;
     const int rank = (int)group_scan<kPoolWaves>(give, red, chunk) - give, m = (int)chunk;
+    if (give) a.held[slot] = keep;
     first[t] = rank;
     from[t] = keep - rank;
-    slots[t] = slot;
     __syncthreads();
     for (int e0 = t; e0 < m; e0 += kAtOnce * kPoolThreads) {
       int32_t* at[kAtOnce];
