@@ -175,6 +175,38 @@ def test_probabilities_lose_no_bits_before_the_values(kv, d, block, page, length
         assert err <= tol, (err / U, tol / U)
 
 
+@pytest.mark.parametrize("newest", [False, True], ids=["codes", "newest"])
+@pytest.mark.parametrize("length", [84, 2000])
+@pytest.mark.parametrize("kv,d,block", [("i8", 128, 64), ("fp8", 64, 64), ("bf16", 128, 64), ("i8", 64, 32), ("fp8", 128, 32),
+                                        ("bf16", 64, 32)])
+def test_two_terms_of_a_probability_would_show(kv, d, block, length, newest):
+    """Nine rows of one 32-row step share the softmax: one of logit 0 and eight whose probability beside it is half of
+    1 + 2^-9 + 2^-17 - 2^-21.  Two terms of 8 bits, cut off or rounded to nearest, miss that by 2^-17 - 2^-21, 120 u, in eight
+    of ten parts of the sum: 96 u.  Nine terms have eight additions that are not of zeros, in each sum: with 18 u as above
+    34 u.  Values are the type's largest code, whose scale is one to a rounding."""
+    print(f"\n[case] {kv} d {d} block {block}, nine of {length} rows, newest {newest}", flush=True)
+    p = params(4, 2, d, kv)
+    c = Blocks(p, kv, block, block, [length], 1, bounds=False)
+    top = {"i8": 127.0, "fp8": 448.0, "bf16": 1.0}[kv]
+    k = torch.zeros((1, 2, length, d), dtype=torch.bfloat16)
+    k[..., d - 4] = 1.0  # without a share
+    at = (length - 1) // 32 * 32 if newest else length // 2 // 32 * 32
+    assert newest == (at >= (length - 1) // block * block) and at + 9 <= length
+    k[:, :, at:at + 9, d - 4] = 0.0
+    k[:, :, at + 1:at + 9, d - 3:] = 1.0
+    _load(c, [0], [length], 1, like=(k, torch.full_like(k, top)))
+    c.rows -= 1
+    rest = math.log(0.5 * (1 + 2.0 ** -9 + 2.0 ** -17 - 2.0 ** -21)) * math.sqrt(d)
+    q = torch.zeros((1, 4, d), dtype=torch.bfloat16)
+    q[..., d - 4] = -300.0 * math.sqrt(d)
+    for i in range(3):  # to 24 bits
+        q[..., d - 3 + i] = rest
+        rest -= float(q[0, 0, d - 3 + i])
+    out, _ = _call(c, [0], q.cuda(), max_rows=length, dtype=torch.float32)
+    err = float((out.double() / top - 1).abs().max())
+    assert err <= 34 * U, err / U
+
+
 # ---------------------------------------------------------------- infinities and NaN
 def _special(kv, length, marks, select=False, keys=(), newest=()):
     """Attention with single values (row, dim, what) and keys replaced, outputs and the definition's in float64."""
