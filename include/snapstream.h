@@ -636,15 +636,18 @@ size_t snap_block_decode_workspace(const snap_params* p, int32_t n, int32_t max_
  * their codes, its own by its rows as they came.
  * Values of every size carry the errors of fp32 sums.  Rows whose share of the
  * softmax is below 2^-120 may count as none; an infinite value makes its dim of out
- * infinite, or NaN beside one of the other sign or where its share is below 2^-90.
+ * infinite, or NaN beside one of the other sign or where its share is below 2^-80.
  * select = 1: over the new token's block and, of the blocks before it,
  *   those with one of the first `sink` rows or of the last `recent` ones, and
  *   the ceil(topk / block) others of the largest score (equal scores: the lower
  *   block),
- * for each KV head.  The score is an upper bound of what a query of the KV head's
- * group may have in a block, formed in whole numbers: with a query's codes a_d =
+ * for each KV head.  The score estimates the largest product that a query of the KV
+ * head's group may have in a block, formed in whole numbers: with a query's codes a_d =
  * round(q_d / u), u its scale (as a block's in int8), and the block's bounds,
  *   score = bound_scale * max_h u_h * sum_d (a_d > 0 ? a_d largest_d : a_d least_d).
+ * It is an upper bound for the rounded query alone: a product q.k may exceed it by half
+ * a code's step a dim, u / 2 sum_d |k_d|, by the roundings of fp32 (bounds beyond +-127
+ * are clamped), and where keys are infinite (they count as 127 * bound_scale).
  * max_rows (host, at most max_pages * page_size) bounds the rows of every sequence;
  * one that holds more attends those of its whole blocks that lie below max_rows.
  * select needs bounds and at most 32768 blocks (SNAP_ERR_UNSUPPORTED above).
