@@ -105,6 +105,34 @@ def test_blocks_of_unequal_size(kv, spread):
         _check(c, slots, [lengths[s] - 1 for s in slots], q[:len(slots)], out)
 
 
+@pytest.mark.parametrize("whole,newest", [(1e-30, 1.0), (1e30, 1.0), (1.0, 1e-30), (1.0, 1e30), (1e-20, 1e15), (1e37, 1e-30)])
+@pytest.mark.parametrize("kv,d", [("i8", 128), ("fp8", 64), ("bf16", 64)])
+def test_the_newest_block_beside_blocks_of_another_size(kv, d, whole, newest):
+    """A wave that goes from codes to rows as they came, and back to none; the newest block's rows with most of the sum, and
+    with little of it."""
+    print(f"\n[case] {kv} d {d}: whole blocks times {whole}, the newest times {newest}", flush=True)
+    p = params(4, 2, d, kv, sm_scale=1.0)
+    lengths = [300, 300, 45, 4127]
+    c = Blocks(p, kv, 32, 64, lengths, 1, bounds=False)
+    g = torch.Generator().manual_seed(8)
+    k = (_rand(g, 4, 2, 4127, d, spread=False).float() / 16).bfloat16()
+    v = 0.05 + _rand(g, 4, 2, 4127, d).float().abs()
+    for b, n in enumerate(lengths):
+        tail = slice((n - 1) // 32 * 32, n)
+        v[b] *= whole
+        v[b, :, tail] *= newest / whole
+        k[b, :, tail, 5] = 4.0 if b % 2 else -4.0
+    v = v.bfloat16()
+    _load(c, [0, 1, 2, 3], lengths, 3, like=(k, v))
+    c.rows -= 1
+    q = (_rand(g, 4, 4, d, spread=False).float() / 16).bfloat16()
+    q[..., 5] = 4.0
+    q = q.cuda()
+    for slots in ([0, 1, 2], [0, 1, 2, 3]):
+        out, _ = _call(c, slots, q[:len(slots)], max_rows=300 if len(slots) == 3 else None, dtype=torch.float32)
+        _check(c, slots, [lengths[s] - 1 for s in slots], q[:len(slots)], out)
+
+
 @pytest.mark.parametrize("kv", ["i8", "fp8", "bf16"])
 @pytest.mark.parametrize("big", [1e20, 1e30, 1e37])
 @pytest.mark.parametrize("first", [True, False], ids=["first", "last"])
@@ -289,8 +317,8 @@ def test_an_infinite_value_without_a_share_is_no_number_less(length):
     g = torch.Generator().manual_seed(7)
     k, v = _rand(g, 1, 1, length, 64, spread=False), _rand(g, 1, 1, length, 64, spread=False)
     k[..., 0] = 0.0
-    k[0, 0, 50, 0], k[0, 0, 51, 0], k[0, 0, 52, 0] = -40.0, -16.0, -1.5
-    v[0, 0, 50, 1], v[0, 0, 51, 2], v[0, 0, 52, 3] = math.inf, math.inf, -math.inf
+    k[0, 0, 50, 0], k[0, 0, 51, 0], k[0, 0, 52, 0], k[0, 0, 53, 0] = -40.0, -16.0, -1.5, -6.0
+    v[0, 0, 50, 1], v[0, 0, 51, 2], v[0, 0, 52, 3], v[0, 0, 53, 0] = math.inf, math.inf, -math.inf, math.inf
     _load(c, [0], [length], 1, like=(k, v))
     c.rows -= 1
     q = torch.zeros((1, 2, 64), dtype=torch.bfloat16)
@@ -298,5 +326,5 @@ def test_an_infinite_value_without_a_share_is_no_number_less(length):
     out, _ = _call(c, [0], q.cuda(), max_rows=length, dtype=torch.float32)
     out = out[0].cpu()
     assert not torch.isfinite(out[:, 1]).any() and not torch.isfinite(out[:, 2]).any()
-    assert (out[:, 3] == -math.inf).all()  # its share is e^-12
-    assert torch.isfinite(out[:, 4:]).all() and torch.isfinite(out[:, 0]).all()
+    assert (out[:, 3] == -math.inf).all() and (out[:, 0] == math.inf).all()  # shares of e^-12 and e^-48 beside rows of one
+    assert torch.isfinite(out[:, 4:]).all()
