@@ -485,7 +485,10 @@ struct BlockAppend {
 // (8 bits, where that is not the last one) the last block's rows into the tail, stored
 // after the barrier, behind which nobody reads the tail's old rows any more; workgroup x:
 // blocks 2 x - 1 and 2 x.  HBM bound: four prompts of 32k tokens or fewer out of the packed
-// projection into int8 (465 MB) 103 us, 4.5 TB/s (a copy: 4.7 to 4.9).
+// projection into int8 (465 MB) 100 us, 4.6 TB/s (a copy: 4.7 to 4.9), without bounds 99;
+// bf16 with bounds (618 MB) 137, without 129.  Short calls, 16 chunks of up to 512 64-wide
+// rows into E4M3: 9.8 us, of which bounds 2.5 (joins over the lanes, then 16 divisions in
+// D / 8 of them), scales and codes 1.1.
 template <int D, int KIND, int B>
 __global__ __launch_bounds__(256) void block_append(BlockAppend p) {
   const BlockArgs& a = p.c;
@@ -1103,7 +1106,7 @@ __device__ __forceinline__ void attend_newest(const BlockArgs& a, const BlockSeq
 // product takes from it; its keys are 16 bytes at byte 64 j + 16 lg of row l16, its values
 // the D / 16 dims from (D / 16) l16 of eight rows.  Every row of a whole block is there, so
 // nothing is masked.  HBM bound: 8 sequences of 4k to 128k int8 rows x 8 KV heads (1.26 GB)
-// 200 us, 6.2 TB/s with the join; 32 of up to 16k E4M3 rows (554 MB) 99 us.
+// 203 us, 6.2 TB/s with the join; 32 of up to 16k E4M3 rows (554 MB) 100 us.
 // AHEAD: the values are loaded a step before they are needed, as the keys are; that changes
 // nothing where the card is full of waves.
 template <int D, int KIND, bool NT, bool AHEAD>
@@ -1525,14 +1528,20 @@ BlockGeometry block_geometry(const snap_params& p, int n, int max_rows, int bloc
 // or by the one workgroup that chooses among them.  That one takes in 30 to 50 bytes a
 // nanosecond; the launch costs 3 to 5 us.  Whole calls, 8 KV heads, one launch / two, us:
 //   bounds a unit           128 KB      256 KB      512 KB      1 MB
-//   d 128     1 sequence   18.7/20.9   21.8/21.8   26.8/22.9   36.4/24.2
-//             4            21.2/23.5   24.4/24.6   30.5/25.9   41.7/31.5
-//            16            29.4/31.4   33.5/36.1   40.3/48.4   57.2/60.7
-//            32            43.6/47.3   49.4/60.8   63.9/72.9   95.4/97.7
-//   d 64      1            19.8/23.2   24.0/23.9   30.4/25.4
-//             4            22.2/25.2   26.1/27.2   34.5/28.6
-//            16            27.0/30.5   31.8/34.8   42.3/42.8
-//            32            33.5/37.1   41.4/44.8   61.4/58.4
+//   d 128     1 sequence   19.1/20.6   22.0/21.6   26.9/22.4   36.5/24.3
+//             4            21.8/23.8   24.7/24.8   31.6/26.6   43.7/32.4
+//             8            24.8/27.0   28.2/28.7   34.4/33.0   46.7/44.3
+//            12            27.5/30.0   30.9/33.6   37.6/39.4   50.9/52.9
+//            16            30.2/33.1   33.9/37.1   42.0/49.1   58.4/61.4
+//            32            46.0/49.9   50.5/61.6   64.8/73.2   97.3/99.7
+//   d 64      1            19.1/21.4   22.8/22.2   30.2/23.7
+//             4            21.3/23.9   25.6/25.6   36.1/28.0
+//             8            23.5/26.0   29.1/28.1   38.5/33.1
+//            12            26.0/28.3   30.8/32.5   41.1/38.7
+//            16            26.8/29.9   32.6/34.4   43.3/42.9
+//            32            34.0/37.6   41.8/45.4   62.0/59.1
+// (Where the rule takes one, 64-wide rows are 1 to 6% faster by two at 512 KB from 12
+// sequences on, and 3% at 256 KB of one or eight.)
 // (Past 8192 blocks the one that scores would not have its keys in LDS.)
 static bool scored_apart(const snap_params& p, int units, int blocks) {
   return units <= 64 ? (size_t)blocks * 2 * p.d_qk >= (size_t)512 << 10 : blocks > 4096;
@@ -1544,18 +1553,27 @@ static bool scored_apart(const snap_params& p, int units, int blocks) {
 // (then nothing is written for the join).  Measured, one launch / two, 32 query heads on 8,
 // us of a replayed call:
 //   rows                250         500        1000        2000        3900
-//   128 int8   1 x   8.7/9.7   10.4/9.7   14.0/9.8   20.7/10.2   33.6/11.3
-//             16     8.8/10.6  10.5/11.6  14.8/14.8  21.7/20.8   35.0/30.0
-//             32     8.8/12.5  11.3/15.7  17.5/22.0  26.7/31.1   46.0/52.7
-//             64    17.8/18.2  23.9/23.9  33.4/33.5  52.1/56.7   103/92.5
-//   128 bf16   1     8.8/9.1   10.9/9.2   16.3/9.2   24.2/9.7    40.8/11.0
-//             16     8.7/10.2  11.3/12.8  17.8/19.0  26.5/28.4   44.5/48.3
-//             32     9.6/13.2  15.9/19.5  25.2/29.5  43.2/50.6   92.4/90.3
-//             64    21.1/20.8  29.8/32.1  48.4/54.1  99.0/93.0   181/166
-//   64 int8    1     6.4/8.2    7.7/8.2    9.9/8.4   14.6/8.8    23.5/10.8
-//             16     6.5/9.4    7.8/10.4  10.0/12.4  15.5/15.0   24.8/19.6
-//             32     6.6/10.9   7.9/13.0  10.8/15.5  16.6/20.4   25.9/28.6
-//             64     8.3/14.5  11.0/17.2  17.9/22.0  27.5/31.1   45.5/52.4
+//   128 int8   1 x   8.8/10.1  10.4/10.1  14.1/10.2  20.5/10.6   33.2/11.9
+//             16     9.0/11.5  11.5/12.6  15.9/16.4  22.4/21.5   36.1/30.2
+//             32    10.5/13.2  13.6/16.7  18.3/22.2  28.5/32.5   54.1/53.1
+//             64    19.0/19.0  24.6/24.6  34.4/35.0  60.4/58.2    104/94.4
+//   128 bf16   1     8.7/9.6   11.0/9.6   16.9/9.7   24.6/10.3   41.4/12.3
+//             16     9.5/11.6  12.8/14.4  19.1/19.7  28.3/30.8   59.3/49.1
+//             32    11.8/14.4  16.4/20.0  25.7/32.5  51.6/51.1   94.4/91.1
+//             64    21.3/21.7  30.4/34.6  57.9/54.8   100/94.7    182/168
+//   64 int8    1     6.5/8.5    8.1/8.6   10.2/8.6   14.8/9.0    23.5/11.1
+//             16     6.6/9.7    8.3/11.0  11.2/12.7  16.5/15.5   25.3/20.3
+//             32     6.8/11.5   9.2/13.5  12.8/16.0  17.6/20.6   26.9/29.7
+//             64     9.5/15.4  13.7/18.1  18.9/22.6  28.5/32.2   54.0/53.2
+//   64 bf16    1     6.7/8.4    8.2/8.5   11.1/8.6   16.1/8.9    26.2/11.2
+//             16     6.9/9.8    8.7/11.3  12.7/14.8  17.9/19.4   28.7/28.0
+//             32     7.7/11.8  11.5/15.7  16.3/19.9  24.9/29.1   49.2/49.1
+//             64    11.4/17.7  16.6/22.7  25.3/31.8  50.3/55.0   91.4/95.1
+// Against the rule, by 4 to 9%: 1000 (bf16) and 2000 128-wide rows of 64 sequences, which
+// two launches take faster; 2000 bf16 rows of 16 sequences and 3900 64-wide ones of 64,
+// which one does.
+// The rule goes by the bound of the rows, not by the rows that are there: a far one takes
+// two launches.
 // (calls that are not replayed cost the host 9 us with one launch, 11 with two)
 static bool whole_units(const snap_params& p, int units, int blocks, int block) {
   const int row_bytes = 2 * p.d_qk * (p.kv_dtype == SNAP_BF16 ? 2 : 1);
