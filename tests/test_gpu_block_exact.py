@@ -203,6 +203,32 @@ def test_probabilities_lose_no_bits_before_the_values(kv, d, block, page, length
         assert err <= tol, (err / U, tol / U)
 
 
+@pytest.mark.parametrize("kv,d,block", [("i8", 128, 64), ("fp8", 64, 32), ("bf16", 128, 64), ("bf16", 64, 32)])
+@pytest.mark.parametrize("length", [20, 300, 5000, 70000])
+@pytest.mark.parametrize("rising", [False, True], ids=["any", "rising"])
+def test_the_largest_values_stay_finite(kv, d, block, length, rising):
+    """Every value is the largest of bf16, of either sign by its dim; logits in any order, or rising by less than what the
+    reference lags behind for many rows at a time (e^5 within 2^8)."""
+    print(f"\n[case] {kv} d {d} block {block}, {length} rows of the largest value, rising {rising}", flush=True)
+    p = params(2, 1, d, kv, sm_scale=1.0)
+    c = Blocks(p, kv, block, 128, [length], 1, bounds=False)
+    g = torch.Generator().manual_seed(9)
+    k = (_rand(g, 1, 1, length, d, spread=False).float() / 16).bfloat16()
+    if rising:
+        k[0, 0, :, 0] = 5.0 * torch.arange(length) / length
+    v = torch.full((1, 1, length, d), torch.finfo(torch.bfloat16).max, dtype=torch.bfloat16)
+    v[..., ::2] *= -1
+    _load(c, [0], [length], 1, like=(k, v))
+    c.rows -= 1
+    q = (_rand(g, 1, 2, d, spread=False).float() / 16).bfloat16()
+    q[..., 0] = 1.0
+    for dtype in (torch.float32, torch.bfloat16):
+        out, _ = _call(c, [0], q.cuda(), max_rows=length, dtype=dtype)
+        rel = (out.double().cpu() / v[0, 0, 0].double() - 1).abs()
+        # as for values of one: the same probabilities in both sums, 18 u beside the additions
+        assert float(rel.max()) <= (2 * (length / 32 + 37) + 18) * U + (0.0 if dtype == torch.float32 else 2.0 ** -8)
+
+
 @pytest.mark.parametrize("newest", [False, True], ids=["codes", "newest"])
 @pytest.mark.parametrize("length", [84, 2000])
 @pytest.mark.parametrize("kv,d,block", [("i8", 128, 64), ("fp8", 64, 64), ("bf16", 128, 64), ("i8", 64, 32), ("fp8", 128, 32),
